@@ -215,6 +215,48 @@ int eg_mla_step(const eg_mla_dims* dims, void* c_pool, void* krope_pool, int32_t
                 const void* w_uv, void* out, int32_t num_splits, void* workspace,
                 size_t workspace_bytes, int32_t* dev_status, void* stream);
 
+/*
+ * eg_mla_decode_shared - one decode step of sequences that share a prefix: a
+ * system prompt, a document, or the prompt that several answers are drawn from.
+ *
+ * Sequence b's cached tokens are the prefix's T = *prefix_len tokens followed by
+ * its own seq_lens[b] tokens; the result is eg_mla_decode's over those T +
+ * seq_lens[b] tokens (Eqs. 11-13).  The prefix is read, gated and normalised once
+ * for the whole batch, and the absorbed queries of all sequences meet it as the
+ * rows of one matrix product; the own tokens go through eg_mla_decode's kernel,
+ * and the partial results of both are merged by log-sum-exp.
+ *
+ * Supported: bf16 with d_c in {192, 256}, every gate mode
+ * (EG_MLA_ERR_UNSUPPORTED otherwise).
+ *
+ *   prefix_table    [ceil(max_prefix_len / page_size)] int32 on the device: the
+ *                   prefix's physical pages in order (may be NULL with
+ *                   max_prefix_len 0)
+ *   prefix_len      one int32 on the device, 0 .. max_prefix_len: its tokens.  Any
+ *                   length: a sequence's own tokens begin in a page of its own
+ *   max_prefix_len  host-side bound of *prefix_len
+ *   block_table, max_pages_per_seq, seq_lens, max_seq_len: of the own tokens (0
+ *                   and more per sequence; the one just appended is an own token)
+ *   num_splits      as for eg_mla_decode; the prefix is divided likewise
+ *   the others      as for eg_mla_decode
+ *   workspace       >= eg_mla_decode_shared_workspace_size(dims, batch,
+ *                   max_prefix_len, num_splits) bytes, 256-byte aligned: that of
+ *                   eg_mla_decode, the gated prefix (with the gate off one page)
+ *                   and the prefix's partial results
+ * A sequence without any token gets u = 0.  Device errors: as for eg_mla_decode;
+ * a *prefix_len outside 0 .. max_prefix_len is reported as
+ * EG_MLA_ERR_OUT_OF_RANGE and taken as the nearer bound.
+ */
+size_t eg_mla_decode_shared_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_prefix_len,
+                                           int32_t num_splits);
+int eg_mla_decode_shared(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
+                         const int32_t* id_pool, const int32_t* prefix_table, const int32_t* prefix_len,
+                         int32_t max_prefix_len, const int32_t* block_table, int32_t max_pages_per_seq,
+                         const int32_t* seq_lens, int32_t max_seq_len, int32_t batch, int32_t num_pages,
+                         const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
+                         const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
+                         int32_t* dev_status, void* stream);
+
 /* Size of the static device scratch array behind eg_mla_decode_static. */
 #define EG_MLA_STATIC_SCRATCH_BYTES ((size_t)16 << 20)
 

@@ -42,6 +42,8 @@ EXPORTED = [
     "eg_mla_decode_workspace_size",
     "eg_mla_decode",
     "eg_mla_decode_static",
+    "eg_mla_decode_shared_workspace_size",
+    "eg_mla_decode_shared",
     "eg_mla_step",
     "eg_mla_decode_r0_workspace_size",
     "eg_mla_decode_r0",
@@ -102,6 +104,11 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.eg_mla_decode.restype = ctypes.c_int
     lib.eg_mla_decode_static.argtypes = [D, P, P, P, P, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P, P]
     lib.eg_mla_decode_static.restype = ctypes.c_int
+    lib.eg_mla_decode_shared_workspace_size.argtypes = [D, I32, I32, I32]
+    lib.eg_mla_decode_shared_workspace_size.restype = SZ
+    lib.eg_mla_decode_shared.argtypes = [D, P, P, P, P, P, P, I32, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P,
+                                         SZ, P, P]
+    lib.eg_mla_decode_shared.restype = ctypes.c_int
     lib.eg_mla_step.argtypes = [D, P, P, P, P, P, P, P, P, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ,
                                 P, P]
     lib.eg_mla_step.restype = ctypes.c_int
@@ -281,6 +288,28 @@ def eg_mla_decode_static(dims: EgMlaDims, q, c_pool, krope_pool, id_pool, block_
         _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk), _ptr(w_uv), _ptr(out), num_splits,
         _ptr(dev_status), _stream(stream))
     _check(code, "eg_mla_decode_static")
+
+
+def eg_mla_decode_shared_workspace_size(dims: EgMlaDims, batch: int, max_prefix_len: int, num_splits: int = 0) -> int:
+    n = load().eg_mla_decode_shared_workspace_size(ctypes.byref(dims), batch, int(max_prefix_len), num_splits)
+    if n == 0:
+        raise EgMlaError(EG_MLA_ERR_UNSUPPORTED, "eg_mla_decode_shared_workspace_size")
+    return int(n)
+
+
+def eg_mla_decode_shared(dims: EgMlaDims, q, c_pool, krope_pool, id_pool, prefix_table, prefix_len, max_prefix_len,
+                         block_table, seq_lens, max_seq_len, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out,
+                         workspace, num_splits=0, dev_status=None, stream=None) -> None:
+    """One decode step of sequences that share a prefix: see include/egmla.h."""
+    if prefix_table is not None and prefix_table.numel() * dims.page_size < max_prefix_len:
+        raise ValueError("prefix_table holds fewer pages than max_prefix_len tokens take")
+    code = load().eg_mla_decode_shared(
+        ctypes.byref(dims), _ptr(q), _ptr(c_pool), _ptr(krope_pool), _ptr(id_pool), _ptr(prefix_table),
+        _ptr(prefix_len), int(max_prefix_len), _ptr(block_table), block_table.shape[1], _ptr(seq_lens),
+        int(max_seq_len), seq_lens.shape[0], c_pool.shape[0], _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta),
+        _ptr(w_uk), _ptr(w_uv), _ptr(out), num_splits, _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream))
+    _check(code, "eg_mla_decode_shared")
 
 
 def make_layer_dims(n_embd: int, rope_theta: float = 10000.0, rms_eps: float = 0.0,

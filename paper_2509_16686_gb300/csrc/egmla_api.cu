@@ -89,6 +89,20 @@ bool encode_absorb_maps(CUtensorMap (&maps)[2], const DecodeArgs& a, int tile) {
          encode_3d(&maps[1], a.q, dn, H, a.batch, qrow, H * qrow, 1, tile);   // q^C: the RoPE part is past the end
 }
 
+// maps of the attention over a shared prefix: {what the latent is read from, its
+// last page, the RoPE keys}, a page per box
+bool encode_shared_maps(CUtensorMap (&maps)[3], const eg_mla_dims* d, const DecodeArgs& a,
+                        const egmla::SharedArgs& sh) {
+  std::memset(maps, 0, sizeof(maps));
+  const uint64_t pool = static_cast<uint64_t>(a.num_pages) * d->page_size, dc = d->d_c, dr = d->d_rope;
+  const uint64_t rows = egmla::shared_z_rows(sh.max_prefix_len, a.gate != 0);
+  const uint32_t cols = static_cast<uint32_t>(dc / 64);
+  const void* z = static_cast<const uint8_t*>(a.workspace) + sh.wl.off_z;
+  return encode_3d(&maps[0], a.gate ? z : a.c_pool, 64, a.gate ? rows : pool, dc / 64, dc, 64, egmla::kPage, cols) &&
+         encode_3d(&maps[1], z, 64, rows, dc / 64, dc, 64, egmla::kPage, cols) &&
+         encode_3d(&maps[2], a.kr_pool, dr, pool, 1, dr, pool * dr, egmla::kPage, 1);
+}
+
 float resolve_scale(const eg_mla_dims* d) {
   return d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / std::sqrt(static_cast<float>(d->d_nope + d->d_rope));
 }
@@ -316,8 +330,35 @@ int fill_append_args(egmla::AppendArgs& a, const eg_mla_dims* dims, void* c_pool
   return EG_MLA_OK;
 }
 
+// a prefix that the batch shares (eg_mla_decode_shared)
+struct Prefix {
+  const int32_t* table;
+  const int32_t* len;
+  int32_t max_len;
+};
+
+// the workspace of eg_mla_decode_shared: eg_mla_decode's, then the prefix's part;
+// EG_MLA_OK or the error code
+int shared_workspace(const eg_mla_dims* d, int32_t batch, int32_t max_prefix_len, int32_t num_splits,
+                     egmla::SharedLayout* out, int32_t* splits) {
+  int rc = check_dims(d);
+  if (rc != EG_MLA_OK) return rc;
+  if (!is_tc_path(d) || !egmla::shared_supported(d->d_c)) return EG_MLA_ERR_UNSUPPORTED;
+  if (batch < 0 || max_prefix_len < 0) return EG_MLA_ERR_INVALID_ARG;
+  // the schedule counts row tiles x pages in 32 bits
+  if ((static_cast<int64_t>(batch) / egmla::kSharedTile + 1) * (max_prefix_len / d->page_size + 1) > INT32_MAX / 2)
+    return EG_MLA_ERR_UNSUPPORTED;
+  rc = resolve_splits(num_splits, splits);
+  if (rc != EG_MLA_OK) return rc;
+  const size_t base = egmla::workspace_layout(batch, *splits, d->num_heads, d->d_c, d->d_rope, true).total;
+  *out = egmla::shared_layout(base, batch, max_prefix_len, *splits, d->num_heads, d->d_c,
+                              d->gate_mode != EG_MLA_GATE_NONE);
+  return EG_MLA_OK;
+}
+
 // eg_mla_decode, preceded by the append of `app` when it is non-null (in the
-// query-absorption kernel's grid).  Every argument is checked before anything is
+// query-absorption kernel's grid), and over the tokens of `prefix` too when that is
+// non-null.  Every argument is checked before anything is
 // launched (`launch` false: checked only).
 int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
                 const int32_t* id_pool, const int32_t* block_table, int32_t max_pages_per_seq,
@@ -325,7 +366,14 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
                 const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
                 const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
                 int32_t* dev_status, const egmla::AppendArgs* app, cudaStream_t st, bool early = false,
-                bool launch = true) {
+                bool launch = true, const Prefix* prefix = nullptr) {
+  egmla::SharedArgs sh;
+  if (prefix != nullptr) {
+    const int rc = shared_workspace(dims, batch, prefix->max_len, num_splits, &sh.wl, &sh.ctas);
+    if (rc != EG_MLA_OK) return rc;
+    if (prefix->len == nullptr || (prefix->table == nullptr && prefix->max_len > 0)) return EG_MLA_ERR_INVALID_ARG;
+    if (workspace_bytes < sh.wl.total) return EG_MLA_ERR_WORKSPACE;
+  }
   DecodeArgs a;
   int rc = fill_decode_args(a, dims, c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens,
                             max_seq_len, batch, num_pages, gate_table, num_splits, workspace, workspace_bytes,
@@ -350,7 +398,22 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     apply_fault(a);
     CUtensorMap amaps[2];
     if (!encode_absorb_maps(amaps, a, egmla::absorb_tile(a.d_c, a.batch))) return EG_MLA_ERR_CUDA;
-    cudaError_t e = egmla::launch_prologue_tc(a, app, amaps, st);
+    egmla::SharedParts parts;
+    CUtensorMap smaps[3];
+    if (prefix != nullptr) {
+      sh.dec = &a;
+      sh.prefix_table = prefix->table;
+      sh.prefix_len = parts.prefix_len = prefix->len;
+      sh.max_prefix_len = parts.max_prefix_len = prefix->max_len;
+      parts.ctas = sh.ctas;
+      parts.ml = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_ml);
+      parts.o = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_o);
+      a.apart = 1;   // the combine has a second list of partials
+      if (prefix->max_len > 0 && !encode_shared_maps(smaps, dims, a, sh)) return EG_MLA_ERR_CUDA;
+    }
+    void* q16 = prefix != nullptr && a.gate_ln ? static_cast<uint8_t*>(workspace) + sh.wl.off_q : nullptr;
+    cudaError_t e = egmla::launch_prologue_tc(a, app, amaps, st, q16);
+    if (e == cudaSuccess && prefix != nullptr && prefix->max_len > 0) e = egmla::launch_shared(sh, smaps, st);
     bool fused = false;
     if (e == cudaSuccess) {
       prof_mark(st, true);
@@ -362,7 +425,7 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       std::memset(&wmap, 0, sizeof(wmap));
       const uint64_t dc = a.d_c, dv = a.d_v;
       if (!encode_3d(&wmap, w_uv, dc, dv, a.H, dc, dv * dc, 128, 1)) return EG_MLA_ERR_CUDA;
-      e = egmla::launch_combine(a, true, &wmap, st);
+      e = egmla::launch_combine(a, true, &wmap, st, prefix != nullptr ? &parts : nullptr);
     }
     return to_status(e);
   }
@@ -478,6 +541,26 @@ int eg_mla_step(const eg_mla_dims* dims, void* c_pool, void* krope_pool, int32_t
   return decode_impl(dims, q, c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens, max_seq_len,
                      batch, num_pages, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace,
                      workspace_bytes, dev_status, &app, static_cast<cudaStream_t>(stream));
+}
+
+size_t eg_mla_decode_shared_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_prefix_len,
+                                           int32_t num_splits) {
+  egmla::SharedLayout wl;
+  int32_t splits = 0;
+  return shared_workspace(dims, batch, max_prefix_len, num_splits, &wl, &splits) == EG_MLA_OK ? wl.total : 0;
+}
+
+int eg_mla_decode_shared(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
+                         const int32_t* id_pool, const int32_t* prefix_table, const int32_t* prefix_len,
+                         int32_t max_prefix_len, const int32_t* block_table, int32_t max_pages_per_seq,
+                         const int32_t* seq_lens, int32_t max_seq_len, int32_t batch, int32_t num_pages,
+                         const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
+                         const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
+                         int32_t* dev_status, void* stream) {
+  const Prefix prefix = {prefix_table, prefix_len, max_prefix_len};
+  return decode_impl(dims, q, c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens, max_seq_len,
+                     batch, num_pages, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace,
+                     workspace_bytes, dev_status, nullptr, static_cast<cudaStream_t>(stream), false, true, &prefix);
 }
 
 int eg_mla_decode_static(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,

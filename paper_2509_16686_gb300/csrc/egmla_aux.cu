@@ -11,6 +11,7 @@
 //                          (exact fp32 arithmetic on CUDA cores; bf16 runs on
 //                          tcgen05 in egmla_decode_tc.cu)
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -246,7 +247,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
                     int d_rope, int d_c, int page_size, uint8_t* __restrict__ qprep, size_t qstride,
                     int32_t* __restrict__ cu, uint32_t* __restrict__ seq_done, int num_splits,
                     const int32_t* __restrict__ block_table, int max_pages, SplitStart* __restrict__ starts, int nt,
-                    uint64_t wait_ns, int32_t* status, const AppendArgs app) {
+                    uint64_t wait_ns, int32_t* status, const AppendArgs app, uint8_t* __restrict__ q16) {
   extern __shared__ uint8_t pm_raw[];
   uint8_t* smem = pm_raw + ((1024u - (smem_u32(pm_raw) & 1023u)) & 1023u);
   constexpr int H = 16;
@@ -357,6 +358,16 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         part[j] = __bfloat162float(bq);
         part[16 + j] = v[j] * bt;
         if (c0 + j < nb) *reinterpret_cast<__nv_bfloat16*>(qb + j * qstride) = bq;
+      }
+      if (q16 != nullptr) {
+        uint8_t* qh = q16 + static_cast<size_t>(b0 + c0) * qprep_lat_bytes(d_c) + qop_offset(h, f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          // (a finite value beyond f16's range stays finite, an infinite one or NaN what it is)
+          float x = v[j] * gm * kShQScale;
+          if (fabsf(x) < INFINITY) x = fminf(fmaxf(x, -65504.f), 65504.f);
+          if (c0 + j < nb) *reinterpret_cast<__half*>(qh + j * qprep_lat_bytes(d_c)) = __float2half_rn(x);
+        }
       }
       const float sum = reduce32_transpose(part, lane);   // lane t: value t
       if (c0 + (lane & 15) < nb) {
@@ -477,6 +488,9 @@ prologue_f32_kernel(const float* __restrict__ q, const float* __restrict__ w_uk,
 //    pairs than threads, the slots are dealt to groups of threads whose sums are
 //    added in group order.  The time is then a few round trips to L2 whatever
 //    the number of slots.
+// With SHARED the partials of a prefix that the batch shares follow those of the
+// sequence's own splits: the CTAs c0..c1 of SharedSchedule whose ranges meet its
+// row tile, kSharedTile partials apart.
 // emit(j, f, o) is called for features f .. f + 3 of sequence b0 + j, by one
 // thread; the caller's next __syncthreads makes what it stored visible.
 constexpr int kCombineSlots = 128;
@@ -487,6 +501,7 @@ struct MergeShared {
   float wts[kMergeMaxSeq][kCombineSlots];
   float inv_l[kMergeMaxSeq];
   int slots[kMergeMaxSeq], slot0[kMergeMaxSeq];
+  int own[kMergeMaxSeq], prefix0[kMergeMaxSeq];   // with a shared prefix: the slots before it, its first partial
   float4 red[T];
 };
 
@@ -498,9 +513,10 @@ int merge_group(int H, int batch, int most) {
   return nt;
 }
 
-template <int PPT, int T, int TS, typename Emit>
+template <int PPT, int T, bool SHARED = false, int TS, typename Emit>
 __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const float* part_ml, const float* part_o,
-                               int batch, int H, int h, int b0, int nt, int d_c, int num_splits, Emit emit) {
+                               int batch, int H, int h, int b0, int nt, int d_c, int num_splits, Emit emit,
+                               const SharedParts& prefix = SharedParts()) {
   static_assert(T <= TS, "threads");
   constexpr int kFlight = PPT >= 4 ? 4 : 8;   // slots of a pair in flight
   constexpr int kWarps = T / 32;
@@ -512,6 +528,13 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
   int n[2] = {0, 0};
   float M[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
   const float* pml[2] = {part_ml, part_ml};
+  int n1[2] = {0, 0};
+  const float* pml2[2] = {prefix.ml, prefix.ml};
+  // (m, l) of slot k of this warp's sequence e
+  auto ml_of = [&](int e, int k) {
+    if (SHARED && k >= n1[e]) return pml2[e] + (k - n1[e]) * (kSharedTile * mlstride);
+    return pml[e] + k * mlstride;
+  };
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int j = warp + kWarps * e;
@@ -519,11 +542,23 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
     const int b = b0 + j, p0 = cu[b] + kSegCost, p1 = cu[b + 1], c0 = p0 / chunk;   // units of the sequence's pages
     n[e] = p1 > p0 ? (p1 - 1) / chunk - c0 + 1 : 0;
     pml[e] += (static_cast<size_t>(c0 + b) * H + h) * 2;
+    if constexpr (SHARED) {
+      n1[e] = n[e];
+      const SharedSchedule s(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), prefix.ctas);
+      if (s.pages > 0) {
+        const int t = b / kSharedTile, s0 = t * s.pages / s.chunk, s1 = ((t + 1) * s.pages - 1) / s.chunk;
+        const int first = (s0 + t) * kSharedTile + b % kSharedTile;
+        n[e] += s1 - s0 + 1;
+        pml2[e] += (static_cast<size_t>(first) * H + h) * 2;
+        if (lane == 0) sh.prefix0[j] = first;
+      }
+      if (lane == 0) sh.own[j] = n1[e];
+    }
     if (lane == 0) {
       sh.slots[j] = n[e];
       sh.slot0[j] = c0 + b;
     }
-    for (int k = lane; k < n[e]; k += 32) M[e] = fmaxf(M[e], pml[e][k * mlstride]);
+    for (int k = lane; k < n[e]; k += 32) M[e] = fmaxf(M[e], *ml_of(e, k));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) M[e] = fmaxf(M[e], __shfl_xor_sync(0xffffffffu, M[e], o));
   }
@@ -554,7 +589,7 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
       for (int k = lane; k < kCombineSlots; k += 32) {
         float wk = 0.f;
         if (k0 + k < n[e]) {
-          const float2 ml = *reinterpret_cast<const float2*>(pml[e] + (k0 + k) * mlstride);
+          const float2 ml = *reinterpret_cast<const float2*>(ml_of(e, k0 + k));
           wk = exp2f(ml.x - M[e]);
           lsum[e] = fmaf(wk, ml.y, lsum[e]);
         }
@@ -571,8 +606,16 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
         for (int e = 0; e < kFlight; ++e) {
           const int kk = k + e * groups;
           v[u][e] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (pj[u] >= 0 && kk < kn && k0 + kk < sh.slots[pj[u]])
-            v[u][e] = *reinterpret_cast<const float4*>(po[u] + (k0 + kk) * sstride);
+          if (pj[u] >= 0 && kk < kn && k0 + kk < sh.slots[pj[u]]) {
+            const float* src = po[u] + (k0 + kk) * sstride;
+            if constexpr (SHARED) {
+              const int own = sh.own[pj[u]];
+              if (k0 + kk >= own)
+                src = prefix.o + (static_cast<size_t>(sh.prefix0[pj[u]]) * H + h) * d_c + pf[u] +
+                      (k0 + kk - own) * (kSharedTile * sstride);
+            }
+            v[u][e] = *reinterpret_cast<const float4*>(src);
+          }
         }
 #pragma unroll
       for (int u = 0; u < PPT; ++u)
@@ -734,11 +777,12 @@ static_assert(ct_smem(kCombineMaxDc, kMergeMaxSeq) <= kSmemMost, "shared memory"
 // that is more than one pair each: more of the partials in flight, 128 ragged
 // sequences 69.3 -> 67.7 us, 128 at d_c 512 123.6 -> 118.9; 256 otherwise, 32 x 4K
 // 37.5 against 38.1)
-template <int PPT, int kCtThreads>
+template <int PPT, int kCtThreads, bool SHARED>
 __global__ void __launch_bounds__(kCtThreads)
 combine_tc_kernel(const __grid_constant__ CUtensorMap wmap, const int32_t* __restrict__ cu,
                   const float* __restrict__ part_ml, const float* __restrict__ part_o, __nv_bfloat16* __restrict__ out,
-                  int batch, int d_c, int d_v, int num_splits, int nt, int early, uint64_t wait_ns, int32_t* status) {
+                  int batch, int d_c, int d_v, int num_splits, int nt, int early, uint64_t wait_ns, int32_t* status,
+                  const SharedParts prefix) {
   constexpr int H = 16;
   extern __shared__ uint8_t ct_raw[];
   uint8_t* smem = ct_raw + ((1024u - (smem_u32(ct_raw) & 1023u)) & 1023u);
@@ -769,8 +813,8 @@ combine_tc_kernel(const __grid_constant__ CUtensorMap wmap, const int32_t* __res
   grid_dependency_wait();
   // the merged vectors as three bf16 pieces, rows j, nt + j and 2 nt + j of the N
   // operand (K-major, 128-byte swizzle)
-  merge_partials<PPT, kCtThreads>(sh.merge, cu, part_ml, part_o, batch, H, h, b0, nt, d_c, num_splits,
-                                  [&](int j, int f, const float4& o) {
+  merge_partials<PPT, kCtThreads, SHARED>(sh.merge, cu, part_ml, part_o, batch, H, h, b0, nt, d_c, num_splits,
+                                          [&](int j, int f, const float4& o) {
     float x[4] = {o.x, o.y, o.z, o.w};
     const int kc = f / 64, unit = (f % 64) / 8;
 #pragma unroll
@@ -790,7 +834,7 @@ combine_tc_kernel(const __grid_constant__ CUtensorMap wmap, const int32_t* __res
       *reinterpret_cast<uint2*>(smem + o_off + kc * o_chunk + row * 128 + ((unit ^ (row & 7)) << 4) + (f & 4) * 2) =
           make_uint2(w[0], w[1]);
     }
-  });
+  }, prefix);
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
@@ -1196,7 +1240,8 @@ int absorb_tile(int d_c, int batch) {
   return nt;
 }
 
-cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st) {
+cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
+                               void* q16) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, 16, a.d_c, a.d_rope, true);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   // with the gate off the latent is used as cached: no LayerNorm affine to fold into q^
@@ -1216,7 +1261,7 @@ cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const
       static_cast<const __nv_bfloat16*>(a.q), gamma, beta, a.seq_lens, a.batch, a.d_nope, a.d_rope, a.d_c,
       a.page_size, ws + wl.off_qprep, wl.qprep_stride, reinterpret_cast<int32_t*>(ws + wl.off_cu),
       reinterpret_cast<uint32_t*>(ws + wl.off_done), a.num_splits, a.block_table, a.max_pages,
-      reinterpret_cast<SplitStart*>(ws + wl.off_start), nt, kWaitLimitNs, a.status, ap);
+      reinterpret_cast<SplitStart*>(ws + wl.off_start), nt, kWaitLimitNs, a.status, ap, static_cast<uint8_t*>(q16));
 }
 
 namespace {
@@ -1256,32 +1301,39 @@ cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaSt
 }
 
 namespace {
-template <int PPT, int T>
+template <int PPT, int T, bool SHARED>
 cudaError_t launch_combine_tc(const DecodeArgs& a, const CUtensorMap* wmap, const int32_t* cu, const float* ml,
-                              const float* po, int nt, cudaStream_t st) {
+                              const float* po, int nt, cudaStream_t st, const SharedParts& prefix) {
   const size_t smem = ct_smem(a.d_c, nt);
-  const cudaError_t e = allow_smem(combine_tc_kernel<PPT, T>, ct_smem(kCombineMaxDc, kMergeMaxSeq));
+  const cudaError_t e = allow_smem(combine_tc_kernel<PPT, T, SHARED>, ct_smem(kCombineMaxDc, kMergeMaxSeq));
   if (e != cudaSuccess) return e;
-  return launch_chained(combine_tc_kernel<PPT, T>, dim3(16 * ((a.batch + nt - 1) / nt), (a.d_v + 127) / 128),
+  return launch_chained(combine_tc_kernel<PPT, T, SHARED>, dim3(16 * ((a.batch + nt - 1) / nt), (a.d_v + 127) / 128),
                         dim3(T), smem, st, *wmap, cu, ml, po, static_cast<__nv_bfloat16*>(a.out), a.batch,
-                        a.d_c, a.d_v, a.num_splits, nt, a.early, kWaitLimitNs, a.status);
+                        a.d_c, a.d_v, a.num_splits, nt, a.early, kWaitLimitNs, a.status, prefix);
+}
+
+template <bool SHARED>
+cudaError_t launch_combine_bf16(const DecodeArgs& a, const CUtensorMap* wmap, const int32_t* cu, const float* ml,
+                                const float* po, cudaStream_t st, const SharedParts& prefix) {
+  const int nt = merge_group(16, a.batch, kMergeMaxSeq);
+  const int pairs = nt * (a.d_c / 4);
+  if (pairs <= 256) return launch_combine_tc<1, 256, SHARED>(a, wmap, cu, ml, po, nt, st, prefix);
+  if (pairs <= 512) return launch_combine_tc<1, 512, SHARED>(a, wmap, cu, ml, po, nt, st, prefix);
+  if (pairs <= 1024) return launch_combine_tc<2, 512, SHARED>(a, wmap, cu, ml, po, nt, st, prefix);
+  return launch_combine_tc<4, 512, SHARED>(a, wmap, cu, ml, po, nt, st, prefix);
 }
 }  // namespace
 
-cudaError_t launch_combine(const DecodeArgs& a, bool tc_path, const CUtensorMap* wmap, cudaStream_t st) {
+cudaError_t launch_combine(const DecodeArgs& a, bool tc_path, const CUtensorMap* wmap, cudaStream_t st,
+                           const SharedParts* shared) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, tc_path);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const int32_t* cu = reinterpret_cast<const int32_t*>(ws + wl.off_cu);
   const float* ml = reinterpret_cast<const float*>(ws + wl.off_ml);
   const float* po = reinterpret_cast<const float*>(ws + wl.off_o);
-  if (tc_path) {
-    const int nt = merge_group(16, a.batch, kMergeMaxSeq);
-    const int pairs = nt * (a.d_c / 4);
-    if (pairs <= 256) return launch_combine_tc<1, 256>(a, wmap, cu, ml, po, nt, st);
-    if (pairs <= 512) return launch_combine_tc<1, 512>(a, wmap, cu, ml, po, nt, st);
-    if (pairs <= 1024) return launch_combine_tc<2, 512>(a, wmap, cu, ml, po, nt, st);
-    return launch_combine_tc<4, 512>(a, wmap, cu, ml, po, nt, st);
-  }
+  if (tc_path)
+    return shared != nullptr ? launch_combine_bf16<true>(a, wmap, cu, ml, po, st, *shared)
+                             : launch_combine_bf16<false>(a, wmap, cu, ml, po, st, SharedParts());
   // small batches: the output rows spread over more blocks (a pass of the block's
   // warps covers 32 rows), so that most SMs read a part of W_UV
   const int nt = merge_group(a.H, a.batch, kCombineGroup), pairs = nt * (a.d_c / 4);

@@ -130,4 +130,56 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
   return lo;
 }
 
+// Attention over a shared prefix (egmla_shared.cu).  A unit is (row tile of
+// kSharedTile sequences, prefix page), row tiles outermost; the units are cut into
+// equal contiguous ranges, one per CTA.  CTA c's partial of row tile t is slot
+// c + t (as for the splits above), kSharedTile sequences x H heads per slot.
+constexpr int kSharedTile = 8;
+
+struct SharedSchedule {
+  int pages, units, chunk;
+  __host__ __device__ SharedSchedule(int batch, int prefix_len, int ctas) {
+    pages = (prefix_len + kPage - 1) / kPage;
+    units = (batch + kSharedTile - 1) / kSharedTile * pages;
+    chunk = split_chunk(units, ctas);
+  }
+};
+
+// A normalised latent has |z'| <= sqrt(d_c), so the gate modes with a LayerNorm
+// meet the prefix in f16, whose three more bits of significand than bf16's make the
+// roundings of z', of the softmax weights and of q^ gamma small against the output's
+// (rel-L2 against 64 bits of the emulated arithmetic, 8 and 17 sequences of a few
+// tokens after 64: 3.0e-3 in bf16, 1.9e-3 in f16).  q^ gamma is kept 2^-kShQShift
+// times its value: it may reach 1.6e7, and its smallest step, 1.5e-5, moves a score
+// by about 1e-5.
+constexpr int kShQShift = 8;
+constexpr float kShQScale = 1.f / (1 << kShQShift);
+
+// rows of the gated prefix: whole pages; with the gate off only the last page
+__host__ __device__ inline size_t shared_z_rows(int max_prefix_len, bool gate) {
+  return gate ? align_up(static_cast<size_t>(max_prefix_len), kPage) : kPage;
+}
+
+// after the own tokens' decode workspace (`base` bytes)
+struct SharedLayout {
+  size_t off_q, off_z, off_ml, off_o, total;
+};
+
+__host__ __device__ inline SharedLayout shared_layout(size_t base, int batch, int max_prefix_len, int ctas, int H,
+                                                      int d_c, bool gate) {
+  SharedLayout w;
+  const size_t slots = static_cast<size_t>(ctas) + (batch + kSharedTile - 1) / kSharedTile;
+  size_t off = align_up(base, 256);
+  w.off_q = off;   // q^ gamma in f16, laid out as in the prepared query blocks
+  off = align_up(off + static_cast<size_t>(batch) * qprep_lat_bytes(d_c), 256);
+  w.off_z = off;
+  off = align_up(off + shared_z_rows(max_prefix_len, gate) * d_c * 2, 256);
+  w.off_ml = off;
+  off = align_up(off + slots * kSharedTile * H * 2 * 4, 256);
+  w.off_o = off;
+  off = align_up(off + slots * kSharedTile * H * d_c * 4, 256);
+  w.total = off;
+  return w;
+}
+
 }  // namespace egmla

@@ -1640,7 +1640,7 @@ cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_
   p.stall_cta = a.stall_cta;
   p.stall_tile = a.stall_tile;
   // (the fused combine holds kCombineRowsPerWarp rows of W_UV,h per warp)
-  p.fuse = DBG != 1 && D_C <= 256 && a.batch > 0 && kHeads * a.batch <= a.num_splits &&
+  p.fuse = DBG != 1 && !a.apart && D_C <= 256 && a.batch > 0 && kHeads * a.batch <= a.num_splits &&
            a.d_v <= kCombineRowsPerWarp * (kThreads / 32) &&
            a.num_splits <= resident_ctas<decode_tc_kernel<D_C, GM, DBG>>(C::SMEM);
   if (fused) *fused = p.fuse != 0;

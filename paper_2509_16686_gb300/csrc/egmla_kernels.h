@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "../../include/egmla.h"
+#include "egmla_common.cuh"
 
 namespace egmla {
 
@@ -158,6 +159,7 @@ struct DecodeArgs {
   const void* w_uv;
   void* out;
   int num_splits;
+  int apart;   // the split combine always as a kernel of its own
   int early;   // let the kernel after the split-KV kernel start early (it streams weights of its own)
   void* workspace;
   int32_t* status;
@@ -180,13 +182,25 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t st);
 // append the new token of every sequence (the pools are read by no block of it)
 // `maps`: W_UK as {d_c, d_nope, H} in boxes of {64, 64, 1} and q^C as {d_nope, H,
 // batch} in boxes of {64, 1, absorb_tile}
-cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st);
+// `q16` (may be null): q^ gamma in f16 too, for the attention over a shared prefix
+cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
+                               void* q16 = nullptr);
 // sequences per block of the absorption
 int absorb_tile(int d_c, int batch);
 // fp32: absorption (with the append blocks of `app` when it is non-null) and the split-KV kernel
 cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st);
-// `wmap` (tensor-core path): W_UV as {d_c, d_v, H} in boxes of {64, 128, 1}
-cudaError_t launch_combine(const DecodeArgs& a, bool tc_path, const CUtensorMap* wmap, cudaStream_t st);
+// The partials of a prefix that the batch shares, merged with the sequences' own
+// (combine of the tensor-core path); how they lie: see SharedSchedule.
+struct SharedParts {
+  const float* ml;
+  const float* o;
+  const int32_t* prefix_len;
+  int max_prefix_len, ctas;
+};
+// `wmap` (tensor-core path): W_UV as {d_c, d_v, H} in boxes of {64, 128, 1};
+// `shared` (may be null; tensor-core path): a second list of partials
+cudaError_t launch_combine(const DecodeArgs& a, bool tc_path, const CUtensorMap* wmap, cudaStream_t st,
+                           const SharedParts* shared = nullptr);
 // tensor-core split-KV kernel; `maps` = {c_pool map (3-D box of a tile), kr_pool map}.
 // *fused (may be null) is set when the split combine ran inside the kernel
 // (cooperative launch); otherwise launch_combine must follow.
@@ -194,6 +208,20 @@ cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool 
                              bool* fused);
 // true if the bf16 tensor-core path has a kernel for these shapes
 bool tc_supported(int d_c, int gate);
+
+// Attention over a shared prefix (egmla_shared.cu): the gated prefix and the
+// partials of every sequence over it, into the workspace parts `wl` of `dec`.
+// `maps`: the gated prefix (gate off: the latent pool), its last page (gate off),
+// the RoPE keys, each in boxes of one page.
+struct SharedArgs {
+  const DecodeArgs* dec;
+  SharedLayout wl;
+  const int32_t* prefix_table;
+  const int32_t* prefix_len;
+  int max_prefix_len, ctas;
+};
+bool shared_supported(int d_c);
+cudaError_t launch_shared(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st);
 
 // R0 decode (egmla_r0.cu): bf16, 16 heads, d_n = d_v = 128, d_r = 64,
 // d_c in {192, 256}
