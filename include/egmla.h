@@ -58,7 +58,8 @@ typedef enum {
   EG_MLA_ERR_OUT_OF_RANGE = -4,  /* device: page id >= num_pages or token id >= vocab */
   EG_MLA_ERR_TIMEOUT = -5,       /* device: a pipeline wait exceeded its limit */
   EG_MLA_ERR_WORKSPACE = -6,     /* workspace too small or misaligned */
-  EG_MLA_ERR_SCRATCH_LIMIT = -7  /* needs more than EG_MLA_STATIC_SCRATCH_BYTES of static scratch */
+  EG_MLA_ERR_SCRATCH_LIMIT = -7, /* needs more than EG_MLA_STATIC_SCRATCH_BYTES of static scratch */
+  EG_MLA_ERR_NO_PAGES = -8       /* device: eg_mla_page_plan refused a request for want of pages */
 } eg_mla_status;
 
 typedef enum { EG_MLA_BF16 = 0, EG_MLA_FP32 = 1 } eg_mla_dtype;
@@ -256,6 +257,125 @@ int eg_mla_decode_shared(const eg_mla_dims* dims, const void* q, const void* c_p
                          const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
                          const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
                          int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_page_plan - the pages of one serving step, from the lengths of its
+ * requests: what the other calls take as block_table, seq_lens, positions and
+ * cu_seqlens.  The page size is 64 (EG-MLA's cache of eg_mla_append_latent).
+ *
+ * For sequence b with L = seq_lens[b] cached tokens and n = new_tokens[b]:
+ *   n > 0   the step adds n tokens (1 in a decode step, a prompt's length with
+ *           L = 0).  It needs need_b = ceil((L + n) / 64) - ceil(L / 64) pages
+ *   n = 0   nothing changes
+ *   n < 0   the sequence leaves: its ceil(L / 64) pages go back, its length
+ *           becomes 0 (the block-table row keeps its stale entries)
+ * Pages that go back are pushed first, in the order of the batch and of each row:
+ * page i of them onto free_pages[F + i], F = *free_count.  With avail entries
+ * then on the stack, requests are served first come, first served: request b is
+ * granted if need_b = 0 or E_b + need_b <= avail, E_b = sum_{b' < b} need_b', and
+ * its i-th new page is free_pages[avail - 1 - (E_b + i)].  A request whose row
+ * cannot hold L + n tokens is refused and needs nothing.  A refused request adds
+ * no token, and its sequence is unchanged.
+ *
+ *   new_tokens      [batch] int32
+ *   seq_lens        [batch] int32
+ *   seq_lens_out    [batch] int32, written: lengths after the step; may be
+ *                   seq_lens
+ *   block_table     [batch, max_pages_per_seq] int32: the entries of granted
+ *                   pages are written
+ *   free_pages      [num_pages] int32: a stack of the free pages' ids
+ *   free_count, free_count_out   one int32 each: the stack's height before and
+ *                   after; may be the same word
+ *   cu_seqlens      [batch + 1] int32, written: exclusive sums of the granted
+ *                   tokens: where each sequence's new tokens start when packed
+ *   positions       [batch] int32, written: the first new token's position (L),
+ *                   -1 without one; may be NULL
+ *   slots           [max_slots] int32, written: for packed new token k the row
+ *                   page * 64 + offset of the cache it belongs in, -1 for the
+ *                   entries past cu_seqlens[batch]; may be NULL
+ *   batch           at most 16384; num_pages * 64 + batch * 64, batch *
+ *                   max_pages_per_seq and max_pages_per_seq * 64 within 32 bits
+ *                   (EG_MLA_ERR_UNSUPPORTED otherwise)
+ * The results do not depend on timing.  Other arguments must not overlap.
+ * Device errors: EG_MLA_ERR_NO_PAGES if a request was refused (which ones:
+ * cu_seqlens) and nothing was out of range; EG_MLA_ERR_OUT_OF_RANGE for a length outside 0 ..
+ * max_pages_per_seq * 64 (that sequence is left alone), *free_count outside 0 ..
+ * num_pages (taken as 0), more pages going back than the stack holds (the rest
+ * is dropped), a page id outside [0, num_pages) in a row or on the stack (handed
+ * on as it is; slots in it are -1), or more granted tokens than max_slots (the
+ * rest has no slot).
+ */
+int eg_mla_page_plan(const int32_t* new_tokens, const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* block_table,
+                     int32_t max_pages_per_seq, int32_t batch, int32_t* free_pages, int32_t num_pages,
+                     const int32_t* free_count, int32_t* free_count_out, int32_t* cu_seqlens, int32_t* positions,
+                     int32_t* slots, int32_t max_slots, int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_page_summary - the mean keys of the pages that a step completed, which
+ * eg_mla_decode_sparse ranks pages by: for every page whose last row is among the
+ * last new_tokens[b] tokens of sequence b,
+ *   summary[page] = 1/64 sum_j [c~_j ; k^R_j]   over the page's 64 rows,
+ * c~_j the gated latent of row j as in eg_mla_decode, in fp32.  Pages that are not
+ * full have no summary (the sparse decode always reads a sequence's last page).
+ * Call it after the tokens were written: with new_tokens NULL it covers all full
+ * pages of seq_lens, as after a prompt.
+ *
+ *   c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens,
+ *   max_seq_len, batch, num_pages, gate_table, ln_gamma, ln_beta: as for
+ *                   eg_mla_decode (the same dims are supported; row sizes in bytes
+ *                   must be multiples of 16)
+ *   new_tokens      [batch] int32 or NULL (all tokens); negative: none
+ *   max_new_tokens  host-side bound of new_tokens (ignored with NULL)
+ *   summary         [num_pages, d_c + d_rope] fp32, 16-byte aligned; the rows of
+ *                   completed pages are written
+ * Device errors: EG_MLA_ERR_OUT_OF_RANGE for a page id outside [0, num_pages)
+ * (skipped), a token id outside [0, vocab) (row 0 is used), a length outside 0 ..
+ * max_seq_len or new_tokens above max_new_tokens (the bound is used).
+ */
+int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void* krope_pool, const int32_t* id_pool,
+                        const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                        int32_t max_seq_len, const int32_t* new_tokens, int32_t max_new_tokens, int32_t batch,
+                        int32_t num_pages, const void* gate_table, const float* ln_gamma, const float* ln_beta,
+                        float* summary, int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_decode_sparse - one decode step over the pages of each sequence that
+ * matter most to its query.
+ *
+ * A sequence of np = ceil(L_b / 64) <= budget pages is attended as a whole.  Of a
+ * longer one, `budget` pages are: the first keep_first, the last keep_last, and of
+ * those between the ones with the largest
+ *   score_b(p) = max_h scale (q^_b,h . m^c_p + q^R_b,h . m^R_p),
+ * [m^c_p ; m^R_p] = summary[page p] (eg_mla_page_summary): a page is as important
+ * as its mean key is to the head that wants it most.  Equal scores: the earlier
+ * page first; a score that is no number comes last.  Scores are computed and
+ * compared in fp32.  The result is eg_mla_decode's over the chosen pages' tokens.
+ * One selection serves all heads, which share the latent.
+ *
+ *   summary      [num_pages, d_c + d_rope] fp32, 16-byte aligned; read for the
+ *                pages that are ranked, all of which are full
+ *   budget       pages per sequence, >= keep_first + keep_last
+ *   keep_first   >= 0;  keep_last >= 1 (the last page may not be full)
+ *   selected     [batch, budget] int32, written: the chosen logical pages in
+ *                order, -1 past a shorter sequence's; may be NULL
+ *   workspace    >= eg_mla_decode_sparse_workspace_size(dims, batch,
+ *                max_pages_per_seq, budget, num_splits) bytes, 256-byte aligned:
+ *                that of eg_mla_decode, the absorbed queries in fp32, a score per
+ *                page and the selected block table
+ *   the others   as for eg_mla_decode; every dims that it supports with d_rope a
+ *                multiple of 4
+ * Device errors: as for eg_mla_decode; a length outside 0 .. max_seq_len is
+ * reported as EG_MLA_ERR_OUT_OF_RANGE and taken as the nearer bound.
+ */
+size_t eg_mla_decode_sparse_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_pages_per_seq,
+                                           int32_t budget, int32_t num_splits);
+int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
+                         const int32_t* id_pool, const int32_t* block_table, int32_t max_pages_per_seq,
+                         const int32_t* seq_lens, int32_t max_seq_len, int32_t batch, int32_t num_pages,
+                         const float* summary, int32_t budget, int32_t keep_first, int32_t keep_last,
+                         const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
+                         const void* w_uv, void* out, int32_t* selected, int32_t num_splits, void* workspace,
+                         size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* Size of the static device scratch array behind eg_mla_decode_static. */
 #define EG_MLA_STATIC_SCRATCH_BYTES ((size_t)16 << 20)

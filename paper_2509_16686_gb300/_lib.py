@@ -24,6 +24,7 @@ EG_MLA_ERR_OUT_OF_RANGE = -4
 EG_MLA_ERR_TIMEOUT = -5
 EG_MLA_ERR_WORKSPACE = -6
 EG_MLA_ERR_SCRATCH_LIMIT = -7
+EG_MLA_ERR_NO_PAGES = -8
 
 # size of the library's static scratch array (EG_MLA_STATIC_SCRATCH_BYTES)
 STATIC_SCRATCH_BYTES = 16 << 20
@@ -44,6 +45,10 @@ EXPORTED = [
     "eg_mla_decode_static",
     "eg_mla_decode_shared_workspace_size",
     "eg_mla_decode_shared",
+    "eg_mla_decode_sparse_workspace_size",
+    "eg_mla_decode_sparse",
+    "eg_mla_page_plan",
+    "eg_mla_page_summary",
     "eg_mla_step",
     "eg_mla_decode_r0_workspace_size",
     "eg_mla_decode_r0",
@@ -109,6 +114,15 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.eg_mla_decode_shared.argtypes = [D, P, P, P, P, P, P, I32, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P,
                                          SZ, P, P]
     lib.eg_mla_decode_shared.restype = ctypes.c_int
+    lib.eg_mla_decode_sparse_workspace_size.argtypes = [D, I32, I32, I32, I32]
+    lib.eg_mla_decode_sparse_workspace_size.restype = SZ
+    lib.eg_mla_decode_sparse.argtypes = [D, P, P, P, P, P, I32, P, I32, I32, I32, P, I32, I32, I32, P, P, P, P, P, P, P,
+                                         I32, P, SZ, P, P]
+    lib.eg_mla_decode_sparse.restype = ctypes.c_int
+    lib.eg_mla_page_plan.argtypes = [P, P, P, P, I32, I32, P, I32, P, P, P, P, P, I32, P, P]
+    lib.eg_mla_page_plan.restype = ctypes.c_int
+    lib.eg_mla_page_summary.argtypes = [D, P, P, P, P, I32, P, I32, P, I32, I32, I32, P, P, P, P, P, P]
+    lib.eg_mla_page_summary.restype = ctypes.c_int
     lib.eg_mla_step.argtypes = [D, P, P, P, P, P, P, P, P, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ,
                                 P, P]
     lib.eg_mla_step.restype = ctypes.c_int
@@ -201,6 +215,11 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     if not t.is_contiguous():
         raise ValueError("contiguous tensor expected")
     return t.data_ptr()
+
+
+def _shaped(t: Optional[torch.Tensor], shape: tuple, name: str) -> None:
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {shape} expected, got {tuple(t.shape)}")
 
 
 def _stream(stream) -> int:
@@ -310,6 +329,58 @@ def eg_mla_decode_shared(dims: EgMlaDims, q, c_pool, krope_pool, id_pool, prefix
         _ptr(w_uk), _ptr(w_uv), _ptr(out), num_splits, _ptr(workspace),
         workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream))
     _check(code, "eg_mla_decode_shared")
+
+
+def eg_mla_decode_sparse_workspace_size(dims: EgMlaDims, batch: int, max_pages_per_seq: int, budget: int,
+                                        num_splits: int = 0) -> int:
+    n = load().eg_mla_decode_sparse_workspace_size(ctypes.byref(dims), batch, int(max_pages_per_seq), int(budget),
+                                                   num_splits)
+    if n == 0:
+        raise EgMlaError(EG_MLA_ERR_UNSUPPORTED, "eg_mla_decode_sparse_workspace_size")
+    return int(n)
+
+
+def eg_mla_decode_sparse(dims: EgMlaDims, q, c_pool, krope_pool, id_pool, block_table, seq_lens, max_seq_len, summary,
+                         budget, keep_first, keep_last, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, workspace,
+                         selected=None, num_splits=0, dev_status=None, stream=None) -> None:
+    """One decode step over the pages that score best: see include/egmla.h."""
+    _shaped(summary, (c_pool.shape[0], dims.d_c + dims.d_rope), "summary")
+    _shaped(selected, (seq_lens.shape[0], budget), "selected")
+    code = load().eg_mla_decode_sparse(
+        ctypes.byref(dims), _ptr(q), _ptr(c_pool), _ptr(krope_pool), _ptr(id_pool), _ptr(block_table),
+        block_table.shape[1], _ptr(seq_lens), int(max_seq_len), seq_lens.shape[0], c_pool.shape[0], _ptr(summary),
+        int(budget), int(keep_first), int(keep_last), _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk),
+        _ptr(w_uv), _ptr(out), _ptr(selected), num_splits, _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream(stream))
+    _check(code, "eg_mla_decode_sparse")
+
+
+def eg_mla_page_summary(dims: EgMlaDims, c_pool, krope_pool, id_pool, block_table, seq_lens, max_seq_len, gate_table,
+                        ln_gamma, ln_beta, summary, new_tokens=None, max_new_tokens=0, dev_status=None,
+                        stream=None) -> None:
+    """Mean keys of the pages that the last new_tokens (None: all) tokens completed: see include/egmla.h."""
+    _shaped(summary, (c_pool.shape[0], dims.d_c + dims.d_rope), "summary")
+    _shaped(new_tokens, tuple(seq_lens.shape), "new_tokens")
+    code = load().eg_mla_page_summary(
+        ctypes.byref(dims), _ptr(c_pool), _ptr(krope_pool), _ptr(id_pool), _ptr(block_table), block_table.shape[1],
+        _ptr(seq_lens), int(max_seq_len), _ptr(new_tokens), int(max_new_tokens), seq_lens.shape[0], c_pool.shape[0],
+        _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(summary), _ptr(dev_status), _stream(stream))
+    _check(code, "eg_mla_page_summary")
+
+
+def eg_mla_page_plan(new_tokens, seq_lens, seq_lens_out, block_table, free_pages, free_count, free_count_out,
+                     cu_seqlens, positions=None, slots=None, dev_status=None, stream=None) -> None:
+    """A serving step's pages, offsets and cache slots from its requests' lengths: see include/egmla.h.
+    num_pages is the length of free_pages, the slots' capacity that of slots."""
+    batch = seq_lens.shape[0]
+    for name, t, n in (("new_tokens", new_tokens, batch), ("seq_lens_out", seq_lens_out, batch),
+                       ("cu_seqlens", cu_seqlens, batch + 1), ("positions", positions, batch)):
+        _shaped(t, (n,), name)
+    code = load().eg_mla_page_plan(
+        _ptr(new_tokens), _ptr(seq_lens), _ptr(seq_lens_out), _ptr(block_table), block_table.shape[1], batch,
+        _ptr(free_pages), free_pages.shape[0], _ptr(free_count), _ptr(free_count_out), _ptr(cu_seqlens),
+        _ptr(positions), _ptr(slots), slots.shape[0] if slots is not None else 0, _ptr(dev_status), _stream(stream))
+    _check(code, "eg_mla_page_plan")
 
 
 def make_layer_dims(n_embd: int, rope_theta: float = 10000.0, rms_eps: float = 0.0,

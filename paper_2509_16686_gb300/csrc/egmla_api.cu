@@ -337,6 +337,13 @@ struct Prefix {
   int32_t max_len;
 };
 
+// the pages to attend over (eg_mla_decode_sparse): the decode's block table and
+// lengths are those that `select` writes
+struct Sparse {
+  egmla::SelectArgs select;
+  float* q;   // where the tensor-core path leaves the absorbed queries in fp32
+};
+
 // the workspace of eg_mla_decode_shared: eg_mla_decode's, then the prefix's part;
 // EG_MLA_OK or the error code
 int shared_workspace(const eg_mla_dims* d, int32_t batch, int32_t max_prefix_len, int32_t num_splits,
@@ -358,15 +365,15 @@ int shared_workspace(const eg_mla_dims* d, int32_t batch, int32_t max_prefix_len
 
 // eg_mla_decode, preceded by the append of `app` when it is non-null (in the
 // query-absorption kernel's grid), and over the tokens of `prefix` too when that is
-// non-null.  Every argument is checked before anything is
-// launched (`launch` false: checked only).
+// non-null, or over the pages that `sparse` selects when that is.  Every argument is
+// checked before anything is launched (`launch` false: checked only).
 int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
                 const int32_t* id_pool, const int32_t* block_table, int32_t max_pages_per_seq,
                 const int32_t* seq_lens, int32_t max_seq_len, int32_t batch, int32_t num_pages,
                 const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
                 const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
                 int32_t* dev_status, const egmla::AppendArgs* app, cudaStream_t st, bool early = false,
-                bool launch = true, const Prefix* prefix = nullptr) {
+                bool launch = true, const Prefix* prefix = nullptr, const Sparse* sparse = nullptr) {
   egmla::SharedArgs sh;
   if (prefix != nullptr) {
     const int rc = shared_workspace(dims, batch, prefix->max_len, num_splits, &sh.wl, &sh.ctas);
@@ -411,8 +418,22 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       a.apart = 1;   // the combine has a second list of partials
       if (prefix->max_len > 0 && !encode_shared_maps(smaps, dims, a, sh)) return EG_MLA_ERR_CUDA;
     }
-    void* q16 = prefix != nullptr && a.gate_ln ? static_cast<uint8_t*>(workspace) + sh.wl.off_q : nullptr;
-    cudaError_t e = egmla::launch_prologue_tc(a, app, amaps, st, q16);
+    egmla::AbsorbExtra extra = {};
+    if (prefix != nullptr && a.gate_ln) extra.q16 = static_cast<uint8_t*>(workspace) + sh.wl.off_q;
+    cudaError_t e;
+    if (sparse == nullptr) {
+      e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
+    } else {
+      // the queries, the pages by their scores, the schedule over the selected pages
+      extra.q32 = sparse->q;
+      DecodeArgs part = a;
+      part.block_table = nullptr;
+      e = egmla::launch_prologue_tc(part, app, amaps, st, extra);
+      if (e == cudaSuccess) e = egmla::launch_select_pages(sparse->select, st);
+      part = a;
+      part.q = nullptr;
+      if (e == cudaSuccess) e = egmla::launch_prologue_tc(part, nullptr, amaps, st);
+    }
     if (e == cudaSuccess && prefix != nullptr && prefix->max_len > 0) e = egmla::launch_shared(sh, smaps, st);
     bool fused = false;
     if (e == cudaSuccess) {
@@ -429,7 +450,15 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     }
     return to_status(e);
   }
-  cudaError_t e = egmla::launch_decode_f32(a, app, st);
+  cudaError_t e = cudaSuccess;
+  if (sparse != nullptr) {
+    DecodeArgs part = a;
+    part.seq_lens = sparse->select.seq_lens;
+    e = egmla::launch_prologue_f32(part, app, st);
+    if (e == cudaSuccess) e = egmla::launch_select_pages(sparse->select, st);
+    app = nullptr;
+  }
+  if (e == cudaSuccess) e = egmla::launch_decode_f32(a, app, st);
   if (e == cudaSuccess) e = egmla::launch_combine(a, false, nullptr, st);
   return to_status(e);
 }
@@ -479,6 +508,7 @@ const char* eg_mla_status_string(int status) {
     case EG_MLA_ERR_OUT_OF_RANGE: return "page id or token id out of range";
     case EG_MLA_ERR_TIMEOUT: return "device pipeline wait timed out";
     case EG_MLA_ERR_WORKSPACE: return "workspace too small or misaligned";
+    case EG_MLA_ERR_NO_PAGES: return "free pages or a block-table row exhausted";
     case EG_MLA_ERR_SCRATCH_LIMIT:
       return "problem needs more scratch than the static scratch array (EG_MLA_STATIC_SCRATCH_BYTES) holds";
     default: return "unknown status";
@@ -561,6 +591,158 @@ int eg_mla_decode_shared(const eg_mla_dims* dims, const void* q, const void* c_p
   return decode_impl(dims, q, c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens, max_seq_len,
                      batch, num_pages, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace,
                      workspace_bytes, dev_status, nullptr, static_cast<cudaStream_t>(stream), false, true, &prefix);
+}
+
+size_t eg_mla_decode_sparse_workspace_size(const eg_mla_dims* dims, int32_t batch, int32_t max_pages_per_seq,
+                                           int32_t budget, int32_t num_splits) {
+  if (check_dims(dims) != EG_MLA_OK || batch < 0 || max_pages_per_seq <= 0 || budget <= 0) return 0;
+  const size_t base = eg_mla_decode_workspace_size(dims, batch, num_splits);
+  if (base == 0) return 0;
+  return egmla::sparse_layout(base, batch, max_pages_per_seq, budget, dims->num_heads, dims->d_c, dims->d_rope).total;
+}
+
+int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
+                         const int32_t* id_pool, const int32_t* block_table, int32_t max_pages_per_seq,
+                         const int32_t* seq_lens, int32_t max_seq_len, int32_t batch, int32_t num_pages,
+                         const float* summary, int32_t budget, int32_t keep_first, int32_t keep_last,
+                         const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
+                         const void* w_uv, void* out, int32_t* selected, int32_t num_splits, void* workspace,
+                         size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_dims(dims);
+  if (rc != EG_MLA_OK) return rc;
+  if (batch < 0 || num_pages <= 0 || max_pages_per_seq <= 0 || max_seq_len < 0 ||
+      static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_pages_per_seq) * dims->page_size)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (keep_first < 0 || keep_last < 1 || budget < keep_last || budget - keep_last < keep_first)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (dims->d_rope % 4 != 0) return EG_MLA_ERR_UNSUPPORTED;
+  if (block_table == nullptr || seq_lens == nullptr || summary == nullptr || !aligned(summary, 16))
+    return EG_MLA_ERR_INVALID_ARG;
+  int32_t splits = 0;
+  rc = resolve_splits(num_splits, &splits);
+  if (rc != EG_MLA_OK) return rc;
+  const egmla::WorkspaceLayout wl =
+      egmla::workspace_layout(batch, splits, dims->num_heads, dims->d_c, dims->d_rope, is_tc_path(dims));
+  const egmla::SparseLayout sl = egmla::sparse_layout(wl.total, batch, max_pages_per_seq, budget, dims->num_heads,
+                                                      dims->d_c, dims->d_rope);
+  if (workspace == nullptr || workspace_bytes < sl.total || !aligned(workspace, 256)) return EG_MLA_ERR_WORKSPACE;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  Sparse sp;
+  egmla::SelectArgs& s = sp.select;
+  s.chunks = egmla::score_chunks(max_seq_len, keep_first, keep_last);
+  if (static_cast<int64_t>(s.chunks) * batch > INT32_MAX) return EG_MLA_ERR_UNSUPPORTED;
+  sp.q = reinterpret_cast<float*>(ws + sl.off_q);
+  // the fp32 path's prepared queries have this form
+  s.q = is_tc_path(dims) ? sp.q : reinterpret_cast<const float*>(ws + wl.off_qprep);
+  s.q_stride = sl.q_stride;
+  s.summary = summary;
+  s.block_table = block_table;
+  s.seq_lens = seq_lens;
+  s.scores = reinterpret_cast<float*>(ws + sl.off_scores);
+  s.sel_table = reinterpret_cast<int32_t*>(ws + sl.off_table);
+  s.sel_lens = reinterpret_cast<int32_t*>(ws + sl.off_lens);
+  s.selected = selected;
+  s.status = dev_status;
+  s.H = dims->num_heads;
+  s.d_c = dims->d_c;
+  s.d_r = dims->d_rope;
+  s.batch = batch;
+  s.max_pages = max_pages_per_seq;
+  s.max_seq_len = max_seq_len;
+  s.num_pages = num_pages;
+  s.budget = budget;
+  s.keep_first = keep_first;
+  s.keep_last = keep_last;
+  s.width = sl.width;
+  s.scale = resolve_scale(dims);
+  const int64_t most = static_cast<int64_t>(sl.width) * dims->page_size;
+  return decode_impl(dims, q, c_pool, krope_pool, id_pool, s.sel_table, sl.width, s.sel_lens,
+                     max_seq_len < most ? max_seq_len : static_cast<int32_t>(most), batch, num_pages, gate_table,
+                     ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace, workspace_bytes, dev_status, nullptr,
+                     static_cast<cudaStream_t>(stream), false, true, nullptr, &sp);
+}
+
+int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void* krope_pool, const int32_t* id_pool,
+                        const int32_t* block_table, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                        int32_t max_seq_len, const int32_t* new_tokens, int32_t max_new_tokens, int32_t batch,
+                        int32_t num_pages, const void* gate_table, const float* ln_gamma, const float* ln_beta,
+                        float* summary, int32_t* dev_status, void* stream) {
+  const int rc = check_dims(dims);
+  if (rc != EG_MLA_OK) return rc;
+  if (batch < 0 || num_pages <= 0 || max_pages_per_seq <= 0 || max_seq_len < 0 || max_new_tokens < 0 ||
+      static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_pages_per_seq) * dims->page_size)
+    return EG_MLA_ERR_INVALID_ARG;
+  const int eb = elem_bytes(dims);
+  if (dims->d_c * eb % 16 || dims->d_rope * eb % 16) return EG_MLA_ERR_UNSUPPORTED;
+  const bool gate = dims->gate_mode != EG_MLA_GATE_NONE;
+  if (c_pool == nullptr || krope_pool == nullptr || block_table == nullptr || seq_lens == nullptr ||
+      summary == nullptr || (gate && (id_pool == nullptr || gate_table == nullptr)))
+    return EG_MLA_ERR_INVALID_ARG;
+  if (!aligned(c_pool, 16) || !aligned(krope_pool, 16) || !aligned(summary, 16) || (gate && !aligned(gate_table, 16)))
+    return EG_MLA_ERR_INVALID_ARG;
+  egmla::SummaryArgs a;
+  a.max_new = new_tokens != nullptr && max_new_tokens < max_seq_len ? max_new_tokens : max_seq_len;
+  // n tokens complete at most ceil(n / page) pages, and no more than the sequence has
+  a.page_bound = (a.max_new + dims->page_size - 1) / dims->page_size;
+  if (static_cast<int64_t>(a.page_bound) * batch > INT32_MAX) return EG_MLA_ERR_UNSUPPORTED;
+  if (batch == 0 || a.page_bound == 0) return EG_MLA_OK;
+  a.c_pool = c_pool;
+  a.kr_pool = krope_pool;
+  a.id_pool = id_pool;
+  a.block_table = block_table;
+  a.seq_lens = seq_lens;
+  a.new_tokens = new_tokens;
+  a.gate_table = gate_table;
+  a.summary = summary;
+  a.status = dev_status;
+  a.d_c = dims->d_c;
+  a.d_r = dims->d_rope;
+  a.vocab = dims->vocab;
+  a.batch = batch;
+  a.max_pages = max_pages_per_seq;
+  a.max_seq_len = max_seq_len;
+  a.num_pages = num_pages;
+  a.fp32 = dims->dtype == EG_MLA_FP32;
+  a.gate = gate;
+  a.gate_add = dims->gate_mode == EG_MLA_GATE_ADD_LN;
+  a.gate_ln = dims->gate_mode == EG_MLA_GATE_MUL_LN || dims->gate_mode == EG_MLA_GATE_ADD_LN;
+  a.gamma = a.gate_ln ? ln_gamma : nullptr;
+  a.beta = a.gate_ln ? ln_beta : nullptr;
+  a.eps = dims->ln_eps > 0.f ? dims->ln_eps : 1e-5f;
+  return to_status(egmla::launch_page_summary(a, static_cast<cudaStream_t>(stream)));
+}
+
+int eg_mla_page_plan(const int32_t* new_tokens, const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* block_table,
+                     int32_t max_pages_per_seq, int32_t batch, int32_t* free_pages, int32_t num_pages,
+                     const int32_t* free_count, int32_t* free_count_out, int32_t* cu_seqlens, int32_t* positions,
+                     int32_t* slots, int32_t max_slots, int32_t* dev_status, void* stream) {
+  if (batch < 0 || max_pages_per_seq <= 0 || num_pages <= 0 || max_slots < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (free_pages == nullptr || free_count == nullptr || free_count_out == nullptr || cu_seqlens == nullptr)
+    return EG_MLA_ERR_INVALID_ARG;
+  if (batch > 0 && (new_tokens == nullptr || seq_lens == nullptr || seq_lens_out == nullptr || block_table == nullptr))
+    return EG_MLA_ERR_INVALID_ARG;
+  // slots and every sum over the batch are 32-bit
+  const int64_t page = egmla::kPage;
+  if (batch > egmla::kPlanMaxBatch || num_pages * page + batch * page > INT32_MAX ||
+      max_pages_per_seq * page > INT32_MAX || static_cast<int64_t>(batch) * max_pages_per_seq > INT32_MAX)
+    return EG_MLA_ERR_UNSUPPORTED;
+  egmla::PlanArgs a;
+  a.new_tokens = new_tokens;
+  a.seq_lens = seq_lens;
+  a.seq_lens_out = seq_lens_out;
+  a.block_table = block_table;
+  a.free_pages = free_pages;
+  a.free_count = free_count;
+  a.free_count_out = free_count_out;
+  a.cu_seqlens = cu_seqlens;
+  a.positions = positions;
+  a.slots = max_slots > 0 ? slots : nullptr;
+  a.status = dev_status;
+  a.batch = batch;
+  a.max_pages = max_pages_per_seq;
+  a.num_pages = num_pages;
+  a.max_slots = max_slots;
+  return to_status(egmla::launch_page_plan(a, static_cast<cudaStream_t>(stream)));
 }
 
 int eg_mla_decode_static(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,

@@ -247,7 +247,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
                     int d_rope, int d_c, int page_size, uint8_t* __restrict__ qprep, size_t qstride,
                     int32_t* __restrict__ cu, uint32_t* __restrict__ seq_done, int num_splits,
                     const int32_t* __restrict__ block_table, int max_pages, SplitStart* __restrict__ starts, int nt,
-                    uint64_t wait_ns, int32_t* status, const AppendArgs app, uint8_t* __restrict__ q16) {
+                    uint64_t wait_ns, int32_t* status, const AppendArgs app, const AbsorbExtra extra) {
   extern __shared__ uint8_t pm_raw[];
   uint8_t* smem = pm_raw + ((1024u - (smem_u32(pm_raw) & 1023u)) & 1023u);
   constexpr int H = 16;
@@ -261,8 +261,9 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       int32_t* words = reinterpret_cast<int32_t*>(smem);
       constexpr int kWords = 4096;
       static_assert(pm_smem(1, 16) >= 1024 + (kWords + 8) * 4, "schedule area");
-      schedule_block(seq_lens, batch, page_size, cu, seq_done, num_splits, block_table, max_pages, starts, words + 8,
-                     kWords, words);
+      if (block_table != nullptr)
+        schedule_block(seq_lens, batch, page_size, cu, seq_done, num_splits, block_table, max_pages, starts, words + 8,
+                       kWords, words);
     } else {
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);
@@ -332,8 +333,17 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     const int qrow = d_nope + d_rope, pr = d_rope / 8;
     for (int i = tid - 32; i < nb * pr; i += kPmThreads - 32) {
       const int j = i / pr, r = 8 * (i % pr);
+      const uint4 x = *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + j) * H + h) * qrow + d_nope + r);
       *reinterpret_cast<uint4*>(qprep + static_cast<size_t>(b0 + j) * qstride + qprep_lat_bytes(d_c) + qop_offset(h, r)) =
-          *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + j) * H + h) * qrow + d_nope + r);
+          x;
+      if (extra.q32 != nullptr) {
+        float4* qf = reinterpret_cast<float4*>(extra.q32 + static_cast<size_t>(b0 + j) * H * (d_c + d_rope) + H * d_c +
+                                               h * d_rope + r);
+        qf[0] = make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u),
+                            __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u));
+        qf[1] = make_float4(__uint_as_float(x.z << 16), __uint_as_float(x.z & 0xffff0000u),
+                            __uint_as_float(x.w << 16), __uint_as_float(x.w & 0xffff0000u));
+      }
     }
   }
   // ---- epilogue: warp = (lane quadrant, every other group of 16 sequences)
@@ -359,8 +369,14 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         part[16 + j] = v[j] * bt;
         if (c0 + j < nb) *reinterpret_cast<__nv_bfloat16*>(qb + j * qstride) = bq;
       }
-      if (q16 != nullptr) {
-        uint8_t* qh = q16 + static_cast<size_t>(b0 + c0) * qprep_lat_bytes(d_c) + qop_offset(h, f);
+      if (extra.q32 != nullptr) {
+        float* qf = extra.q32 + static_cast<size_t>(b0 + c0) * H * (d_c + d_rope) + h * d_c + f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (c0 + j < nb) qf[static_cast<size_t>(j) * H * (d_c + d_rope)] = v[j];
+      }
+      if (extra.q16 != nullptr) {
+        uint8_t* qh = extra.q16 + static_cast<size_t>(b0 + c0) * qprep_lat_bytes(d_c) + qop_offset(h, f);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           // (a finite value beyond f16's range stays finite, an infinite one or NaN what it is)
@@ -1241,7 +1257,7 @@ int absorb_tile(int d_c, int batch) {
 }
 
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
-                               void* q16) {
+                               const AbsorbExtra& extra) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, 16, a.d_c, a.d_rope, true);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   // with the gate off the latent is used as cached: no LayerNorm affine to fold into q^
@@ -1261,7 +1277,7 @@ cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const
       static_cast<const __nv_bfloat16*>(a.q), gamma, beta, a.seq_lens, a.batch, a.d_nope, a.d_rope, a.d_c,
       a.page_size, ws + wl.off_qprep, wl.qprep_stride, reinterpret_cast<int32_t*>(ws + wl.off_cu),
       reinterpret_cast<uint32_t*>(ws + wl.off_done), a.num_splits, a.block_table, a.max_pages,
-      reinterpret_cast<SplitStart*>(ws + wl.off_start), nt, kWaitLimitNs, a.status, ap, static_cast<uint8_t*>(q16));
+      reinterpret_cast<SplitStart*>(ws + wl.off_start), nt, kWaitLimitNs, a.status, ap, extra);
 }
 
 namespace {
@@ -1281,7 +1297,7 @@ cudaError_t launch_decode_f32_t(const DecodeArgs& a, const WorkspaceLayout& wl, 
 }
 }  // namespace
 
-cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st) {
+cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   AppendArgs none;
@@ -1289,12 +1305,17 @@ cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaSt
   const AppendArgs& ap = app != nullptr ? *app : none;
   const int absorb =
       a.H * ((a.d_c + kPfFeat - 1) / kPfFeat) * ((a.batch + kPfBatch - 1) / kPfBatch);
-  const cudaError_t e = launch_chained(
+  return launch_chained(
       prologue_f32_kernel, dim3(absorb + 1 + ap.batch), dim3(256), 0, st,
       static_cast<const float*>(a.q), static_cast<const float*>(a.w_uk), a.seq_lens, a.batch, a.H, a.d_nope,
       a.d_rope, a.d_c, a.page_size, ws + wl.off_qprep, wl.qprep_stride,
       reinterpret_cast<int32_t*>(ws + wl.off_cu), ap);
+}
+
+cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st) {
+  const cudaError_t e = launch_prologue_f32(a, app, st);
   if (e != cudaSuccess) return e;
+  const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
   if (a.d_c <= 128) return launch_decode_f32_t<1>(a, wl, st);
   if (a.d_c <= 256) return launch_decode_f32_t<2>(a, wl, st);
   return launch_decode_f32_t<4>(a, wl, st);

@@ -182,4 +182,30 @@ __host__ __device__ inline SharedLayout shared_layout(size_t base, int batch, in
   return w;
 }
 
+// the page-sparse decode's own part of the workspace, after the decode workspace
+// (`base` bytes) of the selected pages
+struct SparseLayout {
+  size_t off_q, off_scores, off_table, off_lens, total;
+  size_t q_stride;   // floats
+  int width;         // pages of the selected block table
+};
+
+__host__ __device__ inline SparseLayout sparse_layout(size_t base, int batch, int max_pages, int budget, int H,
+                                                      int d_c, int d_rope) {
+  SparseLayout w;
+  w.width = budget < max_pages ? budget : max_pages;
+  w.q_stride = qprep_bytes_f32(H, d_c, d_rope) / 4;
+  size_t off = align_up(base, 256);
+  w.off_q = off;
+  off = align_up(off + static_cast<size_t>(batch) * w.q_stride * 4, 256);
+  w.off_scores = off;
+  off = align_up(off + static_cast<size_t>(batch) * max_pages * 4, 256);
+  w.off_table = off;
+  off = align_up(off + static_cast<size_t>(batch) * w.width * 4, 256);
+  w.off_lens = off;
+  off = align_up(off + static_cast<size_t>(batch) * 4, 256);
+  w.total = off;
+  return w;
+}
+
 }  // namespace egmla

@@ -182,11 +182,18 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t st);
 // append the new token of every sequence (the pools are read by no block of it)
 // `maps`: W_UK as {d_c, d_nope, H} in boxes of {64, 64, 1} and q^C as {d_nope, H,
 // batch} in boxes of {64, 1, absorb_tile}
-// `q16` (may be null): q^ gamma in f16 too, for the attention over a shared prefix
+// `extra`: the absorbed queries in other forms too.  a.q null: the schedule only;
+// a.block_table null: everything but the schedule
+struct AbsorbExtra {
+  uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
+  float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
+};
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
-                               void* q16 = nullptr);
+                               const AbsorbExtra& extra = AbsorbExtra{});
 // sequences per block of the absorption
 int absorb_tile(int d_c, int batch);
+// fp32: the absorption alone (q^ [H, d_c], then q^R [H, d_rope] per sequence)
+cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st);
 // fp32: absorption (with the append blocks of `app` when it is non-null) and the split-KV kernel
 cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st);
 // The partials of a prefix that the batch shares, merged with the sequences' own
@@ -222,6 +229,64 @@ struct SharedArgs {
 };
 bool shared_supported(int d_c);
 cudaError_t launch_shared(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st);
+
+// Pages of the cache (egmla_pages.cu); see include/egmla.h for what they compute.
+constexpr int kPlanMaxBatch = 16384;   // three words per sequence in shared memory
+constexpr int kStatusNoPages = -8;
+struct PlanArgs {
+  const int32_t* new_tokens;
+  const int32_t* seq_lens;
+  int32_t* seq_lens_out;
+  int32_t* block_table;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* free_count_out;
+  int32_t* cu_seqlens;
+  int32_t* positions;   // may be null
+  int32_t* slots;       // may be null
+  int32_t* status;
+  int batch, max_pages, num_pages, max_slots;
+};
+cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st);
+
+struct SummaryArgs {
+  const void* c_pool;
+  const void* kr_pool;
+  const int32_t* id_pool;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const int32_t* new_tokens;   // null: all tokens
+  const void* gate_table;
+  const float* gamma;          // null: 1
+  const float* beta;           // null: 0
+  float* summary;
+  int32_t* status;
+  int d_c, d_r, vocab, batch, max_pages, max_seq_len, num_pages;
+  int max_new, page_bound;     // tokens and pages per sequence, at most
+  int fp32, gate, gate_add, gate_ln;
+  float eps;
+};
+cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st);
+
+// scores of the pages, and the selected ones as a block table of `width` pages
+struct SelectArgs {
+  const float* q;         // per sequence q^ [H, d_c], then q^R [H, d_r]
+  size_t q_stride;        // floats
+  const float* summary;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  float* scores;          // [batch, max_pages]
+  int32_t* sel_table;     // [batch, width]
+  int32_t* sel_lens;      // [batch]
+  int32_t* selected;      // [batch, budget] logical pages, may be null
+  int32_t* status;
+  int H, d_c, d_r, batch, max_pages, max_seq_len, num_pages;
+  int budget, keep_first, keep_last, width;
+  int chunks;             // score_chunks()
+  float scale;
+};
+int score_chunks(int max_seq_len, int keep_first, int keep_last);   // score blocks per sequence
+cudaError_t launch_select_pages(const SelectArgs& a, cudaStream_t st);
 
 // R0 decode (egmla_r0.cu): bf16, 16 heads, d_n = d_v = 128, d_r = 64,
 // d_c in {192, 256}
