@@ -416,13 +416,17 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       parts.ml = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_ml);
       parts.o = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_o);
       a.apart = 1;   // the combine has a second list of partials
+      a.beside = prefix->max_len > 0 ? 1 : 0;
       if (prefix->max_len > 0 && !encode_shared_maps(smaps, dims, a, sh)) return EG_MLA_ERR_CUDA;
     }
     egmla::AbsorbExtra extra = {};
     if (prefix != nullptr && a.gate_ln) extra.q16 = static_cast<uint8_t*>(workspace) + sh.wl.off_q;
-    cudaError_t e;
+    const bool with_prefix = prefix != nullptr && prefix->max_len > 0;
+    cudaError_t e = cudaSuccess;
     if (sparse == nullptr) {
-      e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
+      if (with_prefix) e = egmla::launch_shared_gate(sh, st);
+      extra.beside = with_prefix ? 1 : 0;
+      if (e == cudaSuccess) e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
     } else {
       // the queries, the pages by their scores, the schedule over the selected pages
       extra.q32 = sparse->q;
@@ -434,7 +438,7 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       part.q = nullptr;
       if (e == cudaSuccess) e = egmla::launch_prologue_tc(part, nullptr, amaps, st);
     }
-    if (e == cudaSuccess && prefix != nullptr && prefix->max_len > 0) e = egmla::launch_shared(sh, smaps, st);
+    if (e == cudaSuccess && with_prefix) e = egmla::launch_shared_attn(sh, smaps, st);
     bool fused = false;
     if (e == cudaSuccess) {
       prof_mark(st, true);

@@ -256,7 +256,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (blockIdx.x == 0 || blockIdx.x > static_cast<unsigned>(ntiles)) {
     grid_launch_dependents();
-    grid_dependency_wait();
+    if (!extra.beside) grid_dependency_wait();
     if (blockIdx.x == 0) {
       int32_t* words = reinterpret_cast<int32_t*>(smem);
       constexpr int kWords = 4096;
@@ -268,6 +268,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);
     }
+    if (extra.beside) grid_dependency_wait();
     return;
   }
   const int item = static_cast<int>(blockIdx.x) - 1;
@@ -300,7 +301,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
   grid_launch_dependents();
-  grid_dependency_wait();
+  if (!extra.beside) grid_dependency_wait();
   if (warp == 0) {
     if (elect_one()) {
       const uint64_t keep = policy_evict_last(), once = policy_evict_first();
@@ -398,6 +399,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, tmem_cols);
   if (tid == 0 && *abort_flag) report_status(status, kStatusTimeout);
+  if (extra.beside) grid_dependency_wait();
 }
 
 // fp32 path: q^ [H, d_c] and q^R [H, d_rope] in fp32, row-major.  Block 0: the

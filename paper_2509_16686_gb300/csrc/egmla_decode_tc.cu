@@ -191,7 +191,7 @@ struct TcParams {
   __nv_bfloat16* out;
   uint32_t* seq_done;   // [b]: the split partials of sequence b stored
   int d_v;
-  int fuse, early;
+  int fuse, early, beside;
   // limit of every wait (ns); a test entry lowers it, together with a
   // withheld page copy (stall_cta, stall_tile; stall_cta < 0: none)
   uint64_t wait_ns;
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // Everything above touches only this CTA's shared and tensor memory; what
   // follows reads the query-absorption kernel's outputs (prepared queries,
   // split schedule, zeroed counters) and the cache it may have appended to.
-  grid_dependency_wait();
+  if (!p.beside) grid_dependency_wait();
 
   // an issuer's wait, the choice of the thread that issues, and the warp's joining after it
   auto issuer_wait = [&](uint64_t& bar, uint32_t parity) {
@@ -1562,6 +1562,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (!DUMP && D_C <= 256) {
     if (p.fuse) fused_combine<D_C, DBG == 2>(p, smem, bars);
   }
+  if (p.beside) grid_dependency_wait();
   phase_mark<DBG == 2>(p, 3);
 }
 
@@ -1636,6 +1637,7 @@ cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_
   p.seq_done = reinterpret_cast<uint32_t*>(ws + wl.off_done);
   p.d_v = a.d_v;
   p.early = a.early;
+  p.beside = a.beside;
   p.wait_ns = a.wait_ns;
   p.stall_cta = a.stall_cta;
   p.stall_tile = a.stall_tile;

@@ -26,6 +26,10 @@ namespace egmla {
 //    split-KV kernel triggers a separate combine only after its own wait.  (An
 //    L2 prefetch reads nothing that could be old.  The first projection's weights
 //    must not be written by the kernel directly before the layer call.)
+//  - a kernel may stand beside the one before it where it needs nothing of that one:
+//    that one lets it start only after its own wait (so that all before it is
+//    complete), and it waits at its end instead of its start (`beside`), so that its
+//    completion stands for both.
 // A kernel lets its successor start early (grid_launch_dependents) where that was
 // measured to pay: mostly where the successor's blocks take a whole SM each, since
 // smaller blocks, started early, crowd onto the first SMs to free up (the R0
@@ -160,6 +164,7 @@ struct DecodeArgs {
   void* out;
   int num_splits;
   int apart;   // the split combine always as a kernel of its own
+  int beside;  // the split-KV kernel runs beside the kernel before it (see launch_chained)
   int early;   // let the kernel after the split-KV kernel start early (it streams weights of its own)
   void* workspace;
   int32_t* status;
@@ -187,6 +192,7 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t st);
 struct AbsorbExtra {
   uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
   float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
+  int beside;       // runs beside the kernel before it (see launch_chained)
 };
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
                                const AbsorbExtra& extra = AbsorbExtra{});
@@ -216,8 +222,9 @@ cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool 
 // true if the bf16 tensor-core path has a kernel for these shapes
 bool tc_supported(int d_c, int gate);
 
-// Attention over a shared prefix (egmla_shared.cu): the gated prefix and the
-// partials of every sequence over it, into the workspace parts `wl` of `dec`.
+// Attention over a shared prefix (egmla_shared.cu): the gated prefix, and the
+// partials of every sequence over it, into the workspace parts `wl` of `dec`.  The
+// kernel after each may run beside it.
 // `maps`: the gated prefix (gate off: the latent pool), its last page (gate off),
 // the RoPE keys, each in boxes of one page.
 struct SharedArgs {
@@ -228,7 +235,8 @@ struct SharedArgs {
   int max_prefix_len, ctas;
 };
 bool shared_supported(int d_c);
-cudaError_t launch_shared(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st);
+cudaError_t launch_shared_gate(const SharedArgs& a, cudaStream_t st);
+cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st);
 
 // Pages of the cache (egmla_pages.cu); see include/egmla.h for what they compute.
 constexpr int kPlanMaxBatch = 16384;   // three words per sequence in shared memory

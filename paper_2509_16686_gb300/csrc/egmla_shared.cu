@@ -83,8 +83,8 @@ struct SharedGateParams {
 // pool itself: only the last page, where it is not full, is copied.
 __global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const SharedGateParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  grid_launch_dependents();
   grid_dependency_wait();
+  grid_launch_dependents();   // the query absorption, which runs beside this kernel
   const int given = __ldg(p.prefix_len), len = min(max(given, 0), p.max_len);
   if (given != len && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, kStatusOutOfRange);
   const int first = p.gate ? 0 : len / kPage * kPage;   // the row that z begins with
@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
   grid_dependency_wait();
+  grid_launch_dependents();   // the own tokens' split-KV kernel, beside this one where an SM has nothing left
   const int len = min(max(__ldg(p.prefix_len), 0), p.max_len);
   SaWalk walk(p);
   int t, lp0, lp1;
@@ -575,7 +576,7 @@ cudaError_t launch_attn(const SharedArgs& a, const CUtensorMap* maps, const Shar
 
 bool shared_supported(int d_c) { return d_c == 192 || d_c == 256; }
 
-cudaError_t launch_shared(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st) {
+cudaError_t launch_shared_gate(const SharedArgs& a, cudaStream_t st) {
   const DecodeArgs& d = *a.dec;
   uint8_t* ws = static_cast<uint8_t*>(d.workspace);
   SharedGateParams g;
@@ -595,9 +596,13 @@ cudaError_t launch_shared(const SharedArgs& a, const CUtensorMap* maps, cudaStre
   g.eps = d.eps;
   g.status = d.status;
   const int rows = static_cast<int>(shared_z_rows(a.max_prefix_len, d.gate != 0));
-  cudaError_t e = launch_chained(shared_gate_kernel, dim3((rows + kSgWarps * kSgRows - 1) / (kSgWarps * kSgRows)),
-                                 dim3(32 * kSgWarps), 0, st, g);
-  if (e != cudaSuccess) return e;
+  return launch_chained(shared_gate_kernel, dim3((rows + kSgWarps * kSgRows - 1) / (kSgWarps * kSgRows)),
+                        dim3(32 * kSgWarps), 0, st, g);
+}
+
+cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st) {
+  const DecodeArgs& d = *a.dec;
+  uint8_t* ws = static_cast<uint8_t*>(d.workspace);
   const WorkspaceLayout wl = workspace_layout(d.batch, d.num_splits, 16, d.d_c, d.d_rope, true);
   SharedAttnParams p;
   p.qprep = ws + wl.off_qprep;
