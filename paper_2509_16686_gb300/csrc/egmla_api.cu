@@ -376,7 +376,8 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
                 bool launch = true, const Prefix* prefix = nullptr, const Sparse* sparse = nullptr) {
   egmla::SharedArgs sh;
   if (prefix != nullptr) {
-    const int rc = shared_workspace(dims, batch, prefix->max_len, num_splits, &sh.wl, &sh.ctas);
+    int32_t splits = 0;
+    const int rc = shared_workspace(dims, batch, prefix->max_len, num_splits, &sh.wl, &splits);
     if (rc != EG_MLA_OK) return rc;
     if (prefix->len == nullptr || (prefix->table == nullptr && prefix->max_len > 0)) return EG_MLA_ERR_INVALID_ARG;
     if (workspace_bytes < sh.wl.total) return EG_MLA_ERR_WORKSPACE;
@@ -412,7 +413,7 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       sh.prefix_table = prefix->table;
       sh.prefix_len = parts.prefix_len = prefix->len;
       sh.max_prefix_len = parts.max_prefix_len = prefix->max_len;
-      parts.ctas = sh.ctas;
+      parts.gate = a.gate;
       parts.ml = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_ml);
       parts.o = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_o);
       a.apart = 1;   // the combine has a second list of partials
@@ -426,6 +427,11 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     if (sparse == nullptr) {
       if (with_prefix) e = egmla::launch_shared_gate(sh, st);
       extra.beside = with_prefix ? 1 : 0;
+      if (prefix != nullptr) {
+        extra.prefix_len = prefix->len;
+        extra.max_prefix_len = prefix->max_len;
+        extra.gate = a.gate;
+      }
       if (e == cudaSuccess) e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
     } else {
       // the queries, the pages by their scores, the schedule over the selected pages

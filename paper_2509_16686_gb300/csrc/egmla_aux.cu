@@ -145,14 +145,16 @@ __device__ void page_prefix_sums_block(const int32_t* seq_lens, int batch, int p
 }
 
 // Start record of every split (see SplitStart), from the prefix sums this
-// block just wrote (its shared copy).  Split c
+// block just wrote (its shared copy).  `total` units are cut for `splits` of the
+// num_splits splits (the others are empty).  Split c
 // owns units [c chunk, (c + 1) chunk); its first sequence is the last one whose
 // first unit is at most c chunk (empty sequences skipped), as in the decode
 // kernel's walk.
 __device__ void split_starts(const int32_t* cu, const int32_t* seq_lens, int batch, int num_splits,
-                             const int32_t* __restrict__ block_table, int max_pages, SplitStart* starts) {
+                             int splits, const int32_t* __restrict__ block_table, int max_pages,
+                             SplitStart* starts) {
   const int total = cu[batch];
-  const int chunk = split_chunk(total, num_splits);
+  const int chunk = split_chunk(total, splits);
   for (int c = threadIdx.x; c < num_splits; c += blockDim.x) {
     SplitStart st;
     const int g0 = c * chunk;
@@ -188,18 +190,24 @@ __device__ void split_starts(const int32_t* cu, const int32_t* seq_lens, int bat
 // prefix sums in shared memory too where they fit, so that the splits'
 // searches read them there; `wsum`: eight more ints.
 __device__ void schedule_block(const int32_t* seq_lens, int batch, int page_size, int32_t* cu, uint32_t* seq_done,
-                               int num_splits, const int32_t* block_table, int max_pages, SplitStart* starts,
-                               int32_t* smem, int words, int32_t* wsum) {
+                               int num_splits, const AbsorbExtra& extra, const int32_t* block_table, int max_pages,
+                               SplitStart* starts, int32_t* smem, int words, int32_t* wsum) {
+  // with a shared prefix the own tokens are cut for a part of the splits
+  auto cut_for = [&](int units) {
+    if (extra.prefix_len == nullptr) return num_splits;
+    return SharedSchedule(batch, min(max(__ldg(extra.prefix_len), 0), extra.max_prefix_len), num_splits, units,
+                          extra.gate != 0).own_splits;
+  };
   if (seq_done != nullptr)
     for (int i = threadIdx.x; i < batch; i += blockDim.x) seq_done[i] = 0u;
   if (batch + 1 <= words) {
     page_prefix_sums_block(seq_lens, batch, page_size, cu, smem, wsum);
     __syncthreads();   // the prefix sums are visible to the whole block
-    split_starts(smem, seq_lens, batch, num_splits, block_table, max_pages, starts);
+    split_starts(smem, seq_lens, batch, num_splits, cut_for(smem[batch]), block_table, max_pages, starts);
   } else {
     page_prefix_sums(seq_lens, batch, page_size, cu);
     __syncthreads();
-    split_starts(cu, seq_lens, batch, num_splits, block_table, max_pages, starts);
+    split_starts(cu, seq_lens, batch, num_splits, cut_for(cu[batch]), block_table, max_pages, starts);
   }
 }
 
@@ -262,8 +270,8 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       constexpr int kWords = 4096;
       static_assert(pm_smem(1, 16) >= 1024 + (kWords + 8) * 4, "schedule area");
       if (block_table != nullptr)
-        schedule_block(seq_lens, batch, page_size, cu, seq_done, num_splits, block_table, max_pages, starts, words + 8,
-                       kWords, words);
+        schedule_block(seq_lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
+                       words + 8, kWords, words);
     } else {
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);
@@ -507,8 +515,8 @@ prologue_f32_kernel(const float* __restrict__ q, const float* __restrict__ w_uk,
 //    added in group order.  The time is then a few round trips to L2 whatever
 //    the number of slots.
 // With SHARED the partials of a prefix that the batch shares follow those of the
-// sequence's own splits: the CTAs c0..c1 of SharedSchedule whose ranges meet its
-// row tile, kSharedTile partials apart.
+// sequence's own splits: those of SharedSchedule::ctas_of its row tile, kSharedTile
+// partials apart.
 // emit(j, f, o) is called for features f .. f + 3 of sequence b0 + j, by one
 // thread; the caller's next __syncthreads makes what it stored visible.
 constexpr int kCombineSlots = 128;
@@ -540,7 +548,11 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
   constexpr int kWarps = T / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nb = min(nt, batch - b0), ncol = d_c / 4, pairs = nt * ncol;
-  const int chunk = split_chunk(cu[batch], num_splits);
+  int splits = num_splits;
+  if constexpr (SHARED)
+    splits = SharedSchedule(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), num_splits, cu[batch],
+                            prefix.gate != 0).own_splits;
+  const int chunk = split_chunk(cu[batch], splits);
   const size_t mlstride = static_cast<size_t>(H) * 2, sstride = static_cast<size_t>(H) * d_c;
   // the slots of this warp's sequences (warp, warp + kWarps) and their maxima
   int n[2] = {0, 0};
@@ -562,14 +574,14 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
     pml[e] += (static_cast<size_t>(c0 + b) * H + h) * 2;
     if constexpr (SHARED) {
       n1[e] = n[e];
-      const SharedSchedule s(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), prefix.ctas);
-      if (s.pages > 0) {
-        const int t = b / kSharedTile, s0 = t * s.pages / s.chunk, s1 = ((t + 1) * s.pages - 1) / s.chunk;
-        const int first = (s0 + t) * kSharedTile + b % kSharedTile;
-        n[e] += s1 - s0 + 1;
-        pml2[e] += (static_cast<size_t>(first) * H + h) * 2;
-        if (lane == 0) sh.prefix0[j] = first;
-      }
+      const SharedSchedule s(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), num_splits,
+                             cu[batch], prefix.gate != 0);
+      const int t = b / kSharedTile;
+      int s0 = 0;
+      n[e] += s.ctas_of(t, s0);
+      const int first = (s0 + t) * kSharedTile + b % kSharedTile;
+      pml2[e] += (static_cast<size_t>(first) * H + h) * 2;
+      if (lane == 0) sh.prefix0[j] = first;
       if (lane == 0) sh.own[j] = n1[e];
     }
     if (lane == 0) {

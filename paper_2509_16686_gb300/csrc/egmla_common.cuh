@@ -131,17 +131,69 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
 }
 
 // Attention over a shared prefix (egmla_shared.cu).  A unit is (row tile of
-// kSharedTile sequences, prefix page), row tiles outermost; the units are cut into
-// equal contiguous ranges, one per CTA.  CTA c's partial of row tile t is slot
-// c + t (as for the splits above), kSharedTile sequences x H heads per slot.
+// kSharedTile sequences, prefix page).  Each row tile's pages are cut into `parts`
+// equal ranges, one per CTA, or, where that would leave too many CTAs without work,
+// all units (row tiles outermost) into equal contiguous ranges (parts = 0); a range that
+// meets two row tiles pays for the second about what kSharedSegCost pages cost (its
+// queries, the wait for the first scores, the partial's store).  CTA c's partial of row
+// tile t is slot c + t (as for the splits above), kSharedTile sequences x H heads per
+// slot.
+//
+// The prefix's attention and the own tokens' split-KV kernel run beside each other,
+// a CTA per SM: of `splits` CTAs each has as many as its share of the work, counted
+// in pages (of the schedules' units, 0.70 us a unit for the prefix, 1.37 for own
+// tokens with a gate, 0.93 without).  The rest of either grid has no work and leaves.
+// One after the other on all SMs, 64 sequences over 32K tokens took 59.5 us.
 constexpr int kSharedTile = 8;
+constexpr int kSharedSegCost = 8;
 
 struct SharedSchedule {
-  int pages, units, chunk;
-  __host__ __device__ SharedSchedule(int batch, int prefix_len, int ctas) {
+  int pages, units, chunk, parts;
+  int own_splits;   // CTAs that the own tokens are cut for
+  // own_units: of the own tokens' schedule (its cu[batch])
+  __host__ __device__ SharedSchedule(int batch, int prefix_len, int splits, int own_units, bool gate) {
+    const int tiles = (batch + kSharedTile - 1) / kSharedTile;
     pages = (prefix_len + kPage - 1) / kPage;
-    units = (batch + kSharedTile - 1) / kSharedTile * pages;
+    units = tiles * pages;
+    own_splits = splits;
+    int ctas = splits;
+    if (units > 0 && splits > 1) {
+      const int64_t own = static_cast<int64_t>(own_units) * (gate ? 6 : 4), pre = static_cast<int64_t>(units) * 3;
+      own_splits = static_cast<int>((own * splits + own + pre - 1) / (own + pre));
+      own_splits = own_splits < 1 ? 1 : own_splits > splits - 1 ? splits - 1 : own_splits;
+      ctas = splits - own_splits;
+    }
     chunk = split_chunk(units, ctas);
+    parts = tiles > 0 ? ctas / tiles : 0;
+    if (parts > 0) {
+      const int alone = split_chunk(pages, parts);
+      if (alone <= chunk + kSharedSegCost)
+        chunk = alone;
+      else
+        parts = 0;
+    }
+  }
+  // the units of CTA c
+  __host__ __device__ void range(int c, int& u0, int& u1) const {
+    if (parts > 0) {
+      const int t = c / parts, lp = (c - t * parts) * chunk;
+      u0 = t * pages + lp;
+      u1 = t * pages + (lp + chunk < pages ? lp + chunk : pages);
+      if (u0 >= u1 || u1 > units) u0 = u1 = units;
+    } else {
+      u0 = c * chunk < units ? c * chunk : units;
+      u1 = u0 + chunk < units ? u0 + chunk : units;
+    }
+  }
+  // the CTAs c0 .. c0 + n - 1 that leave a partial of row tile t
+  __host__ __device__ int ctas_of(int t, int& c0) const {
+    if (pages == 0) return 0;
+    if (parts > 0) {
+      c0 = t * parts;
+      return (pages + chunk - 1) / chunk;
+    }
+    c0 = t * pages / chunk;
+    return ((t + 1) * pages - 1) / chunk - c0 + 1;
   }
 };
 

@@ -193,6 +193,9 @@ struct AbsorbExtra {
   uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
   float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
   int beside;       // runs beside the kernel before it (see launch_chained)
+  // a shared prefix, whose attention takes a part of the SMs (null: none; see SharedSchedule)
+  const int32_t* prefix_len;
+  int max_prefix_len, gate;
 };
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
                                const AbsorbExtra& extra = AbsorbExtra{});
@@ -208,7 +211,7 @@ struct SharedParts {
   const float* ml;
   const float* o;
   const int32_t* prefix_len;
-  int max_prefix_len, ctas;
+  int max_prefix_len, gate;
 };
 // `wmap` (tensor-core path): W_UV as {d_c, d_v, H} in boxes of {64, 128, 1};
 // `shared` (may be null; tensor-core path): a second list of partials
@@ -232,7 +235,7 @@ struct SharedArgs {
   SharedLayout wl;
   const int32_t* prefix_table;
   const int32_t* prefix_len;
-  int max_prefix_len, ctas;
+  int max_prefix_len;
 };
 bool shared_supported(int d_c);
 cudaError_t launch_shared_gate(const SharedArgs& a, cudaStream_t st);

@@ -157,9 +157,8 @@ __global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const Shared
 }
 
 // ============================================================================ 2. attention over the prefix
-// A unit is (row tile of 8 sequences, prefix page); the units, row tiles
-// outermost, are cut into equal contiguous ranges, one per CTA, and a CTA leaves
-// one partial per row tile that its range meets, in slot (CTA + row tile).
+// A unit is (row tile of 8 sequences, prefix page); a CTA takes a range of them
+// (SharedSchedule) and leaves one partial per row tile that its range meets.
 //
 // Tensor memory (512 columns): O [128 x D_C] fp32, two score buffers [128 x 64]
 // (P in bf16 written over the first half of each), and the latent part of the
@@ -194,7 +193,8 @@ struct SaCfg {
   static constexpr uint32_t kSlot = (kCols + 1) * kSaCol;
   static constexpr int kSlots = D_C == 256 ? 5 : 6;
   static constexpr uint32_t kOffRing = kSaRows * 128;             // after q^R
-  static constexpr uint32_t kOffBars = kOffRing + kSlots * kSlot;
+  static constexpr uint32_t kOffAffine = kOffRing + kSlots * kSlot;   // gamma, beta
+  static constexpr uint32_t kOffBars = kOffAffine + 2 * D_C * 4;
   static constexpr uint32_t kSmem = kOffBars + sizeof(SaBars) + 1024;
   static constexpr uint32_t kColS = 256, kColQ = 384;             // (O from column 0)
   static_assert(kSlots <= 8 && kSmem <= kSmemMost && kColQ + D_C / 2 <= 512, "shared and tensor memory");
@@ -206,6 +206,7 @@ struct SharedAttnParams {
   const uint8_t* q16;     // q^ gamma in f16
   const int32_t* table;
   const int32_t* prefix_len;
+  const int32_t* own_units;   // of the own tokens' schedule
   const float* gamma;   // null: 1
   const float* beta;    // null: 0
   float* part_ml;
@@ -220,10 +221,10 @@ struct SharedAttnParams {
 struct SaWalk {
   int pages, u, u1;   // pages of the prefix; the next unit and the range's end
   __device__ SaWalk(const SharedAttnParams& p) {
-    const SharedSchedule s(p.batch, min(max(__ldg(p.prefix_len), 0), p.max_len), gridDim.x);
+    const SharedSchedule s(p.batch, min(max(__ldg(p.prefix_len), 0), p.max_len), gridDim.x, __ldg(p.own_units),
+                           p.gate != 0);
     pages = s.pages;
-    u = min(static_cast<int>(blockIdx.x) * s.chunk, s.units);
-    u1 = min(u + s.chunk, s.units);
+    s.range(static_cast<int>(blockIdx.x), u, u1);
   }
   // row tile t, pages lp0 .. lp1 - 1; false at the end
   __device__ bool next(int& t, int& lp0, int& lp1) {
@@ -272,6 +273,11 @@ __global__ void __launch_bounds__(kSaThreads, 1)
   if (warp == 1) {
     tmem_alloc(smem_u32(&bars.tmem_base), 512);
     tmem_relinquish();
+  }
+  float* affine = reinterpret_cast<float*>(smem + C::kOffAffine);
+  for (int f = tid; f < D_C; f += kSaThreads) {   // (inputs: this kernel starts after all that comes before the call)
+    affine[f] = p.gamma ? __ldg(p.gamma + f) : 1.f;
+    affine[D_C + f] = p.beta ? __ldg(p.beta + f) : 0.f;
   }
   tc_fence_before();
   __syncthreads();
@@ -406,31 +412,44 @@ __global__ void __launch_bounds__(kSaThreads, 1)
         const uint8_t* lat = F16 ? p.q16 + bs * qprep_lat_bytes(D_C) : src;
         const bool live = b < p.batch;   // rows past the batch are zero
         constexpr int kHalf = D_C / 16;  // 16-byte units of half a row
+        uint4 xr[4];
 #pragma unroll
-        for (int u0 = 0; u0 < kHalf; u0 += 4) {
-          uint32_t v[16];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (live) x = __ldg(reinterpret_cast<const uint4*>(lat + qop_offset(h, 8 * (sub * kHalf + u0 + u))));
-            v[4 * u] = x.x;
-            v[4 * u + 1] = x.y;
-            v[4 * u + 2] = x.z;
-            v[4 * u + 3] = x.w;
-          }
-          tmem_st16(tmem + (static_cast<uint32_t>(32 * quad) << 16) + C::kColQ + 4 * (sub * kHalf + u0), v);
+        for (int u = 0; u < 4; ++u) {
+          xr[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (live)
+            xr[u] = __ldg(reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C) + qop_offset(h, 8 * (4 * sub + u))));
         }
 #pragma unroll
-        for (int u = 4 * sub; u < 4 * sub + 4; ++u) {
-          uint4 x = make_uint4(0u, 0u, 0u, 0u);
-          if (live) x = __ldg(reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C) + qop_offset(h, 8 * u)));
+        for (int u8 = 0; u8 < kHalf; u8 += 8) {
+          uint4 x[8];   // eight loads in flight
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            x[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (live && u8 + u < kHalf)
+              x[u] = __ldg(reinterpret_cast<const uint4*>(lat + qop_offset(h, 8 * (sub * kHalf + u8 + u))));
+          }
+#pragma unroll
+          for (int u0 = 0; u0 < 8 && u8 + u0 < kHalf; u0 += 4) {
+            uint32_t v[16];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              v[4 * u] = x[u0 + u].x;
+              v[4 * u + 1] = x[u0 + u].y;
+              v[4 * u + 2] = x[u0 + u].z;
+              v[4 * u + 3] = x[u0 + u].w;
+            }
+            tmem_st16(tmem + (static_cast<uint32_t>(32 * quad) << 16) + C::kColQ + 4 * (sub * kHalf + u8 + u0), v);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
           if constexpr (F16) {   // exact: the exponent alone changes
             const __nv_bfloat162 f = __float2bfloat162_rn(kShQScale);
-            __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&x);
+            __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&xr[u]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = __hmul2(w[i], f);
           }
-          *reinterpret_cast<uint4*>(smem + row * 128 + ((u ^ (row & 7)) << 4)) = x;
+          *reinterpret_cast<uint4*>(smem + row * 128 + (((4 * sub + u) ^ (row & 7)) << 4)) = xr[u];
         }
         tmem_wait_st();
         fence_proxy_async_smem();
@@ -543,9 +562,8 @@ __global__ void __launch_bounds__(kSaThreads, 1)
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const int f = 64 * g + 8 * k + c2;
-            float2 gm = make_float2(1.f, 1.f), bt = make_float2(0.f, 0.f);
-            if (p.gamma != nullptr) gm = make_float2(__ldg(p.gamma + f), __ldg(p.gamma + f + 1));
-            if (p.beta != nullptr) bt = make_float2(__ldg(p.beta + f), __ldg(p.beta + f + 1));
+            const float2 gm = *reinterpret_cast<const float2*>(affine + f);
+            const float2 bt = *reinterpret_cast<const float2*>(affine + D_C + f);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
               *reinterpret_cast<float2*>(p.part_o + (row + 8 * e) * D_C + f) =
@@ -568,7 +586,7 @@ template <int D_C, bool F16>
 cudaError_t launch_attn(const SharedArgs& a, const CUtensorMap* maps, const SharedAttnParams& p, cudaStream_t st) {
   const cudaError_t e = allow_smem(shared_attn_kernel<D_C, F16>, SaCfg<D_C>::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_chained(shared_attn_kernel<D_C, F16>, dim3(a.ctas), dim3(kSaThreads), SaCfg<D_C>::kSmem, st, maps[0],
+  return launch_chained(shared_attn_kernel<D_C, F16>, dim3(a.dec->num_splits), dim3(kSaThreads), SaCfg<D_C>::kSmem, st, maps[0],
                         maps[1], maps[2], p);
 }
 
@@ -610,6 +628,7 @@ cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cud
   p.q16 = ws + a.wl.off_q;
   p.table = a.prefix_table;
   p.prefix_len = a.prefix_len;
+  p.own_units = reinterpret_cast<const int32_t*>(ws + wl.off_cu) + d.batch;
   p.gamma = d.gate_ln ? d.ln_gamma : nullptr;
   p.beta = d.gate_ln ? d.ln_beta : nullptr;
   p.part_ml = reinterpret_cast<float*>(ws + a.wl.off_ml);
