@@ -411,9 +411,9 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     if (prefix != nullptr) {
       sh.dec = &a;
       sh.prefix_table = prefix->table;
-      sh.prefix_len = parts.prefix_len = prefix->len;
-      sh.max_prefix_len = parts.max_prefix_len = prefix->max_len;
-      parts.gate = a.gate;
+      sh.prefix_len = prefix->len;
+      sh.max_prefix_len = prefix->max_len;
+      parts.sched = reinterpret_cast<const egmla::SharedSchedule*>(static_cast<uint8_t*>(workspace) + sh.wl.off_sched);
       parts.ml = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_ml);
       parts.o = reinterpret_cast<const float*>(static_cast<uint8_t*>(workspace) + sh.wl.off_o);
       a.apart = 1;   // the combine has a second list of partials
@@ -425,14 +425,15 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     const bool with_prefix = prefix != nullptr && prefix->max_len > 0;
     cudaError_t e = cudaSuccess;
     if (sparse == nullptr) {
-      if (with_prefix) e = egmla::launch_shared_gate(sh, st);
-      extra.beside = with_prefix ? 1 : 0;
+      extra.chain = with_prefix ? 1 : 0;
       if (prefix != nullptr) {
         extra.prefix_len = prefix->len;
         extra.max_prefix_len = prefix->max_len;
         extra.gate = a.gate;
+        extra.sched = const_cast<egmla::SharedSchedule*>(parts.sched);
       }
-      if (e == cudaSuccess) e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
+      e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
+      if (e == cudaSuccess && with_prefix) e = egmla::launch_shared_gate(sh, st);
     } else {
       // the queries, the pages by their scores, the schedule over the selected pages
       extra.q32 = sparse->q;

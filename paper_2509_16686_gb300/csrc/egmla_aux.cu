@@ -192,11 +192,30 @@ __device__ void split_starts(const int32_t* cu, const int32_t* seq_lens, int bat
 __device__ void schedule_block(const int32_t* seq_lens, int batch, int page_size, int32_t* cu, uint32_t* seq_done,
                                int num_splits, const AbsorbExtra& extra, const int32_t* block_table, int max_pages,
                                SplitStart* starts, int32_t* smem, int words, int32_t* wsum) {
-  // with a shared prefix the own tokens are cut for a part of the splits
+  // With a shared prefix the own tokens are cut for a part of the splits: each thread
+  // weighs some of the choices, the cheapest (of equals the fewest own splits) is written.
   auto cut_for = [&](int units) {
     if (extra.prefix_len == nullptr) return num_splits;
-    return SharedSchedule(batch, min(max(__ldg(extra.prefix_len), 0), extra.max_prefix_len), num_splits, units,
-                          extra.gate != 0).own_splits;
+    const int len = min(max(__ldg(extra.prefix_len), 0), extra.max_prefix_len);
+    const bool both = len > 0 && num_splits > 1;
+    unsigned long long best = ~0ull;
+    for (int own = 1 + threadIdx.x; both && own < num_splits; own += blockDim.x) {
+      int cost;
+      SharedSchedule::make(batch, len, num_splits, own, units, extra.gate != 0, cost);
+      best = min(best, static_cast<unsigned long long>(cost) << 32 | static_cast<unsigned>(own));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
+    __shared__ unsigned long long bests[32];
+    if ((threadIdx.x & 31) == 0) bests[threadIdx.x >> 5] = best;
+    __syncthreads();
+    for (int w = 0; w < static_cast<int>(blockDim.x) / 32; ++w) best = min(best, bests[w]);
+    const int own = both ? static_cast<int>(best & 0xffffffffu) : num_splits;
+    if (threadIdx.x == 0) {
+      int cost;
+      *extra.sched = SharedSchedule::make(batch, len, num_splits, own, units, extra.gate != 0, cost);
+    }
+    return own;
   };
   if (seq_done != nullptr)
     for (int i = threadIdx.x; i < batch; i += blockDim.x) seq_done[i] = 0u;
@@ -263,8 +282,9 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   const int ntiles = q != nullptr ? H * mt * nbg : 0;   // (the cache-read test entry: the schedule only)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (blockIdx.x == 0 || blockIdx.x > static_cast<unsigned>(ntiles)) {
-    grid_launch_dependents();
-    if (!extra.beside) grid_dependency_wait();
+    if (!extra.chain) grid_launch_dependents();
+    grid_dependency_wait();
+    if (extra.chain) grid_launch_dependents();
     if (blockIdx.x == 0) {
       int32_t* words = reinterpret_cast<int32_t*>(smem);
       constexpr int kWords = 4096;
@@ -276,7 +296,6 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);
     }
-    if (extra.beside) grid_dependency_wait();
     return;
   }
   const int item = static_cast<int>(blockIdx.x) - 1;
@@ -308,8 +327,9 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
-  grid_launch_dependents();
-  if (!extra.beside) grid_dependency_wait();
+  if (!extra.chain) grid_launch_dependents();
+  grid_dependency_wait();
+  if (extra.chain) grid_launch_dependents();
   if (warp == 0) {
     if (elect_one()) {
       const uint64_t keep = policy_evict_last(), once = policy_evict_first();
@@ -407,7 +427,6 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, tmem_cols);
   if (tid == 0 && *abort_flag) report_status(status, kStatusTimeout);
-  if (extra.beside) grid_dependency_wait();
 }
 
 // fp32 path: q^ [H, d_c] and q^R [H, d_rope] in fp32, row-major.  Block 0: the
@@ -549,9 +568,11 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nb = min(nt, batch - b0), ncol = d_c / 4, pairs = nt * ncol;
   int splits = num_splits;
-  if constexpr (SHARED)
-    splits = SharedSchedule(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), num_splits, cu[batch],
-                            prefix.gate != 0).own_splits;
+  SharedSchedule sched;
+  if constexpr (SHARED) {
+    sched = *prefix.sched;
+    splits = sched.own_splits;
+  }
   const int chunk = split_chunk(cu[batch], splits);
   const size_t mlstride = static_cast<size_t>(H) * 2, sstride = static_cast<size_t>(H) * d_c;
   // the slots of this warp's sequences (warp, warp + kWarps) and their maxima
@@ -574,11 +595,9 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
     pml[e] += (static_cast<size_t>(c0 + b) * H + h) * 2;
     if constexpr (SHARED) {
       n1[e] = n[e];
-      const SharedSchedule s(batch, min(max(__ldg(prefix.prefix_len), 0), prefix.max_prefix_len), num_splits,
-                             cu[batch], prefix.gate != 0);
       const int t = b / kSharedTile;
       int s0 = 0;
-      n[e] += s.ctas_of(t, s0);
+      n[e] += sched.ctas_of(t, s0);
       const int first = (s0 + t) * kSharedTile + b % kSharedTile;
       pml2[e] += (static_cast<size_t>(first) * H + h) * 2;
       if (lane == 0) sh.prefix0[j] = first;

@@ -132,49 +132,56 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
 
 // Attention over a shared prefix (egmla_shared.cu).  A unit is (row tile of
 // kSharedTile sequences, prefix page).  Each row tile's pages are cut into `parts`
-// equal ranges, one per CTA, or, where that would leave too many CTAs without work,
-// all units (row tiles outermost) into equal contiguous ranges (parts = 0); a range that
-// meets two row tiles pays for the second about what kSharedSegCost pages cost (its
-// queries, the wait for the first scores, the partial's store).  CTA c's partial of row
-// tile t is slot c + t (as for the splits above), kSharedTile sequences x H heads per
-// slot.
+// equal ranges, one per CTA, or (parts = 0) all units, row tiles outermost, into equal
+// contiguous ranges; a range that meets two row tiles leaves two partials.  CTA c's
+// partial of row tile t is slot c + t (as for the splits above), kSharedTile sequences x
+// H heads per slot.
 //
-// The prefix's attention and the own tokens' split-KV kernel run beside each other,
-// a CTA per SM: of `splits` CTAs each has as many as its share of the work, counted
-// in pages (of the schedules' units, 0.70 us a unit for the prefix, 1.37 for own
-// tokens with a gate, 0.93 without).  The rest of either grid has no work and leaves.
-// One after the other on all SMs, 64 sequences over 32K tokens took 59.5 us.
+// The prefix's attention and the own tokens' split-KV kernel run beside each other, a
+// CTA per SM: own_splits of the num_splits CTAs are for the own tokens (cut as above),
+// the rest for the prefix; what is left of either grid has no work and leaves.  Of
+// all such cuts the one whose longer side is shortest, by what was measured (in 10 ns):
+// a prefix unit, a page of own tokens with and without a gate, and what a CTA of either
+// kind takes besides (its queries, first scores and partial), the prefix's again for a
+// second row tile.  One after the other on all SMs, 64 sequences over 32K tokens took
+// 59.5 us a call, beside each other 57.0.
 constexpr int kSharedTile = 8;
-constexpr int kSharedSegCost = 8;
+constexpr int kShUnitCost = 70, kShOwnGated = 137, kShOwnPlain = 93, kShFixed = 700, kShOwnFixed = 500;
 
-struct SharedSchedule {
-  int pages, units, chunk, parts;
-  int own_splits;   // CTAs that the own tokens are cut for
-  // own_units: of the own tokens' schedule (its cu[batch])
-  __host__ __device__ SharedSchedule(int batch, int prefix_len, int splits, int own_units, bool gate) {
+struct alignas(16) SharedSchedule {
+  int32_t pages, chunk, parts, own_splits;
+
+  // for `own` of `splits` CTAs; cost: of the longer side.  own_units: of the own
+  // tokens' schedule (its cu[batch])
+  static __host__ __device__ SharedSchedule make(int batch, int prefix_len, int splits, int own, int own_units,
+                                                 bool gate, int& cost) {
+    SharedSchedule s;
     const int tiles = (batch + kSharedTile - 1) / kSharedTile;
-    pages = (prefix_len + kPage - 1) / kPage;
-    units = tiles * pages;
-    own_splits = splits;
-    int ctas = splits;
-    if (units > 0 && splits > 1) {
-      const int64_t own = static_cast<int64_t>(own_units) * (gate ? 6 : 4), pre = static_cast<int64_t>(units) * 3;
-      own_splits = static_cast<int>((own * splits + own + pre - 1) / (own + pre));
-      own_splits = own_splits < 1 ? 1 : own_splits > splits - 1 ? splits - 1 : own_splits;
-      ctas = splits - own_splits;
+    s.pages = (prefix_len + kPage - 1) / kPage;
+    s.own_splits = own;
+    const int ctas = splits > own ? splits - own : 1, units = tiles * s.pages;
+    s.chunk = split_chunk(units, ctas);
+    s.parts = tiles > 0 ? ctas / tiles : 0;
+    int64_t pre = static_cast<int64_t>(s.chunk) * kShUnitCost + kShFixed;
+    if (s.pages % s.chunk != 0 && tiles > 1) pre += kShFixed;
+    if (s.parts > 0) {
+      const int chunk = split_chunk(s.pages, s.parts);
+      if (static_cast<int64_t>(chunk) * kShUnitCost + kShFixed <= pre) {
+        s.chunk = chunk;
+        pre = static_cast<int64_t>(chunk) * kShUnitCost + kShFixed;
+      } else {
+        s.parts = 0;
+      }
     }
-    chunk = split_chunk(units, ctas);
-    parts = tiles > 0 ? ctas / tiles : 0;
-    if (parts > 0) {
-      const int alone = split_chunk(pages, parts);
-      if (alone <= chunk + kSharedSegCost)
-        chunk = alone;
-      else
-        parts = 0;
-    }
+    int64_t most = own_units > 0 ? kShOwnFixed : 0;
+    if (own_units > 0) most += static_cast<int64_t>(split_chunk(own_units, own)) * (gate ? kShOwnGated : kShOwnPlain);
+    if (pre > most) most = pre;
+    cost = static_cast<int>(most < INT32_MAX ? most : INT32_MAX);
+    return s;
   }
   // the units of CTA c
-  __host__ __device__ void range(int c, int& u0, int& u1) const {
+  __host__ __device__ void range(int batch, int c, int& u0, int& u1) const {
+    const int units = (batch + kSharedTile - 1) / kSharedTile * pages;
     if (parts > 0) {
       const int t = c / parts, lp = (c - t * parts) * chunk;
       u0 = t * pages + lp;
@@ -187,6 +194,7 @@ struct SharedSchedule {
   }
   // the CTAs c0 .. c0 + n - 1 that leave a partial of row tile t
   __host__ __device__ int ctas_of(int t, int& c0) const {
+    c0 = 0;
     if (pages == 0) return 0;
     if (parts > 0) {
       c0 = t * parts;
@@ -214,7 +222,7 @@ __host__ __device__ inline size_t shared_z_rows(int max_prefix_len, bool gate) {
 
 // after the own tokens' decode workspace (`base` bytes)
 struct SharedLayout {
-  size_t off_q, off_z, off_ml, off_o, total;
+  size_t off_sched, off_q, off_z, off_ml, off_o, total;
 };
 
 __host__ __device__ inline SharedLayout shared_layout(size_t base, int batch, int max_prefix_len, int ctas, int H,
@@ -222,6 +230,8 @@ __host__ __device__ inline SharedLayout shared_layout(size_t base, int batch, in
   SharedLayout w;
   const size_t slots = static_cast<size_t>(ctas) + (batch + kSharedTile - 1) / kSharedTile;
   size_t off = align_up(base, 256);
+  w.off_sched = off;
+  off = align_up(off + sizeof(SharedSchedule), 256);
   w.off_q = off;   // q^ gamma in f16, laid out as in the prepared query blocks
   off = align_up(off + static_cast<size_t>(batch) * qprep_lat_bytes(d_c), 256);
   w.off_z = off;

@@ -192,10 +192,12 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t st);
 struct AbsorbExtra {
   uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
   float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
-  int beside;       // runs beside the kernel before it (see launch_chained)
-  // a shared prefix, whose attention takes a part of the SMs (null: none; see SharedSchedule)
+  int chain;        // the kernel after this one runs beside it (see launch_chained)
+  // a shared prefix, whose attention takes a part of the SMs (null: none): its length,
+  // and where the schedule of both is written
   const int32_t* prefix_len;
   int max_prefix_len, gate;
+  SharedSchedule* sched;
 };
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,
                                const AbsorbExtra& extra = AbsorbExtra{});
@@ -210,8 +212,7 @@ cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaSt
 struct SharedParts {
   const float* ml;
   const float* o;
-  const int32_t* prefix_len;
-  int max_prefix_len, gate;
+  const SharedSchedule* sched;
 };
 // `wmap` (tensor-core path): W_UV as {d_c, d_v, H} in boxes of {64, 128, 1};
 // `shared` (may be null; tensor-core path): a second list of partials
@@ -225,9 +226,9 @@ cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool 
 // true if the bf16 tensor-core path has a kernel for these shapes
 bool tc_supported(int d_c, int gate);
 
-// Attention over a shared prefix (egmla_shared.cu): the gated prefix, and the
-// partials of every sequence over it, into the workspace parts `wl` of `dec`.  The
-// kernel after each may run beside it.
+// Attention over a shared prefix (egmla_shared.cu): the gated prefix (runs beside the
+// absorption), and the partials of every sequence over it (the kernel after it may run
+// beside it), into the workspace parts `wl` of `dec`.
 // `maps`: the gated prefix (gate off: the latent pool), its last page (gate off),
 // the RoPE keys, each in boxes of one page.
 struct SharedArgs {

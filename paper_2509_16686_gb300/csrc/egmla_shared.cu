@@ -83,15 +83,18 @@ struct SharedGateParams {
 // pool itself: only the last page, where it is not full, is copied.
 __global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const SharedGateParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  grid_dependency_wait();
-  grid_launch_dependents();   // the query absorption, which runs beside this kernel
+  // beside the query absorption (nothing here needs it): its wait comes at the end
+  grid_launch_dependents();
   const int given = __ldg(p.prefix_len), len = min(max(given, 0), p.max_len);
   if (given != len && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, kStatusOutOfRange);
   const int first = p.gate ? 0 : len / kPage * kPage;   // the row that z begins with
   const int rows = (len + kPage - 1) / kPage * kPage - first;
   const int t0 = (blockIdx.x * kSgWarps + warp) * kSgRows;
   const bool live = lane < p.d_c / 8;   // a lane holds eight features
-  if (t0 >= rows) return;
+  if (t0 >= rows) {
+    grid_dependency_wait();
+    return;
+  }
   // four rows never straddle a page
   const int page = __ldg(p.table + (first + t0) / kPage);
   const bool page_ok = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
@@ -154,6 +157,7 @@ __global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const Shared
     if (live) *(reinterpret_cast<uint4*>(p.z + static_cast<size_t>(t0 + r) * p.d_c) + lane) = out;
   }
   if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
+  grid_dependency_wait();
 }
 
 // ============================================================================ 2. attention over the prefix
@@ -206,7 +210,7 @@ struct SharedAttnParams {
   const uint8_t* q16;     // q^ gamma in f16
   const int32_t* table;
   const int32_t* prefix_len;
-  const int32_t* own_units;   // of the own tokens' schedule
+  const SharedSchedule* sched;
   const float* gamma;   // null: 1
   const float* beta;    // null: 0
   float* part_ml;
@@ -221,10 +225,10 @@ struct SharedAttnParams {
 struct SaWalk {
   int pages, u, u1;   // pages of the prefix; the next unit and the range's end
   __device__ SaWalk(const SharedAttnParams& p) {
-    const SharedSchedule s(p.batch, min(max(__ldg(p.prefix_len), 0), p.max_len), gridDim.x, __ldg(p.own_units),
-                           p.gate != 0);
+    const int4 v = __ldg(reinterpret_cast<const int4*>(p.sched));
+    const SharedSchedule s = {v.x, v.y, v.z, v.w};
     pages = s.pages;
-    s.range(static_cast<int>(blockIdx.x), u, u1);
+    s.range(p.batch, static_cast<int>(blockIdx.x), u, u1);
   }
   // row tile t, pages lp0 .. lp1 - 1; false at the end
   __device__ bool next(int& t, int& lp0, int& lp1) {
@@ -283,9 +287,9 @@ __global__ void __launch_bounds__(kSaThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
+  const int len = min(max(__ldg(p.prefix_len), 0), p.max_len);   // (an input too)
   grid_dependency_wait();
-  grid_launch_dependents();   // the own tokens' split-KV kernel, beside this one where an SM has nothing left
-  const int len = min(max(__ldg(p.prefix_len), 0), p.max_len);
+  grid_launch_dependents();   // the own tokens' split-KV kernel, beside this one
   SaWalk walk(p);
   int t, lp0, lp1;
 
@@ -628,7 +632,7 @@ cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cud
   p.q16 = ws + a.wl.off_q;
   p.table = a.prefix_table;
   p.prefix_len = a.prefix_len;
-  p.own_units = reinterpret_cast<const int32_t*>(ws + wl.off_cu) + d.batch;
+  p.sched = reinterpret_cast<const SharedSchedule*>(ws + a.wl.off_sched);
   p.gamma = d.gate_ln ? d.ln_gamma : nullptr;
   p.beta = d.gate_ln ? d.ln_beta : nullptr;
   p.part_ml = reinterpret_cast<float*>(ws + a.wl.off_ml);
