@@ -563,7 +563,8 @@ __device__ void merge_partials(MergeShared<TS>& sh, const int32_t* cu, const flo
                                int batch, int H, int h, int b0, int nt, int d_c, int num_splits, Emit emit,
                                const SharedParts& prefix = SharedParts()) {
   static_assert(T <= TS, "threads");
-  constexpr int kFlight = PPT >= 4 ? 4 : 8;   // slots of a pair in flight
+  // slots of a pair in flight; with a shared prefix a sequence has tens of them
+  constexpr int kFlight = PPT >= 4 ? 4 : SHARED && PPT == 1 ? 16 : 8;
   constexpr int kWarps = T / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nb = min(nt, batch - b0), ncol = d_c / 4, pairs = nt * ncol;

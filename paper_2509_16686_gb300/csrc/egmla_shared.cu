@@ -186,7 +186,7 @@ constexpr float kSaLazyLog2 = 8.f;              // how far a row's maximum runs 
 struct SaBars {
   uint64_t full[8], empty[8];
   uint64_t sfull[2], pfull[2];
-  uint64_t qfull, odone, drain;
+  uint64_t qfull, qfree, odone, drain;
   uint32_t tmem_base;
   int abort;
 };
@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
       mbar_init(smem_u32(&bars.pfull[x]), kSaSoftWarps);
     }
     mbar_init(smem_u32(&bars.qfull), kSaSoftWarps);
+    mbar_init(smem_u32(&bars.qfree), kSaSoftWarps);
     mbar_init(smem_u32(&bars.odone), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     bars.abort = 0;
@@ -403,9 +404,14 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(32 * quad + 16 * sub) << 16);
     const int r0 = lane >> 2, c2 = 2 * (lane & 3);
     const float sl2 = p.scale_log2 * (F16 ? 1.f / kShQScale : 1.f);
-    int n = 0;
+    // a partial leaves through the memory of q^R, which is read no more by then: 2 KB a warp
+    uint8_t* stage = smem + (warp - 2) * 2048;
+    int n = 0, seg = 0;
     bool ok = true;
     while (ok && walk.next(t, lp0, lp1)) {
+      // (the last partial has left that memory)
+      if (seg > 0 && !sh_warp_wait(smem_u32(&bars.qfree), (seg - 1) & 1, abort_flag, p.wait_ns)) break;
+      ++seg;
       // the tile's queries (every MMA that read the last tile's is complete).  A lane
       // takes its row of the quadrant, this warp one half of its latent features
       // (the A operand in tensor memory) and of its RoPE part (shared memory).
@@ -460,6 +466,17 @@ __global__ void __launch_bounds__(kSaThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.qfull));
+      }
+      // the constant q^ . beta of a row's scores, from its per-chunk partials
+      float bias[2] = {0.f, 0.f};
+      if (p.beta != nullptr) {
+        const float* sums = reinterpret_cast<const float*>(p.qprep + static_cast<size_t>(min(t * kSaSeqs + seq, p.batch - 1)) *
+                                                                         p.qstride +
+                                                           qprep_lat_bytes(D_C) + qprep_rope_bytes(64));
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int c = 0; c < D_C / kSumFeatures; ++c) bias[e] += __ldg(sums + c * 32 + 16 + r0 + 8 * e);
       }
       float m_ref[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
       for (int lp = lp0; ok && lp < lp1; ++lp, ++n) {
@@ -546,37 +563,44 @@ __global__ void __launch_bounds__(kSaThreads, 1)
       const int b = t * kSaSeqs + seq;
       const size_t row = (static_cast<size_t>(blockIdx.x + t) * kSaSeqs + seq) * 16 + r0;   // and row + 8
       if (b < p.batch && (lane & 3) == 0) {
-        // the constant q^ . beta of a row's scores, from its per-chunk partials
-        const float* sums = reinterpret_cast<const float*>(p.qprep + static_cast<size_t>(b) * p.qstride +
-                                                           qprep_lat_bytes(D_C) + qprep_rope_bytes(64));
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float bias = 0.f;
-          if (p.beta != nullptr)
-            for (int c = 0; c < D_C / kSumFeatures; ++c) bias += __ldg(sums + c * 32 + 16 + r0 + 8 * e);
-          *reinterpret_cast<float2*>(p.part_ml + (row + 8 * e) * 2) = make_float2(fmaf(bias, p.scale_log2, m_ref[e] - kPShift), l[e]);
-        }
+        for (int e = 0; e < 2; ++e)
+          *reinterpret_cast<float2*>(p.part_ml + (row + 8 * e) * 2) =
+              make_float2(fmaf(bias[e], p.scale_log2, m_ref[e] - kPShift), l[e]);
       }
 #pragma unroll
       for (int g = 0; g < C::kCols; ++g) {
         float o[32];
         tmem_ld_16x256b_x8(lane_base + 64 * g, o);
         tmem_wait_ld();
-        if (b < p.batch) {
+        if (b >= p.batch) continue;   // uniform in the warp
+        // 32 columns at a time through shared memory, so that a store covers whole lines
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int k = 4 * half; k < 4 * half + 4; ++k) {
             const int f = 64 * g + 8 * k + c2;
             const float2 gm = *reinterpret_cast<const float2*>(affine + f);
             const float2 bt = *reinterpret_cast<const float2*>(affine + D_C + f);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              *reinterpret_cast<float2*>(p.part_o + (row + 8 * e) * D_C + f) =
+            for (int e = 0; e < 2; ++e) {
+              const int rr = r0 + 8 * e, u = ((8 * k + c2) & 31) >> 2;
+              *reinterpret_cast<float2*>(stage + rr * 128 + ((u ^ (rr & 7)) << 4) + (c2 & 2) * 4) =
                   make_float2(fmaf(gm.x, o[4 * k + 2 * e], bt.x * l[e]), fmaf(gm.y, o[4 * k + 2 * e + 1], bt.y * l[e]));
+            }
           }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int rr = 4 * i + (lane >> 3), u = lane & 7;
+            const float4 x = *reinterpret_cast<const float4*>(stage + rr * 128 + ((u ^ (rr & 7)) << 4));
+            *reinterpret_cast<float4*>(p.part_o + (row - r0 + rr) * D_C + 64 * g + 32 * half + 4 * u) = x;
+          }
+          __syncwarp();
         }
-        __syncwarp();
       }
       tc_fence_before();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.qfree));
     }
   }
   tc_fence_before();
