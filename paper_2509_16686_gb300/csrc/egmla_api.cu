@@ -689,7 +689,8 @@ int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void*
   if (c_pool == nullptr || krope_pool == nullptr || block_table == nullptr || seq_lens == nullptr ||
       summary == nullptr || (gate && (id_pool == nullptr || gate_table == nullptr)))
     return EG_MLA_ERR_INVALID_ARG;
-  if (!aligned(c_pool, 16) || !aligned(krope_pool, 16) || !aligned(summary, 16) || (gate && !aligned(gate_table, 16)))
+  if (!aligned(c_pool, 16) || !aligned(krope_pool, 16) || !aligned(summary, 16) ||
+      (gate && (!aligned(gate_table, 16) || !aligned(id_pool, 16))))
     return EG_MLA_ERR_INVALID_ARG;
   egmla::SummaryArgs a;
   a.max_new = new_tokens != nullptr && max_new_tokens < max_seq_len ? max_new_tokens : max_seq_len;
@@ -714,11 +715,9 @@ int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void*
   a.max_seq_len = max_seq_len;
   a.num_pages = num_pages;
   a.fp32 = dims->dtype == EG_MLA_FP32;
-  a.gate = gate;
-  a.gate_add = dims->gate_mode == EG_MLA_GATE_ADD_LN;
-  a.gate_ln = dims->gate_mode == EG_MLA_GATE_MUL_LN || dims->gate_mode == EG_MLA_GATE_ADD_LN;
-  a.gamma = a.gate_ln ? ln_gamma : nullptr;
-  a.beta = a.gate_ln ? ln_beta : nullptr;
+  a.gate_mode = dims->gate_mode;
+  a.gamma = ln_gamma;
+  a.beta = ln_beta;
   a.eps = dims->ln_eps > 0.f ? dims->ln_eps : 1e-5f;
   return to_status(egmla::launch_page_summary(a, static_cast<cudaStream_t>(stream)));
 }

@@ -275,7 +275,7 @@ struct SummaryArgs {
   int32_t* status;
   int d_c, d_r, vocab, batch, max_pages, max_seq_len, num_pages;
   int max_new, page_bound;     // tokens and pages per sequence, at most
-  int fp32, gate, gate_add, gate_ln;
+  int fp32, gate_mode;
   float eps;
 };
 cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st);

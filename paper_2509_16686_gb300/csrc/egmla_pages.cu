@@ -198,38 +198,74 @@ constexpr int kSumWarps = 8;
 constexpr int kSumRows = kPage / kSumWarps;   // rows of a page per warp
 constexpr int kSumMaxDc = 512, kSumMaxDr = 64;
 
-__device__ __forceinline__ void widen16(const uint4& w, float (&x)[8]) {
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+// 16 bytes of a row as pairs of fp32 values
+template <typename T>
+struct Unit;
+template <>
+struct Unit<__nv_bfloat16> {
+  static constexpr int kPairs = 4;
+  static __device__ __forceinline__ void widen(const uint4& w, float2 (&x)[4]) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(v[i] << 16);
-    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
   }
-}
-__device__ __forceinline__ void widen16(const uint4& w, float (&x)[4]) {
-  x[0] = __uint_as_float(w.x);
-  x[1] = __uint_as_float(w.y);
-  x[2] = __uint_as_float(w.z);
-  x[3] = __uint_as_float(w.w);
-}
+};
+template <>
+struct Unit<float> {
+  static constexpr int kPairs = 2;
+  static __device__ __forceinline__ void widen(const uint4& w, float2 (&x)[2]) {
+    x[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    x[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+  }
+};
 
-// A block takes a page, a warp eight of its rows, a lane 16-byte units lane, lane +
-// 32, .. of a row (NU of them).  LayerNorm in two passes over the registers.  The mean of
-// gamma x_j + beta is gamma mean(x_j) + beta, so the affine part comes last.
-template <typename T, int NU>
-__global__ void __launch_bounds__(32 * kSumWarps) page_summary_kernel(const SummaryArgs p) {
-  constexpr int VE = 16 / sizeof(T);   // elements of a unit
+// v[r] summed over the warp's lanes, for every lane
+__device__ __forceinline__ void warp_sums(float (&v)[2], int lane) {
+  const bool h16 = lane & 16;
+  float c = (h16 ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, h16 ? v[0] : v[1], 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) v[r] = __shfl_sync(0xffffffffu, c, 16 * r);
+}
+__device__ __forceinline__ void warp_sums(float (&v)[4], int lane) {
+  const bool h16 = lane & 16, h8 = lane & 8;
+  const float a = (h16 ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, h16 ? v[0] : v[2], 16);
+  const float b = (h16 ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, h16 ? v[1] : v[3], 16);
+  float c = (h8 ? b : a) + __shfl_xor_sync(0xffffffffu, h8 ? a : b, 8);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = __shfl_sync(0xffffffffu, c, 16 * (r >> 1) + 8 * (r & 1));
+}
+// A block takes a page, a warp eight of its rows, kFlight of them at a time with every
+// load in flight; a lane has 16-byte units lane, lane + 32, .. of a row (NU of them).  LayerNorm in two passes over the
+// registers, the sums of the rows in flight reduced together.  The mean of gamma x_j +
+// beta is gamma mean(x_j) + beta, so the affine part comes last.  k^R rows: a lane has one
+// unit of every few rows.
+// Bound by issue and latency (0.5 of the issue slots, 136 instructions a row, most of them
+// widening, the two passes and the two reductions): 57.0 us for 8 x 32K tokens at d_c
+// 256, 5.3 TB/s of cache and gate rows; floor 27.4.  GM, the gate mode, at compile time:
+// 59.2 -> 57.0.  Forms that copy the pages by TMA into a ring or keep the next page's ids
+// ahead in persistent blocks measured 57.1 and 73.2 and were not kept.
+template <typename T, int NU, int GM>
+__global__ void __launch_bounds__(32 * kSumWarps, NU == 4 ? 2 : 3) page_summary_kernel(const SummaryArgs p) {
+  using U = Unit<T>;
+  constexpr bool GATE = GM != EG_MLA_GATE_NONE, GATE_ADD = GM == EG_MLA_GATE_ADD_LN;
+  constexpr bool GATE_LN = GM == EG_MLA_GATE_MUL_LN || GM == EG_MLA_GATE_ADD_LN;
+  constexpr int VP = U::kPairs, VE = 2 * VP;   // pairs and elements of a unit
+  constexpr int kFlight = NU == 1 ? 4 : 2;
   __shared__ float part[kSumWarps][kSumMaxDc + kSumMaxDr];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = blockIdx.x / p.page_bound, i = blockIdx.x - b * p.page_bound;
   grid_dependency_wait();
   int L = __ldg(p.seq_lens + b);
+  int n = p.new_tokens != nullptr ? __ldg(p.new_tokens + b) : L;
   bool bad = false;
   if (L < 0 || L > p.max_seq_len) {
     bad = true;
     L = L < 0 ? 0 : p.max_seq_len;
   }
-  int n = p.new_tokens != nullptr ? __ldg(p.new_tokens + b) : L;
   n = min(max(n, 0), L);
   if (n > p.max_new) {
     bad = true;
@@ -245,99 +281,120 @@ __global__ void __launch_bounds__(32 * kSumWarps) page_summary_kernel(const Summ
   }
   const int units = p.d_c / VE, runits = p.d_r / VE;
   const size_t row0 = static_cast<size_t>(page) * kPage + warp * kSumRows;
-  const T* c = static_cast<const T*>(p.c_pool) + row0 * p.d_c;
   const T* kr = static_cast<const T*>(p.kr_pool) + row0 * p.d_r;
-  int ids[kSumRows];
-  bad = false;
+  // k^R: unit lane % rw of rows lane / rw, + 32 / rw, ..  (rw: the units of a row, padded)
+  int rw = 1;
+  while (rw < runits) rw *= 2;
+  const int ru = lane & (rw - 1);
+  float2 racc[VP];
 #pragma unroll
-  for (int r = 0; r < kSumRows; ++r) {
-    ids[r] = p.gate ? __ldg(p.id_pool + row0 + r) : 0;
-    if (p.gate && static_cast<unsigned>(ids[r]) >= static_cast<unsigned>(p.vocab)) {
-      bad = true;
-      ids[r] = 0;
+  for (int e = 0; e < VP; ++e) racc[e] = make_float2(0.f, 0.f);
+  for (int r = lane / rw; r < kSumRows; r += 32 / rw) {
+    if (ru < runits) {
+      float2 t[VP];
+      U::widen(__ldg(reinterpret_cast<const uint4*>(kr + static_cast<size_t>(r) * p.d_r) + ru), t);
+#pragma unroll
+      for (int e = 0; e < VP; ++e) racc[e] = __fadd2_rn(racc[e], t[e]);
     }
   }
-  float acc[NU][VE], racc[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) racc[e] = 0.f;
+  int id_row = 0;   // lane r: row r's token
+  if (GATE && lane < kSumRows) id_row = __ldg(p.id_pool + row0 + lane);
+  if (GATE && static_cast<unsigned>(id_row) >= static_cast<unsigned>(p.vocab)) {
+    report_status(p.status, kStatusOutOfRange);
+    id_row = 0;
+  }
+  float2 acc[NU][VP];
 #pragma unroll
   for (int u = 0; u < NU; ++u)
 #pragma unroll
-    for (int e = 0; e < VE; ++e) acc[u][e] = 0.f;
-  constexpr int kFlight = NU == 1 ? 4 : 2;   // rows whose loads are in flight together
+    for (int e = 0; e < VP; ++e) acc[u][e] = make_float2(0.f, 0.f);
+  const T* c = static_cast<const T*>(p.c_pool) + row0 * p.d_c;
+  const T* table = static_cast<const T*>(p.gate_table);
   const float inv_n = 1.f / static_cast<float>(p.d_c);
-#pragma unroll
+#pragma unroll 1
   for (int r0 = 0; r0 < kSumRows; r0 += kFlight) {
-    uint4 cw[kFlight][NU], gw[kFlight][NU], rw[kFlight];
+    uint4 cw[kFlight][NU], gw[kFlight][NU];
 #pragma unroll
     for (int r = 0; r < kFlight; ++r) {
+      const int id = __shfl_sync(0xffffffffu, id_row, r0 + r);
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         const int at = lane + 32 * u;
         cw[r][u] = gw[r][u] = make_uint4(0u, 0u, 0u, 0u);
         if (at < units) {
           cw[r][u] = __ldg(reinterpret_cast<const uint4*>(c + static_cast<size_t>(r0 + r) * p.d_c) + at);
-          if (p.gate)
-            gw[r][u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.gate_table) +
-                                                            static_cast<size_t>(ids[r0 + r]) * p.d_c) + at);
+          if (GATE) gw[r][u] = __ldg(reinterpret_cast<const uint4*>(table + static_cast<size_t>(id) * p.d_c) + at);
         }
       }
-      rw[r] = make_uint4(0u, 0u, 0u, 0u);
-      if (lane < runits) rw[r] = __ldg(reinterpret_cast<const uint4*>(kr + static_cast<size_t>(r0 + r) * p.d_r) + lane);
     }
+    float2 x[kFlight][NU][VP];
+    float s[kFlight];
 #pragma unroll
     for (int r = 0; r < kFlight; ++r) {
-      float x[NU][VE], t[VE];
-      float sum = 0.f;
+      float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
-        widen16(cw[r][u], x[u]);
-        widen16(gw[r][u], t);
+        float2 t[VP];
+        U::widen(cw[r][u], x[r][u]);
+        if (GATE) U::widen(gw[r][u], t);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          if (p.gate) x[u][e] = p.gate_add ? x[u][e] + t[e] : x[u][e] * t[e];
-          sum += x[u][e];
+        for (int e = 0; e < VP; ++e) {
+          if (GATE) x[r][u][e] = GATE_ADD ? __fadd2_rn(x[r][u][e], t[e]) : __fmul2_rn(x[r][u][e], t[e]);
+          sum = __fadd2_rn(sum, x[r][u][e]);
         }
       }
-      if (p.gate_ln) {
+      s[r] = sum.x + sum.y;
+    }
+    if (GATE_LN) {
+      warp_sums(s, lane);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float mu = sum * inv_n;
-        float sq = 0.f;
+      for (int r = 0; r < kFlight; ++r) {
+        const float2 mu = make_float2(-s[r] * inv_n, -s[r] * inv_n);
+        float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < NU; ++u) {
+          const bool live = lane + 32 * u < units;
 #pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            x[u][e] = lane + 32 * u < units ? x[u][e] - mu : 0.f;
-            sq = fmaf(x[u][e], x[u][e], sq);
+          for (int e = 0; e < VP; ++e) {
+            x[r][u][e] = live ? __fadd2_rn(x[r][u][e], mu) : make_float2(0.f, 0.f);
+            sq = __ffma2_rn(x[r][u][e], x[r][u][e], sq);
           }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        const float rstd = rsqrtf(fmaf(sq, inv_n, p.eps));
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int e = 0; e < VE; ++e) acc[u][e] = fmaf(x[u][e], rstd, acc[u][e]);
-      } else {
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int e = 0; e < VE; ++e) acc[u][e] += x[u][e];
+        }
+        s[r] = sq.x + sq.y;
       }
-      widen16(rw[r], t);
+      warp_sums(s, lane);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) racc[e] += t[e];
+      for (int r = 0; r < kFlight; ++r) {
+        const float rstd = rsqrtf(fmaf(s[r], inv_n, p.eps));
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int e = 0; e < VP; ++e) acc[u][e] = __ffma2_rn(x[r][u][e], make_float2(rstd, rstd), acc[u][e]);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < kFlight; ++r)
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int e = 0; e < VP; ++e) acc[u][e] = __fadd2_rn(acc[u][e], x[r][u][e]);
     }
   }
 #pragma unroll
   for (int u = 0; u < NU; ++u)
+    if (lane + 32 * u < units)
 #pragma unroll
-    for (int e = 0; e < VE; ++e)
-      if (lane + 32 * u < units) part[warp][VE * (lane + 32 * u) + e] = acc[u][e];
+      for (int e = 0; e < VP; ++e)
+        *reinterpret_cast<float2*>(&part[warp][VE * (lane + 32 * u) + 2 * e]) = acc[u][e];
+#pragma unroll
+  for (int e = 0; e < VP; ++e)
+    for (int o = rw; o < 32; o *= 2) {
+      racc[e].x += __shfl_xor_sync(0xffffffffu, racc[e].x, o);
+      racc[e].y += __shfl_xor_sync(0xffffffffu, racc[e].y, o);
+    }
   if (lane < runits)
 #pragma unroll
-    for (int e = 0; e < VE; ++e) part[warp][p.d_c + VE * lane + e] = racc[e];
-  if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
+    for (int e = 0; e < VP; ++e) *reinterpret_cast<float2*>(&part[warp][p.d_c + VE * lane + 2 * e]) = racc[e];
   __syncthreads();
   float* out = p.summary + static_cast<size_t>(page) * (p.d_c + p.d_r);
   for (int f = threadIdx.x; f < p.d_c + p.d_r; f += blockDim.x) {
@@ -345,7 +402,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) page_summary_kernel(const Summ
 #pragma unroll
     for (int w = 0; w < kSumWarps; ++w) s += part[w][f];   // in row order
     s *= 1.f / kPage;
-    if (p.gate_ln && f < p.d_c) s = fmaf(s, p.gamma ? __ldg(p.gamma + f) : 1.f, p.beta ? __ldg(p.beta + f) : 0.f);
+    if (GATE_LN && f < p.d_c) s = fmaf(s, p.gamma ? __ldg(p.gamma + f) : 1.f, p.beta ? __ldg(p.beta + f) : 0.f);
     out[f] = s;
   }
 }
@@ -553,18 +610,27 @@ cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, page_plan_kernel, a);
 }
 
-cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st) {
-  const int units = a.d_c * (a.fp32 ? 4 : 2) / 16;
+namespace {
+template <typename T, int NU>
+cudaError_t launch_summary(const SummaryArgs& a, cudaStream_t st) {
   auto launch = [&](auto kernel) {
     return launch_chained(kernel, dim3(static_cast<unsigned>(a.batch) * a.page_bound), dim3(32 * kSumWarps), 0, st, a);
   };
-  if (a.fp32) {
-    if (units <= 32) return launch(page_summary_kernel<float, 1>);
-    if (units <= 64) return launch(page_summary_kernel<float, 2>);
-    return launch(page_summary_kernel<float, 4>);
+  switch (a.gate_mode) {
+    case EG_MLA_GATE_MUL_LN: return launch(page_summary_kernel<T, NU, EG_MLA_GATE_MUL_LN>);
+    case EG_MLA_GATE_MUL: return launch(page_summary_kernel<T, NU, EG_MLA_GATE_MUL>);
+    case EG_MLA_GATE_ADD_LN: return launch(page_summary_kernel<T, NU, EG_MLA_GATE_ADD_LN>);
+    default: return launch(page_summary_kernel<T, NU, EG_MLA_GATE_NONE>);
   }
-  if (units <= 32) return launch(page_summary_kernel<__nv_bfloat16, 1>);
-  return launch(page_summary_kernel<__nv_bfloat16, 2>);
+}
+}  // namespace
+
+cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st) {
+  const int units = a.d_c * (a.fp32 ? 4 : 2) / 16;
+  if (a.fp32)
+    return units <= 32 ? launch_summary<float, 1>(a, st)
+                       : units <= 64 ? launch_summary<float, 2>(a, st) : launch_summary<float, 4>(a, st);
+  return units <= 32 ? launch_summary<__nv_bfloat16, 1>(a, st) : launch_summary<__nv_bfloat16, 2>(a, st);
 }
 
 int score_chunks(int max_seq_len, int keep_first, int keep_last) {
