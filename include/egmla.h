@@ -294,8 +294,8 @@ int eg_mla_decode_shared(const eg_mla_dims* dims, const void* q, const void* c_p
  *                   page * 64 + offset of the cache it belongs in, -1 for the
  *                   entries past cu_seqlens[batch]; may be NULL
  *   batch           at most 16384; num_pages * 64 + batch * 64, batch *
- *                   max_pages_per_seq and max_pages_per_seq * 64 within 32 bits
- *                   (EG_MLA_ERR_UNSUPPORTED otherwise)
+ *                   max_pages_per_seq and max_pages_per_seq * 64 within 32 bits, and
+ *                   max_slots below 2^31 - 2^20 (EG_MLA_ERR_UNSUPPORTED otherwise)
  * The results do not depend on timing.  Other arguments must not overlap.
  * Device errors: EG_MLA_ERR_NO_PAGES if a request was refused (which ones:
  * cu_seqlens) and nothing was out of range; EG_MLA_ERR_OUT_OF_RANGE for a length outside 0 ..

@@ -337,10 +337,11 @@ struct Prefix {
   int32_t max_len;
 };
 
-// the pages to attend over (eg_mla_decode_sparse): the decode's block table and
-// lengths are those that `select` writes
+// the pages to attend over (eg_mla_decode_sparse): the decode's block table is the one
+// that `select` writes, its lengths are `lens`
 struct Sparse {
   egmla::SelectArgs select;
+  egmla::SparseLens lens;
   float* q;   // where the tensor-core path leaves the absorbed queries in fp32
 };
 
@@ -435,15 +436,14 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       e = egmla::launch_prologue_tc(a, app, amaps, st, extra);
       if (e == cudaSuccess && with_prefix) e = egmla::launch_shared_gate(sh, st);
     } else {
-      // the queries, the pages by their scores, the schedule over the selected pages
+      // the queries, and the schedule for what will be left of the sequences; then the pages
       extra.q32 = sparse->q;
+      extra.sparse = sparse->lens;
       DecodeArgs part = a;
+      part.seq_lens = sparse->select.seq_lens;
       part.block_table = nullptr;
       e = egmla::launch_prologue_tc(part, app, amaps, st, extra);
       if (e == cudaSuccess) e = egmla::launch_select_pages(sparse->select, st);
-      part = a;
-      part.q = nullptr;
-      if (e == cudaSuccess) e = egmla::launch_prologue_tc(part, nullptr, amaps, st);
     }
     if (e == cudaSuccess && with_prefix) e = egmla::launch_shared_attn(sh, smaps, st);
     bool fused = false;
@@ -461,15 +461,16 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     }
     return to_status(e);
   }
-  cudaError_t e = cudaSuccess;
-  if (sparse != nullptr) {
+  cudaError_t e;
+  if (sparse == nullptr) {
+    e = egmla::launch_prologue_f32(a, app, st);
+  } else {
     DecodeArgs part = a;
     part.seq_lens = sparse->select.seq_lens;
-    e = egmla::launch_prologue_f32(part, app, st);
+    e = egmla::launch_prologue_f32(part, app, st, sparse->lens);
     if (e == cudaSuccess) e = egmla::launch_select_pages(sparse->select, st);
-    app = nullptr;
   }
-  if (e == cudaSuccess) e = egmla::launch_decode_f32(a, app, st);
+  if (e == cudaSuccess) e = egmla::launch_decode_f32(a, st);
   if (e == cudaSuccess) e = egmla::launch_combine(a, false, nullptr, st);
   return to_status(e);
 }
@@ -640,8 +641,6 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Sparse sp;
   egmla::SelectArgs& s = sp.select;
-  s.chunks = egmla::score_chunks(max_seq_len, keep_first, keep_last);
-  if (static_cast<int64_t>(s.chunks) * batch > INT32_MAX) return EG_MLA_ERR_UNSUPPORTED;
   sp.q = reinterpret_cast<float*>(ws + sl.off_q);
   // the fp32 path's prepared queries have this form
   s.q = is_tc_path(dims) ? sp.q : reinterpret_cast<const float*>(ws + wl.off_qprep);
@@ -651,8 +650,9 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
   s.seq_lens = seq_lens;
   s.scores = reinterpret_cast<float*>(ws + sl.off_scores);
   s.sel_table = reinterpret_cast<int32_t*>(ws + sl.off_table);
-  s.sel_lens = reinterpret_cast<int32_t*>(ws + sl.off_lens);
   s.selected = selected;
+  s.counters = reinterpret_cast<int32_t*>(ws + sl.off_counters);
+  sp.lens = {reinterpret_cast<int32_t*>(ws + sl.off_lens), s.counters, budget, max_seq_len};
   s.status = dev_status;
   s.H = dims->num_heads;
   s.d_c = dims->d_c;
@@ -666,8 +666,10 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
   s.keep_last = keep_last;
   s.width = sl.width;
   s.scale = resolve_scale(dims);
+  egmla::select_blocks(s);
+  if (static_cast<int64_t>(s.chunks) * batch > INT32_MAX) return EG_MLA_ERR_UNSUPPORTED;
   const int64_t most = static_cast<int64_t>(sl.width) * dims->page_size;
-  return decode_impl(dims, q, c_pool, krope_pool, id_pool, s.sel_table, sl.width, s.sel_lens,
+  return decode_impl(dims, q, c_pool, krope_pool, id_pool, s.sel_table, sl.width, sp.lens.lens,
                      max_seq_len < most ? max_seq_len : static_cast<int32_t>(most), batch, num_pages, gate_table,
                      ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace, workspace_bytes, dev_status, nullptr,
                      static_cast<cudaStream_t>(stream), false, true, nullptr, &sp);
@@ -733,7 +735,7 @@ int eg_mla_page_plan(const int32_t* new_tokens, const int32_t* seq_lens, int32_t
     return EG_MLA_ERR_INVALID_ARG;
   // slots and every sum over the batch are 32-bit
   const int64_t page = egmla::kPage;
-  if (batch > egmla::kPlanMaxBatch || num_pages * page + batch * page > INT32_MAX ||
+  if (batch > egmla::kPlanMaxBatch || max_slots > INT32_MAX - (1 << 20) || num_pages * page + batch * page > INT32_MAX ||
       max_pages_per_seq * page > INT32_MAX || static_cast<int64_t>(batch) * max_pages_per_seq > INT32_MAX)
     return EG_MLA_ERR_UNSUPPORTED;
   egmla::PlanArgs a;

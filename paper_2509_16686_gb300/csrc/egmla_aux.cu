@@ -174,7 +174,8 @@ __device__ void split_starts(const int32_t* cu, const int32_t* seq_lens, int bat
       st.lp_end = min(st.g1, cu[lo + 1]) - base;
       st.L = seq_lens[lo];
       st.done = st.lp_end <= st.lp;
-      if (!st.done) st.npages = min(kStartPages, min(st.lp_end, max_pages) - st.lp);
+      // (no block table yet: the page-sparse decode's is made after the schedule)
+      if (!st.done && block_table != nullptr) st.npages = min(kStartPages, min(st.lp_end, max_pages) - st.lp);
     }
     for (int i = 0; i < kStartPages; ++i)
       st.page[i] = i < st.npages ? block_table[static_cast<size_t>(st.b) * max_pages + st.lp + i] : -1;
@@ -182,6 +183,17 @@ __device__ void split_starts(const int32_t* cu, const int32_t* seq_lens, int bat
     int4* dst = reinterpret_cast<int4*>(starts + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k) dst[k] = src[k];
+  }
+}
+
+// The page-sparse decode's lengths: what is left of each sequence when all but `budget`
+// of its pages are dropped (never its last one), known before the pages are; and its
+// selection's counters zeroed.
+__device__ void selected_lengths(const SparseLens& s, const int32_t* seq_lens, int batch) {
+  for (int b = threadIdx.x; b < batch; b += blockDim.x) {
+    const int L = min(max(seq_lens[b], 0), s.max_seq_len);
+    s.lens[b] = L - max((L + kPage - 1) / kPage - s.budget, 0) * kPage;
+    s.counters[b] = 0;
   }
 }
 
@@ -289,8 +301,11 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       int32_t* words = reinterpret_cast<int32_t*>(smem);
       constexpr int kWords = 4096;
       static_assert(pm_smem(1, 16) >= 1024 + (kWords + 8) * 4, "schedule area");
-      if (block_table != nullptr)
-        schedule_block(seq_lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
+      if (extra.sparse.lens != nullptr) {
+        selected_lengths(extra.sparse, seq_lens, batch);
+        __syncthreads();
+      }
+      schedule_block(extra.sparse.lens != nullptr ? extra.sparse.lens : seq_lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
                        words + 8, kWords, words);
     } else {
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
@@ -442,7 +457,7 @@ constexpr int kPfBatch = 8, kPfFeat = 64, kPfParts = 16, kPfRows = 8;
 __global__ void __launch_bounds__(256)
 prologue_f32_kernel(const float* __restrict__ q, const float* __restrict__ w_uk, const int32_t* __restrict__ seq_lens,
                     int batch, int H, int d_nope, int d_rope, int d_c, int page_size, uint8_t* __restrict__ qprep,
-                    size_t qstride, int32_t* __restrict__ cu, const AppendArgs app) {
+                    size_t qstride, int32_t* __restrict__ cu, const AppendArgs app, const SparseLens sparse) {
   __shared__ float qn[kPfBatch][256];
   __shared__ __align__(16) float red[kPfParts][kPfBatch][kPfFeat];
   const int nfc = (d_c + kPfFeat - 1) / kPfFeat, nbg = (batch + kPfBatch - 1) / kPfBatch;
@@ -450,7 +465,11 @@ prologue_f32_kernel(const float* __restrict__ q, const float* __restrict__ w_uk,
   grid_launch_dependents();
   grid_dependency_wait();
   if (blockIdx.x == 0) {
-    page_prefix_sums(seq_lens, batch, page_size, cu);
+    if (sparse.lens != nullptr) {
+      selected_lengths(sparse, seq_lens, batch);
+      __syncthreads();
+    }
+    page_prefix_sums(sparse.lens != nullptr ? sparse.lens : seq_lens, batch, page_size, cu);
     return;
   }
   if (blockIdx.x > static_cast<unsigned>(nabs)) {   // no block of this kernel reads the pools
@@ -1331,7 +1350,7 @@ cudaError_t launch_decode_f32_t(const DecodeArgs& a, const WorkspaceLayout& wl, 
 }
 }  // namespace
 
-cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st) {
+cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st, const SparseLens& sparse) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   AppendArgs none;
@@ -1343,12 +1362,10 @@ cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cuda
       prologue_f32_kernel, dim3(absorb + 1 + ap.batch), dim3(256), 0, st,
       static_cast<const float*>(a.q), static_cast<const float*>(a.w_uk), a.seq_lens, a.batch, a.H, a.d_nope,
       a.d_rope, a.d_c, a.page_size, ws + wl.off_qprep, wl.qprep_stride,
-      reinterpret_cast<int32_t*>(ws + wl.off_cu), ap);
+      reinterpret_cast<int32_t*>(ws + wl.off_cu), ap, sparse);
 }
 
-cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st) {
-  const cudaError_t e = launch_prologue_f32(a, app, st);
-  if (e != cudaSuccess) return e;
+cudaError_t launch_decode_f32(const DecodeArgs& a, cudaStream_t st) {
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
   if (a.d_c <= 128) return launch_decode_f32_t<1>(a, wl, st);
   if (a.d_c <= 256) return launch_decode_f32_t<2>(a, wl, st);

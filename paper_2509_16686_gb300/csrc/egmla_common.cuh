@@ -247,7 +247,7 @@ __host__ __device__ inline SharedLayout shared_layout(size_t base, int batch, in
 // the page-sparse decode's own part of the workspace, after the decode workspace
 // (`base` bytes) of the selected pages
 struct SparseLayout {
-  size_t off_q, off_scores, off_table, off_lens, total;
+  size_t off_q, off_scores, off_table, off_lens, off_counters, total;
   size_t q_stride;   // floats
   int width;         // pages of the selected block table
 };
@@ -265,6 +265,8 @@ __host__ __device__ inline SparseLayout sparse_layout(size_t base, int batch, in
   w.off_table = off;
   off = align_up(off + static_cast<size_t>(batch) * w.width * 4, 256);
   w.off_lens = off;
+  off = align_up(off + static_cast<size_t>(batch) * 4, 256);
+  w.off_counters = off;
   off = align_up(off + static_cast<size_t>(batch) * 4, 256);
   w.total = off;
   return w;

@@ -187,11 +187,18 @@ cudaError_t launch_append(const AppendArgs& a, cudaStream_t st);
 // append the new token of every sequence (the pools are read by no block of it)
 // `maps`: W_UK as {d_c, d_nope, H} in boxes of {64, 64, 1} and q^C as {d_nope, H,
 // batch} in boxes of {64, 1, absorb_tile}
-// `extra`: the absorbed queries in other forms too.  a.q null: the schedule only;
-// a.block_table null: everything but the schedule
+// the page-sparse decode: the schedule is for these lengths, which are made from
+// seq_lens, before the pages are known (lens null: not that)
+struct SparseLens {
+  int32_t* lens;       // [batch]
+  int32_t* counters;   // [batch], zeroed
+  int budget, max_seq_len;
+};
+// `extra`: the absorbed queries in other forms too.  a.q null: the schedule only
 struct AbsorbExtra {
   uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
   float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
+  SparseLens sparse;
   int chain;        // the kernel after this one runs beside it (see launch_chained)
   // a shared prefix, whose attention takes a part of the SMs (null: none): its length,
   // and where the schedule of both is written
@@ -203,10 +210,12 @@ cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const
                                const AbsorbExtra& extra = AbsorbExtra{});
 // sequences per block of the absorption
 int absorb_tile(int d_c, int batch);
-// fp32: the absorption alone (q^ [H, d_c], then q^R [H, d_rope] per sequence)
-cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st);
-// fp32: absorption (with the append blocks of `app` when it is non-null) and the split-KV kernel
-cudaError_t launch_decode_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st);
+// fp32: absorption (with the append blocks of `app` when it is non-null; q^ [H, d_c],
+// then q^R [H, d_rope] per sequence) and page prefix sums
+cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cudaStream_t st,
+                                const SparseLens& sparse = SparseLens{});
+// the split-KV kernel after it
+cudaError_t launch_decode_f32(const DecodeArgs& a, cudaStream_t st);
 // The partials of a prefix that the batch shares, merged with the sequences' own
 // (combine of the tensor-core path); how they lie: see SharedSchedule.
 struct SharedParts {
@@ -289,15 +298,15 @@ struct SelectArgs {
   const int32_t* seq_lens;
   float* scores;          // [batch, max_pages]
   int32_t* sel_table;     // [batch, width]
-  int32_t* sel_lens;      // [batch]
   int32_t* selected;      // [batch, budget] logical pages, may be null
+  int32_t* counters;      // [batch], zeroed by the absorption
   int32_t* status;
   int H, d_c, d_r, batch, max_pages, max_seq_len, num_pages;
   int budget, keep_first, keep_last, width;
-  int chunks;             // score_chunks()
+  int chunks, rounds;     // blocks per sequence, groups of pages per block: set by select_blocks
   float scale;
 };
-int score_chunks(int max_seq_len, int keep_first, int keep_last);   // score blocks per sequence
+void select_blocks(SelectArgs& a);
 cudaError_t launch_select_pages(const SelectArgs& a, cudaStream_t st);
 
 // R0 decode (egmla_r0.cu): bf16, 16 heads, d_n = d_v = 128, d_r = 64,

@@ -5,17 +5,17 @@
 //                        table, the packed offsets and the cache slot of every new
 //                        token
 //   page_summary_kernel  the mean key [c~ ; k^R] of every page that became full
-//   page_scores_kernel   each sequence's pages by their mean keys: the largest
-//                        logit that any head gives it
-//   select_pages_kernel  the best pages of each sequence as a block table
+//   select_pages_kernel  each sequence's pages by the largest logit that any head gives
+//                        their mean key, the best of them as a block table
 //
-// The last three make the page-sparse decode: the split-KV kernels then attend over
+// The last two make the page-sparse decode: the split-KV kernels then attend over
 // the selected pages alone (a cached RoPE key carries its position, so a page may
 // stand anywhere in a block table).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "egmla_common.cuh"
 #include "egmla_kernels.h"
@@ -25,6 +25,35 @@ namespace egmla {
 namespace {
 
 __device__ __forceinline__ int pages_of(int n) { return (n + kPage - 1) / kPage; }
+
+// inclusive sums of two values over the block's threads; `total`: of all.  ws: a pair per warp
+__device__ __forceinline__ int2 block_scan2(int2 v, int2* ws, int2& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x / 32;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v.x, o), y = __shfl_up_sync(0xffffffffu, v.y, o);
+    if (lane >= o) {
+      v.x += x;
+      v.y += y;
+    }
+  }
+  if (lane == 31) ws[warp] = v;
+  __syncthreads();
+  int2 s = lane < nw ? ws[lane] : make_int2(0, 0);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, s.x, o), y = __shfl_up_sync(0xffffffffu, s.y, o);
+    if (lane >= o) {
+      s.x += x;
+      s.y += y;
+    }
+  }
+  total = make_int2(__shfl_sync(0xffffffffu, s.x, nw - 1), __shfl_sync(0xffffffffu, s.y, nw - 1));
+  const int bw = warp > 0 ? warp - 1 : 0;
+  const int bx = __shfl_sync(0xffffffffu, s.x, bw), by = __shfl_sync(0xffffffffu, s.y, bw);
+  __syncthreads();   // ws is rewritten by the next scan
+  return warp > 0 ? make_int2(v.x + bx, v.y + by) : v;
+}
 
 // inclusive sum over the block's threads; `total`: the sum of all.  ws: a word per warp
 __device__ __forceinline__ int block_scan(int v, int* ws, int& total) {
@@ -63,16 +92,16 @@ __device__ __forceinline__ int find_in(const int32_t* cum, int n, int x) {
 // sequence in its shared memory), and takes its share of the pages and slots.  The
 // first cluster barrier lets outputs overwrite inputs (seq_lens, free_count), the
 // second orders the pages pushed before those popped.
-constexpr int kPlanThreads = 512;
+constexpr int kPlanThreads = 1024;   // 256 for small steps (fewer warps to wait for)
 
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs p) {
   extern __shared__ int32_t plan_smem[];
-  __shared__ int ws[32];
+  __shared__ int2 ws[32];
   int32_t* E = plan_smem;              // [batch + 1] exclusive sums of the pages asked for
   int32_t* len = E + p.batch + 1;      // [batch] lengths before the step
   int32_t* cum = len + p.batch;        // [batch + 1] of the pages released, then of the tokens granted
-  const int tid = threadIdx.x, C = static_cast<int>(gridDim.x), rank = static_cast<int>(blockIdx.x);
-  const int first = rank * kPlanThreads + tid, step = C * kPlanThreads;   // this thread's share of a list
+  const int tid = threadIdx.x, T = blockDim.x, C = static_cast<int>(gridDim.x), rank = static_cast<int>(blockIdx.x);
+  const int first = rank * T + tid, step = C * T;   // this thread's share of a list
   const int64_t most = static_cast<int64_t>(p.max_pages) * kPage;
   grid_dependency_wait();
   const int given = __ldg(p.free_count);
@@ -90,20 +119,20 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
     return sane;
   };
   int total_need = 0, R = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < p.batch; b0 += T) {
     const int b = b0 + tid;
-    int L = 0, back = 0, need = 0, ask = 0, sum;
+    int L = 0, back = 0, need = 0, ask = 0;
     bool fits = true;
     if (b < p.batch && !request(b, L, back, need, ask, fits)) bad = true;
-    const int e = block_scan(need, ws, sum);
+    int2 sum;
+    const int2 v = block_scan2(make_int2(need, back), ws, sum);
     if (b < p.batch) {
-      E[b] = total_need + e - need;
+      E[b] = total_need + v.x - need;
       len[b] = L;
+      cum[b] = R + v.y - back;
     }
-    total_need += sum;
-    const int r = block_scan(back, ws, sum);
-    if (b < p.batch) cum[b] = R + r - back;
-    R += sum;
+    total_need += sum.x;
+    R += sum.y;
   }
   if (tid == 0) {
     E[p.batch] = total_need;
@@ -126,9 +155,9 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   }
   // what is granted, first come first served
   int total = 0, granted_pages = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < p.batch; b0 += T) {
     const int b = b0 + tid;
-    int t = 0, g = 0, L = 0, sum;
+    int t = 0, g = 0, L = 0;
     if (b < p.batch) {
       L = len[b];
       const int n = __ldg(p.new_tokens + b), need = E[b + 1] - E[b];
@@ -147,12 +176,12 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
         if (p.positions) p.positions[b] = t > 0 ? L : -1;
       }
     }
-    const int c = block_scan(t, ws, sum);
-    if (b < p.batch) cum[b] = total + c - t;
-    if (b < p.batch && b % C == rank) p.cu_seqlens[b] = total + c - t;
-    total += sum;
-    block_scan(g, ws, sum);
-    granted_pages += sum;
+    int2 sum;
+    const int2 v = block_scan2(make_int2(t, g), ws, sum);
+    if (b < p.batch) cum[b] = total + v.x - t;
+    if (b < p.batch && b % C == rank) p.cu_seqlens[b] = total + v.x - t;
+    total += sum.x;
+    granted_pages += sum.y;
   }
   if (tid == 0) cum[p.batch] = total;
   if (tid == 0 && rank == 0) {
@@ -170,20 +199,49 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   // the new tokens' slots
   if (p.slots != nullptr) {
     if (total > p.max_slots) bad = true;
-    for (int k = first; k < p.max_slots; k += step) {
-      int slot = -1;
-      if (k < total) {
-        const int b = find_in(cum, p.batch, k);
-        const int pos = len[b] + (k - cum[b]), lp = pos / kPage, have = pages_of(len[b]);
-        const int page = lp < have ? p.block_table[static_cast<size_t>(b) * p.max_pages + lp]
-                                   : p.free_pages[avail - 1 - (E[b] + lp - have)];
-        if (static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages))
-          slot = page * kPage + pos % kPage;
+    const bool vec = (reinterpret_cast<uintptr_t>(p.slots) & 15) == 0;
+    // G slots of a thread in a row: one search for them
+    auto fill = [&](auto g) {
+      constexpr int G = decltype(g)::value;
+      for (int k0 = first * G; k0 < p.max_slots; k0 += step * G) {
+        int b = k0 < total ? find_in(cum, p.batch, k0) : 0;
+        int page[G], off[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {   // (no load depends on another)
+          const int k = k0 + i;
+          page[i] = -1;
+          off[i] = 0;
+          if (k < total) {
+            while (cum[b + 1] <= k) ++b;
+            const int L = len[b], pos = L + (k - cum[b]), lp = pos / kPage, have = pages_of(L);
+            const int32_t* src = lp < have ? p.block_table + static_cast<size_t>(b) * p.max_pages + lp
+                                           : p.free_pages + (avail - 1 - (E[b] + lp - have));
+            page[i] = *src;
+            off[i] = pos % kPage;
+          }
+        }
+        int slot[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const bool in = static_cast<unsigned>(page[i]) < static_cast<unsigned>(p.num_pages);
+          slot[i] = in ? page[i] * kPage + off[i] : -1;
+          if (!in && k0 + i < total) bad = true;
+        }
+        if (G >= 4 && vec && k0 + G <= p.max_slots)
+#pragma unroll
+          for (int i = 0; i < G; i += 4)
+            *reinterpret_cast<int4*>(p.slots + k0 + i) =
+                make_int4(slot[i], slot[(i + 1) % G], slot[(i + 2) % G], slot[(i + 3) % G]);
         else
-          bad = true;
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+            if (k0 + i < p.max_slots) p.slots[k0 + i] = slot[i];
       }
-      p.slots[k] = slot;
-    }
+    };
+    if (p.max_slots <= step)
+      fill(std::integral_constant<int, 1>{});
+    else
+      fill(std::integral_constant<int, 8>{});
   }
   // a refusal (which every CTA has seen) is reported where nothing is out of range
   if (bad) report_status(p.status, kStatusOutOfRange);
@@ -407,12 +465,23 @@ __global__ void __launch_bounds__(32 * kSumWarps, NU == 4 ? 2 : 3) page_summary_
   }
 }
 
-// ============================================================================ 3. page scores
-// score(b, p) = max_h scale (q^_bh . m^c_p + q^R_bh . m^R_p) in exact fp32 products.
-// A block takes a sequence's queries into shared memory and kScPages of its pages; a
-// warp four pages at a time, so that a query value read serves four products.  Lanes
-// share a row; the 16 heads' sums of two pages take one transposing reduction.
-constexpr int kScWarps = 8, kScPages = 32, kScHeads = 16;
+// ============================================================================ 3. page selection
+// score(b, p) = max_h scale (q^_bh . m^c_p + q^R_bh . m^R_p), fp32 products and sums.
+// One launch: a block scores 8 PP pages of a sequence, `rounds` times (its queries in
+// shared memory, a warp PP pages at a time, so that a query value read serves PP
+// products; lanes share a row, the heads' sums take one transposing reduction); the last
+// block of a sequence to finish selects its pages.  The lengths that are left do not
+// depend on the choice, so the split-KV schedule is already made (selected_lengths).
+//
+// The selection: scores as whole numbers of the same order (no number comes last); the
+// want-th largest by up to four passes over a histogram of eight bits each; then, in
+// order, the pages above it and the first of those equal to it, between the pages that
+// are always kept.
+constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32, kScHeads = 16;
+constexpr int kSelKeys = 4096;   // scores kept in shared memory; of more the rest is read again
+
+// pages of a warp at a time, by the row's 16-byte units per lane
+__host__ __device__ constexpr int score_pages(int nu) { return nu <= 3 ? 4 : 2; }
 
 // v[i] summed over the warp's lanes, value t returned to lane t
 __device__ __forceinline__ float sum32_transpose(float (&v)[32], int lane) {
@@ -430,156 +499,209 @@ __device__ __forceinline__ float sum32_transpose(float (&v)[32], int lane) {
   return v[0];
 }
 
-__global__ void __launch_bounds__(32 * kScWarps) page_scores_kernel(const SelectArgs p) {
-  extern __shared__ float4 sc_q[];   // [kScHeads][units]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int b = blockIdx.x / p.chunks, D = p.d_c + p.d_r, units = D / 4;
-  grid_dependency_wait();
-  const int np = pages_of(min(max(__ldg(p.seq_lens + b), 0), p.max_seq_len));
-  if (np <= p.budget) return;   // every page is taken
-  const int lo = p.keep_first, hi = np - p.keep_last;   // the pages that are ranked
-  const int p0 = lo + (blockIdx.x - b * p.chunks) * kScPages;
-  if (p0 >= hi) return;
-  const float* q = p.q + static_cast<size_t>(b) * p.q_stride;
-  for (int i = threadIdx.x; i < kScHeads * units; i += blockDim.x) {
-    const int h = i / units, u = i - h * units;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (h < p.H)
-      v = 4 * u < p.d_c ? *reinterpret_cast<const float4*>(q + h * p.d_c + 4 * u)
-                        : *reinterpret_cast<const float4*>(q + p.H * p.d_c + h * p.d_r + 4 * u - p.d_c);
-    sc_q[i] = v;
-  }
-  __syncthreads();
-  const int w0 = p0 + 4 * warp;
-  if (w0 >= hi) return;
-  const float4* row[4];
-  bool bad = false;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    int page = __ldg(p.block_table + static_cast<size_t>(b) * p.max_pages + min(w0 + k, hi - 1));
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) {
-      bad = true;
-      page = 0;
-    }
-    row[k] = reinterpret_cast<const float4*>(p.summary + static_cast<size_t>(page) * D);
-  }
-  float acc[2][32];   // pages 2 i and 2 i + 1: [page % 2][head]
-#pragma unroll
-  for (int i = 0; i < 32; ++i) acc[0][i] = acc[1][i] = 0.f;
-  for (int u = lane; u < units; u += 32) {
-    float4 m[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = __ldg(row[k] + u);
-#pragma unroll
-    for (int h = 0; h < kScHeads; ++h) {
-      const float4 x = sc_q[h * units + u];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float& a = acc[k / 2][16 * (k % 2) + h];
-        a = fmaf(x.x, m[k].x, a);
-        a = fmaf(x.y, m[k].y, a);
-        a = fmaf(x.z, m[k].z, a);
-        a = fmaf(x.w, m[k].w, a);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float s = sum32_transpose(acc[i], lane);
-    if ((lane & 15) >= p.H) s = -INFINITY;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-    const int lp = w0 + 2 * i + (lane >> 4);
-    if ((lane & 15) == 0 && lp < hi) p.scores[static_cast<size_t>(b) * p.max_pages + lp] = s * p.scale;
-  }
-  if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
-}
-
-// ============================================================================ 4. page selection
-// A block per sequence.  The ranked pages' scores as whole numbers of the same order
-// (no number comes last); the count-th largest by four passes over a histogram of
-// eight bits each; then the pages above it and the first of those equal to it, in
-// order, between the pages that are always kept.
-constexpr int kSelThreads = 256;
-
 __device__ __forceinline__ uint32_t score_key(float s) {
   const uint32_t u = __float_as_uint(s);
   return s != s ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSelThreads) select_pages_kernel(const SelectArgs p) {
+__device__ __forceinline__ void copy16_async(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
+// one of the block's threads announces that the block is done (of `of`); true for the
+// whole block if it is the last, which then sees what the others wrote
+__device__ __forceinline__ bool last_to_finish(int32_t* count, int of, int* flag) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    *flag = atomicAdd(count, 1) == of - 1;
+  }
+  __syncthreads();
+  const bool last = *flag != 0;
+  if (last) __threadfence();
+  return last;
+}
+
+template <int NU>
+__global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const SelectArgs p) {
+  constexpr int PP = score_pages(NU);
+  extern __shared__ __align__(16) uint8_t sel_smem[];
   __shared__ int hist[256];
-  __shared__ int ws[32];
-  __shared__ uint32_t sh_digit;
-  __shared__ int sh_above;
-  const int b = blockIdx.x, tid = threadIdx.x;
+  __shared__ int ws[32], flag, digit, above;
+  float4* sq = reinterpret_cast<float4*>(sel_smem);            // [kScHeads][units]
+  uint2* keys = reinterpret_cast<uint2*>(sel_smem);            // afterwards: (key, page id)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = blockIdx.x / p.chunks, j = blockIdx.x - b * p.chunks;
+  const int D = p.d_c + p.d_r, units = D / 4;
   grid_dependency_wait();
   const int given = __ldg(p.seq_lens + b);
-  const int L = min(max(given, 0), p.max_seq_len);
-  const int np = pages_of(L);
-  if (given != L && tid == 0) report_status(p.status, kStatusOutOfRange);
+  const int L = min(max(given, 0), p.max_seq_len), np = (L + kPage - 1) / kPage;
   const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_pages;
+  float* scores = p.scores + static_cast<size_t>(b) * p.max_pages;
+  // of a longer sequence the pages lo .. hi - 1 are ranked, `want` of them taken
+  const int lo = p.keep_first, hi = np - p.keep_last, want = p.budget - p.keep_first - p.keep_last;
+  const bool ranked = np > p.budget && want > 0;
+  const int per = kSelWarps * PP * p.rounds, blocks = ranked ? (hi - lo + per - 1) / per : 1;
+  if (j >= blocks) return;
+  if (given != L && j == 0 && tid == 0) report_status(p.status, kStatusOutOfRange);
+  if (ranked) {
+    const float* q = p.q + static_cast<size_t>(b) * p.q_stride;
+    for (int h = warp; h < kScHeads; h += kSelWarps)
+      for (int u = lane; u < units; u += 32) {
+        float4* dst = sq + h * units + u;
+        if (h >= p.H)
+          *dst = make_float4(0.f, 0.f, 0.f, 0.f);
+        else if (4 * u < p.d_c)
+          copy16_async(dst, q + h * p.d_c + 4 * u);
+        else
+          copy16_async(dst, q + p.H * p.d_c + h * p.d_r + 4 * u - p.d_c);
+      }
+    bool bad = false, staged = false;
+    for (int r = 0; r < p.rounds; ++r) {
+      const int w0 = lo + ((j * p.rounds + r) * kSelWarps + warp) * PP;
+      if (staged && w0 >= hi) break;
+      float4 m[PP][NU];
+#pragma unroll
+      for (int k = 0; k < PP; ++k) {
+        int page = __ldg(table + min(w0 + k, hi - 1));
+        if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) {
+          bad = true;
+          page = 0;
+        }
+        const float4* row = reinterpret_cast<const float4*>(p.summary + static_cast<size_t>(page) * D);
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+          m[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (lane + 32 * i < units) m[k][i] = __ldg(row + lane + 32 * i);
+        }
+      }
+      if (!staged) {   // (every warp comes here once)
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        staged = true;
+        if (w0 >= hi) break;
+      }
+      // the heads in passes of HH, 32 sums a pass: [page][head]
+      constexpr int HH = 32 / PP;
+      float best = -INFINITY;   // lane l: of page l / HH
+#pragma unroll
+      for (int h0 = 0; h0 < kScHeads; h0 += HH) {
+        float acc[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+          const bool in = lane + 32 * i < units;   // (past the row both are zero)
+#pragma unroll
+          for (int h = 0; h < HH; ++h) {
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (in) x = sq[(h0 + h) * units + lane + 32 * i];
+#pragma unroll
+            for (int k = 0; k < PP; ++k) {
+              float& a = acc[k * HH + h];
+              a = fmaf(x.x, m[k][i].x, a);
+              a = fmaf(x.y, m[k][i].y, a);
+              a = fmaf(x.z, m[k][i].z, a);
+              a = fmaf(x.w, m[k][i].w, a);
+            }
+          }
+        }
+        const float t = sum32_transpose(acc, lane);
+        if (h0 + lane % HH < p.H) best = fmaxf(best, t);
+      }
+#pragma unroll
+      for (int o = HH / 2; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+      const int lp = w0 + lane / HH;
+      if (lane % HH == 0 && lp < hi) scores[lp] = best * p.scale;
+    }
+    if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
+    if (blocks > 1 && !last_to_finish(p.counters + b, blocks, &flag)) return;
+  }
+  __syncthreads();   // (the scores of this block's warps; sq is read no more)
+
+  // ---- the sequence's pages
   int32_t* out = p.sel_table + static_cast<size_t>(b) * p.width;
   int32_t* sel = p.selected != nullptr ? p.selected + static_cast<size_t>(b) * p.budget : nullptr;
   const int taken = min(np, p.budget);
-  if (tid == 0) p.sel_lens[b] = L - (np - taken) * kPage;
   if (sel != nullptr)
     for (int i = taken + tid; i < p.budget; i += kSelThreads) sel[i] = -1;
+  auto take_page = [&](int pos, int i) {
+    out[pos] = __ldg(table + i);
+    if (sel != nullptr) sel[pos] = i;
+  };
   if (np <= p.budget) {
-    for (int i = tid; i < np; i += kSelThreads) {
-      out[i] = __ldg(table + i);
-      if (sel != nullptr) sel[i] = i;
-    }
-    return;
+    for (int i = tid; i < np; i += kSelThreads) take_page(i, i);
+  } else {
+    for (int i = tid; i < lo; i += kSelThreads) take_page(i, i);
+    for (int i = tid; i < p.keep_last; i += kSelThreads) take_page(p.budget - p.keep_last + i, hi + i);
   }
-  const float* scores = p.scores + static_cast<size_t>(b) * p.max_pages;
-  const int lo = p.keep_first, hi = np - p.keep_last, want = p.budget - p.keep_first - p.keep_last;
-  // the want-th largest key (`prefix`) and how many of its equals are wanted (`left`)
-  uint32_t prefix = 0;
-  int left = want;
-  if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
+  if (ranked) {
+    const int n = hi - lo;
+    for (int i = tid; i < min(n, kSelKeys); i += kSelThreads)
+      keys[i] = make_uint2(score_key(scores[lo + i]), static_cast<uint32_t>(__ldg(table + lo + i)));
+    __syncthreads();
+    auto key = [&](int i) { return i < kSelKeys ? keys[i].x : score_key(scores[lo + i]); };
+    // the want-th largest key begins with the digits of `prefix` from `shift` up; `left` of
+    // those that do are wanted
+    uint32_t prefix = 0;
+    int left = want, shift = 32;
+    for (bool all = false; shift > 0 && !all;) {
+      shift -= 8;
       hist[tid] = 0;
       __syncthreads();
-      for (int i = lo + tid; i < hi; i += kSelThreads) {
-        const uint32_t k = score_key(scores[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+      for (int i0 = 0; i0 < n; i0 += kSelThreads) {   // the equal digits of a warp counted once
+        const uint32_t k = i0 + tid < n ? key(i0 + tid) : 0u;
+        const bool in = i0 + tid < n && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+        const uint32_t d = in ? (k >> shift) & 255u : 256u, same = __match_any_sync(0xffffffffu, d);
+        if (in && lane == __ffs(same) - 1) atomicAdd(&hist[d], __popc(same));
       }
       __syncthreads();
-      // digits from the largest down: thread t has digit 255 - t
-      int total;
-      const int mine = hist[255 - tid], incl = block_scan(mine, ws, total);
-      if (incl >= left && incl - mine < left) {
-        sh_digit = static_cast<uint32_t>(255 - tid);
-        sh_above = incl - mine;
+      if (warp == 0) {   // digits from the largest down: lane l has 255 - 8 l and the seven below
+        int c[8], sum = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          c[e] = hist[255 - 8 * lane - e];
+          sum += c[e];
+        }
+        int before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int t = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += t;
+        }
+        before -= sum;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (before < left && before + c[e] >= left) {
+            digit = 255 - 8 * lane - e;
+            above = before;
+            flag = before + c[e] == left;   // every one of them is wanted: no further digit matters
+          }
+          before += c[e];
+        }
       }
       __syncthreads();
-      prefix |= sh_digit << shift;
-      left -= sh_above;
+      prefix |= static_cast<uint32_t>(digit) << shift;
+      left -= above;
+      all = flag != 0;
     }
-  }
-  int at = lo, equal = 0;   // pages written, and equals met, before this round
-  for (int i = tid; i < lo; i += kSelThreads) {
-    out[i] = __ldg(table + i);
-    if (sel != nullptr) sel[i] = i;
-  }
-  for (int i = tid; i < p.keep_last; i += kSelThreads) {
-    out[p.budget - p.keep_last + i] = __ldg(table + hi + i);
-    if (sel != nullptr) sel[p.budget - p.keep_last + i] = hi + i;
-  }
-  for (int i0 = lo; want > 0 && i0 < hi; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const uint32_t k = i < hi ? score_key(scores[i]) : 0u;
-    const bool tie = i < hi && k == prefix;
-    int total;
-    const int t = block_scan(tie ? 1 : 0, ws, total) - (tie ? 1 : 0) + equal;   // equals before this page
-    equal += total;
-    const bool take = i < hi && (k > prefix || (tie && t < left));
-    const int pos = block_scan(take ? 1 : 0, ws, total) - 1 + at;
-    at += total;
-    if (take) {
-      out[pos] = __ldg(table + i);
-      if (sel != nullptr) sel[pos] = i;
+    // in order: a page's place is the number before it of pages above, and of the first
+    // `left` equals
+    int larger = 0, equal = 0;
+    for (int i0 = 0; i0 < n; i0 += kSelThreads) {
+      const int i = i0 + tid;
+      const uint32_t k = i < n ? key(i) >> shift : 0u, t = prefix >> shift;
+      const bool up = i < n && k > t, tie = i < n && k == t;
+      int total;
+      const int incl = block_scan((up ? 1 : 0) + (tie ? 1 << 16 : 0), ws, total);   // (256 of each at most)
+      const int ups = larger + (incl & 0xffff) - (up ? 1 : 0), ties = equal + (incl >> 16) - (tie ? 1 : 0);
+      if (up || (tie && ties < left)) {
+        const int pos = lo + ups + min(ties, left);
+        out[pos] = i < kSelKeys ? static_cast<int32_t>(keys[i].y) : __ldg(table + lo + i);
+        if (sel != nullptr) sel[pos] = lo + i;
+      }
+      larger += total & 0xffff;
+      equal += total >> 16;
     }
   }
 }
@@ -593,10 +715,11 @@ cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st) {
   const size_t smem = (3 * static_cast<size_t>(a.batch) + 2) * 4;
   const cudaError_t e = allow_smem(page_plan_kernel, (3 * static_cast<size_t>(kPlanMaxBatch) + 2) * 4);
   if (e != cudaSuccess) return e;
-  const int ctas = (a.slots != nullptr ? a.max_slots : 0) + a.batch > 4096 ? 8 : 1;
+  const int slots = a.slots != nullptr ? a.max_slots : 0;
+  const int ctas = slots + a.batch > 4096 ? 8 : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kPlanThreads);
+  cfg.blockDim = dim3(a.batch <= 256 && ctas == 1 ? 256 : kPlanThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -633,21 +756,38 @@ cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st) {
   return units <= 32 ? launch_summary<__nv_bfloat16, 1>(a, st) : launch_summary<__nv_bfloat16, 2>(a, st);
 }
 
-int score_chunks(int max_seq_len, int keep_first, int keep_last) {
-  const int ranked = (max_seq_len + kPage - 1) / kPage - keep_first - keep_last;
-  return ranked > 0 ? (ranked + kScPages - 1) / kScPages : 0;
+namespace {
+int units_per_lane(int d_c, int d_r) { return ((d_c + d_r) / 4 + 31) / 32 <= 3 ? 3 : 5; }
+
+template <int NU>
+cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
+  auto bytes = [](int D) {
+    const size_t q = static_cast<size_t>(kScHeads) * D * 4, keys = kSelKeys * sizeof(uint2);
+    return q > keys ? q : keys;
+  };
+  const cudaError_t e = allow_smem(select_pages_kernel<NU>, bytes(kSumMaxDc + kSumMaxDr));
+  if (e != cudaSuccess) return e;
+  return launch_chained(select_pages_kernel<NU>, dim3(static_cast<unsigned>(a.chunks) * a.batch), dim3(kSelThreads),
+                        bytes(a.d_c + a.d_r), st, a);
+}
+}  // namespace
+
+// Two rounds per block where one would leave more blocks than fit at once (two per SM):
+// the second round's queries are already in shared memory.
+void select_blocks(SelectArgs& a) {
+  const int pages = (a.max_seq_len + kPage - 1) / kPage, ranked = pages - a.keep_first - a.keep_last;
+  a.chunks = a.rounds = 1;
+  if (pages <= a.budget || a.budget <= a.keep_first + a.keep_last) return;
+  const int per = kSelWarps * score_pages(units_per_lane(a.d_c, a.d_r));
+  const int64_t groups = static_cast<int64_t>((ranked + per - 1) / per) * a.batch;
+  a.rounds = groups > 2 * kSms ? 2 : 1;
+  const int64_t all = static_cast<int64_t>(per) * a.rounds;
+  a.chunks = static_cast<int>((ranked + all - 1) / all);
 }
 
 cudaError_t launch_select_pages(const SelectArgs& a, cudaStream_t st) {
-  if ((a.max_seq_len + kPage - 1) / kPage > a.budget && a.budget > a.keep_first + a.keep_last) {
-    const size_t smem = static_cast<size_t>(kScHeads) * (a.d_c + a.d_r) * 4;
-    cudaError_t e = allow_smem(page_scores_kernel, static_cast<size_t>(kScHeads) * (kSumMaxDc + kSumMaxDr) * 4);
-    if (e == cudaSuccess)
-      e = launch_chained(page_scores_kernel, dim3(static_cast<unsigned>(a.chunks) * a.batch), dim3(32 * kScWarps), smem,
-                         st, a);
-    if (e != cudaSuccess) return e;
-  }
-  return launch_chained(select_pages_kernel, dim3(a.batch), dim3(kSelThreads), 0, st, a);
+  static_assert((kSumMaxDc + kSumMaxDr) / 4 <= 5 * 32, "a row's units over the lanes");
+  return units_per_lane(a.d_c, a.d_r) == 3 ? launch_select<3>(a, st) : launch_select<5>(a, st);
 }
 
 }  // namespace egmla

@@ -142,7 +142,7 @@ def test_plan_refusals(lib):
     for kw in (dict(batch=-1), dict(max_pages=0), dict(num_pages=0), dict(max_slots=-1)):
         assert rc(**kw) == INVALID, kw
     for kw in (dict(batch=16385), dict(num_pages=2 ** 25), dict(max_pages=2 ** 25),
-               dict(batch=16384, max_pages=2 ** 18)):
+               dict(batch=16384, max_pages=2 ** 18), dict(slots=FAKE, max_slots=2 ** 31 - 1)):
         assert rc(**kw) == UNSUPPORTED, kw
 
 
