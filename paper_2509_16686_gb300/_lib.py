@@ -172,6 +172,8 @@ def library_path() -> str:
 def load(build_if_needed: bool = True) -> ctypes.CDLL:
     """Load (building first if needed) the in-tree libegmla.so."""
     global _handle
+    if _handle is not None:
+        return _handle
     with _lock:
         if _handle is None:
             path = _build.build() if build_if_needed else _build.LIB
@@ -218,7 +220,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _shaped(t: Optional[torch.Tensor], shape: tuple, name: str) -> None:
-    if t is not None and tuple(t.shape) != shape:
+    if t is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {shape} expected, got {tuple(t.shape)}")
 
 
