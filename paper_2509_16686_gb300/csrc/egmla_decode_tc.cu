@@ -660,9 +660,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   phase_mark<DBG == 2>(p, 0);
   // beside the attention over a shared prefix most of the grid has no work: out of the
   // way at once (what comes before that kernel, the schedule with it, is complete)
-  if (p.beside && p.starts[blockIdx.x].done) {
-    grid_dependency_wait();
-    return;
+  if (p.beside) {
+    beside_acquire();
+    if (p.starts[blockIdx.x].done) {
+      grid_dependency_wait();
+      return;
+    }
   }
   // a fused launch inside a layer lets the output projection take each SM this
   // kernel leaves, so that its weights stream early

@@ -203,7 +203,9 @@ __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* map) {
 // kernel launched without the attribute the wait returns at once.
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
+// In place of that wait for a kernel beside the one before it, which let it start after
+// its own wait: what was complete then is read as it is in L2 from here on.
+__device__ __forceinline__ void beside_acquire() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 
 // ---------------------------------------------------------------- tcgen05
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {

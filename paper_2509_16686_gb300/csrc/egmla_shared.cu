@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const Shared
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // beside the query absorption (nothing here needs it): its wait comes at the end
   grid_launch_dependents();
+  beside_acquire();
   const int given = __ldg(p.prefix_len), len = min(max(given, 0), p.max_len);
   if (given != len && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, kStatusOutOfRange);
   const int first = p.gate ? 0 : len / kPage * kPage;   // the row that z begins with

@@ -112,3 +112,68 @@ def test_calls_allocate_nothing_and_can_be_captured(gpu_lib, name):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want) and int(layer.status.item()) == 0
+
+
+def alternating(which, graph, rounds=60):
+    """Two different problems in turn on one workspace and the same input tensors, which a
+    copy on the stream rewrites before every call: each result is that of the problem
+    alone, so no kernel of a call reads what the call before it left."""
+    serve = example()
+    layer = serve.Layer(9, 400, 100, seed=6)   # (the slots of 5331 tokens)
+    layer.plan([1500, 700, 64, 3, 130, 1, 900, 33, 2000])
+    for b, n in enumerate((1500, 700, 64, 3, 130, 1, 900, 33, 2000)):
+        layer.prefill(b, n)
+    layer.summarise()
+    base_table, base_lens = layer.table.clone(), layer.lens.clone()
+    qs = [layer.tokens(8)[3] for _ in range(2)]
+    ws = layer.bytes(max(_lib.eg_mla_decode_shared_workspace_size(layer.dims, 8, 2000),
+                         _lib.eg_mla_decode_sparse_workspace_size(layer.dims, 8, 100, 6)))
+    out = torch.zeros((8, 16, 128), dtype=torch.bfloat16, device="cuda")
+    q, table, lens = torch.empty_like(qs[0]), base_table[:8].clone(), base_lens[:8].clone()
+    prefix, plen = layer.ints(32), layer.ints(1)
+    order = [torch.arange(8, device="cuda"), torch.tensor([7, 3, 5, 1, 6, 2, 4, 0], device="cuda")]
+    inputs = [(qs[k], base_table[order[k]].contiguous(), base_lens[order[k]].contiguous(),
+               base_table[8 if k else 1, :32].contiguous(), base_lens[8 if k else 1:][:1].contiguous()) for k in range(2)]
+
+    def call(k):
+        for dst, src in zip((q, table, lens, prefix, plen), inputs[k]):
+            dst.copy_(src)
+        if which == "shared":
+            _lib.eg_mla_decode_shared(layer.dims, q, *layer.cache(), prefix, plen, 2000, table, lens, 2000, *layer.gate,
+                                      layer.w_uk, layer.w_uv, out, ws, dev_status=layer.status)
+        else:
+            _lib.eg_mla_decode_sparse(layer.dims, q, *layer.cache(), table, lens, 2000, layer.summary, 6, 1, 1,
+                                      *layer.gate, layer.w_uk, layer.w_uv, out, ws, dev_status=layer.status)
+
+    want = []
+    for k in range(2):
+        ws.fill_(255)
+        call(k)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+    got = [torch.empty_like(out) for _ in range(rounds)]
+
+    def run():
+        for i in range(rounds):
+            call(i % 2)
+            got[i].copy_(out)
+
+    if graph:   # back to back, without the host's pace
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        for _ in range(5):
+            g.replay()
+    else:
+        run()
+    torch.cuda.synchronize()
+    assert int(layer.status.item()) == 0
+    assert not torch.equal(want[0], want[1])
+    for i, g in enumerate(got):
+        assert torch.equal(g, want[i % 2]), i
+
+
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("which", ["shared", "sparse"])
+def test_calls_in_turn_on_one_workspace(gpu_lib, which, graph):
+    alternating(which, graph)
