@@ -280,8 +280,9 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     tmem_alloc(smem_u32(&bars.tmem_base), 512);
     tmem_relinquish();
   }
+  beside_acquire();   // (inputs are read before the wait)
   float* affine = reinterpret_cast<float*>(smem + C::kOffAffine);
-  for (int f = tid; f < D_C; f += kSaThreads) {   // (inputs: this kernel starts after all that comes before the call)
+  for (int f = tid; f < D_C; f += kSaThreads) {   // (this kernel starts after all that comes before the call)
     affine[f] = p.gamma ? __ldg(p.gamma + f) : 1.f;
     affine[D_C + f] = p.beta ? __ldg(p.beta + f) : 0.f;
   }
