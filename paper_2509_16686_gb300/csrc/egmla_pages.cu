@@ -267,6 +267,17 @@ struct Unit<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
   }
+  // x = c (*) g, exact: bf16 factors, an fp32 product
+  static __device__ __forceinline__ void mul(const uint4& c, const uint4& g, float2 (&x)[4]) {
+    const uint32_t a[4] = {c.x, c.y, c.z, c.w}, b[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm("{\n\t.reg .b16 al, ah, bl, bh;\n\t"
+          "mov.b32 {al, ah}, %2;\n\tmov.b32 {bl, bh}, %3;\n\t"
+          "fma.rn.f32.bf16 %0, al, bl, %4;\n\tfma.rn.f32.bf16 %1, ah, bh, %4;\n\t}"
+          : "=f"(x[i].x), "=f"(x[i].y)
+          : "r"(a[i]), "r"(b[i]), "f"(-0.f));
+  }
 };
 template <>
 struct Unit<float> {
@@ -274,6 +285,13 @@ struct Unit<float> {
   static __device__ __forceinline__ void widen(const uint4& w, float2 (&x)[2]) {
     x[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
     x[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+  }
+  static __device__ __forceinline__ void mul(const uint4& c, const uint4& g, float2 (&x)[2]) {
+    float2 t[2];
+    widen(c, x);
+    widen(g, t);
+    x[0] = __fmul2_rn(x[0], t[0]);
+    x[1] = __fmul2_rn(x[1], t[1]);
   }
 };
 
@@ -301,13 +319,14 @@ __device__ __forceinline__ void warp_sums(float (&v)[4], int lane) {
 // registers, the sums of the rows in flight reduced together.  The mean of gamma x_j +
 // beta is gamma mean(x_j) + beta, so the affine part comes last.  k^R rows: a lane has one
 // unit of every few rows.
-// Bound by issue and latency (0.5 of the issue slots, 136 instructions a row, most of them
-// widening, the two passes and the two reductions): 57.0 us for 8 x 32K tokens at d_c
-// 256, 5.3 TB/s of cache and gate rows; floor 27.4.  GM, the gate mode, at compile time:
-// 59.2 -> 57.0.  Forms that copy the pages by TMA into a ring or keep the next page's ids
-// ahead in persistent blocks measured 57.1 and 73.2 and were not kept.
+// Bound by issue and latency: 44.7 us for 8 x 32K tokens at d_c 256, 6.8 TB/s of cache and
+// gate rows; floor 28.  What it took (57.0 before): products straight from the bf16 pairs,
+// idle lanes that repeat a unit instead of zeros and selects, 64 registers (four blocks
+// per SM; with three 51.8, five 63.0; eight rows in flight 54.6, two 46.2).  Copies by TMA
+// into a ring, or the next page's ids ahead in persistent blocks, gained nothing.  GM: the
+// gate mode.
 template <typename T, int NU, int GM>
-__global__ void __launch_bounds__(32 * kSumWarps, NU == 4 ? 2 : 3) page_summary_kernel(const SummaryArgs p) {
+__global__ void __launch_bounds__(32 * kSumWarps, NU == 1 ? 4 : NU == 2 ? 3 : 2) page_summary_kernel(const SummaryArgs p) {
   using U = Unit<T>;
   constexpr bool GATE = GM != EG_MLA_GATE_NONE, GATE_ADD = GM == EG_MLA_GATE_ADD_LN;
   constexpr bool GATE_LN = GM == EG_MLA_GATE_MUL_LN || GM == EG_MLA_GATE_ADD_LN;
@@ -362,10 +381,15 @@ __global__ void __launch_bounds__(32 * kSumWarps, NU == 4 ? 2 : 3) page_summary_
     id_row = 0;
   }
   float2 acc[NU][VP];
+  bool live[NU];   // lanes past a row's end repeat its last unit; their sums are left out
+  int at[NU];
 #pragma unroll
-  for (int u = 0; u < NU; ++u)
+  for (int u = 0; u < NU; ++u) {
+    live[u] = lane + 32 * u < units;
+    at[u] = min(lane + 32 * u, units - 1) * VE;
 #pragma unroll
     for (int e = 0; e < VP; ++e) acc[u][e] = make_float2(0.f, 0.f);
+  }
   const T* c = static_cast<const T*>(p.c_pool) + row0 * p.d_c;
   const T* table = static_cast<const T*>(p.gate_table);
   const float inv_n = 1.f / static_cast<float>(p.d_c);
@@ -374,51 +398,55 @@ __global__ void __launch_bounds__(32 * kSumWarps, NU == 4 ? 2 : 3) page_summary_
     uint4 cw[kFlight][NU], gw[kFlight][NU];
 #pragma unroll
     for (int r = 0; r < kFlight; ++r) {
-      const int id = __shfl_sync(0xffffffffu, id_row, r0 + r);
+      const int id = GATE ? __shfl_sync(0xffffffffu, id_row, r0 + r) : 0;
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
-        const int at = lane + 32 * u;
-        cw[r][u] = gw[r][u] = make_uint4(0u, 0u, 0u, 0u);
-        if (at < units) {
-          cw[r][u] = __ldg(reinterpret_cast<const uint4*>(c + static_cast<size_t>(r0 + r) * p.d_c) + at);
-          if (GATE) gw[r][u] = __ldg(reinterpret_cast<const uint4*>(table + static_cast<size_t>(id) * p.d_c) + at);
-        }
+        cw[r][u] = __ldg(reinterpret_cast<const uint4*>(c + (r0 + r) * p.d_c + at[u]));
+        if (GATE) gw[r][u] = __ldg(reinterpret_cast<const uint4*>(table + static_cast<size_t>(id) * p.d_c + at[u]));
       }
     }
     float2 x[kFlight][NU][VP];
     float s[kFlight];
 #pragma unroll
     for (int r = 0; r < kFlight; ++r) {
-      float2 sum = make_float2(0.f, 0.f);
+      s[r] = 0.f;
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
-        float2 t[VP];
-        U::widen(cw[r][u], x[r][u]);
-        if (GATE) U::widen(gw[r][u], t);
+        if (GATE && !GATE_ADD) {
+          U::mul(cw[r][u], gw[r][u], x[r][u]);
+        } else {
+          U::widen(cw[r][u], x[r][u]);
+          if (GATE) {
+            float2 t[VP];
+            U::widen(gw[r][u], t);
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-          if (GATE) x[r][u][e] = GATE_ADD ? __fadd2_rn(x[r][u][e], t[e]) : __fmul2_rn(x[r][u][e], t[e]);
-          sum = __fadd2_rn(sum, x[r][u][e]);
+            for (int e = 0; e < VP; ++e) x[r][u][e] = __fadd2_rn(x[r][u][e], t[e]);
+          }
+        }
+        if (GATE_LN) {
+          float2 sum = x[r][u][0];
+#pragma unroll
+          for (int e = 1; e < VP; ++e) sum = __fadd2_rn(sum, x[r][u][e]);
+          if (live[u]) s[r] += sum.x + sum.y;
         }
       }
-      s[r] = sum.x + sum.y;
     }
     if (GATE_LN) {
       warp_sums(s, lane);
 #pragma unroll
       for (int r = 0; r < kFlight; ++r) {
         const float2 mu = make_float2(-s[r] * inv_n, -s[r] * inv_n);
-        float2 sq = make_float2(0.f, 0.f);
+        s[r] = 0.f;
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
-          const bool live = lane + 32 * u < units;
+          float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
           for (int e = 0; e < VP; ++e) {
-            x[r][u][e] = live ? __fadd2_rn(x[r][u][e], mu) : make_float2(0.f, 0.f);
+            x[r][u][e] = __fadd2_rn(x[r][u][e], mu);
             sq = __ffma2_rn(x[r][u][e], x[r][u][e], sq);
           }
+          if (live[u]) s[r] += sq.x + sq.y;
         }
-        s[r] = sq.x + sq.y;
       }
       warp_sums(s, lane);
 #pragma unroll
