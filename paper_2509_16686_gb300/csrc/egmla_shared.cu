@@ -28,6 +28,7 @@
 #include "egmla_common.cuh"
 #include "egmla_kernels.h"
 #include "egmla_ptx.cuh"
+#include "egmla_rows.cuh"
 
 namespace egmla {
 namespace {
@@ -73,91 +74,103 @@ struct SharedGateParams {
   const __nv_bfloat16* gate_table;
   uint16_t* z;
   int d_c, vocab, num_pages, max_len;
-  int gate, gate_add, gate_ln;
   float eps;
   int32_t* status;
 };
 
-// Rows of whole pages, those past the prefix zero (their weights are zero, and
+// GM: the gate mode.  Rows of whole pages, those past the prefix zero (their weights are zero, and
 // the cache may hold anything there).  With the gate off the attention reads the
 // pool itself: only the last page, where it is not full, is copied.
-__global__ void __launch_bounds__(32 * kSgWarps) shared_gate_kernel(const SharedGateParams p) {
+// Bound by the latency of table - ids - rows and, at 32K tokens (50 MB read and written,
+// 8 us of the call), by L2: four blocks per SM (five spill: 55.2 us the call against 53.0).
+template <int GM>
+__global__ void __launch_bounds__(32 * kSgWarps, 4) shared_gate_kernel(const SharedGateParams p) {
+  constexpr bool GATE = GM != EG_MLA_GATE_NONE, GATE_ADD = GM == EG_MLA_GATE_ADD_LN;
+  constexpr bool GATE_LN = GM == EG_MLA_GATE_MUL_LN || GM == EG_MLA_GATE_ADD_LN;
+  using U = Unit<__nv_bfloat16>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // beside the query absorption (nothing here needs it): its wait comes at the end
   grid_launch_dependents();
   beside_acquire();
   const int given = __ldg(p.prefix_len), len = min(max(given, 0), p.max_len);
   if (given != len && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, kStatusOutOfRange);
-  const int first = p.gate ? 0 : len / kPage * kPage;   // the row that z begins with
+  const int first = GATE ? 0 : len / kPage * kPage;   // the row that z begins with
   const int rows = (len + kPage - 1) / kPage * kPage - first;
   const int t0 = (blockIdx.x * kSgWarps + warp) * kSgRows;
-  const bool live = lane < p.d_c / 8;   // a lane holds eight features
-  if (t0 >= rows) {
-    grid_dependency_wait();
-    return;
-  }
-  // four rows never straddle a page
-  const int page = __ldg(p.table + (first + t0) / kPage);
-  const bool page_ok = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
-  bool bad = !page_ok;
-  uint4 c[kSgRows], g[kSgRows];
-  bool in[kSgRows];
+  if (t0 < rows) {
+    // four rows never straddle a page; rows past the prefix, and of a page that is out of
+    // range, read the first row of the page (of the pool) and are written as zero
+    const int page = __ldg(p.table + (first + t0) / kPage);
+    const bool page_ok = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
+    const size_t base = static_cast<size_t>(page_ok ? page : 0) * kPage;
+    const int off = (first + t0) % kPage, live_rows = page_ok ? len - (first + t0) : 0;
+    const bool live = lane < p.d_c / 8;   // a lane holds eight features; the others repeat the last
+    const int at = 8 * min(lane, p.d_c / 8 - 1);
+    bool bad = !page_ok;
+    uint4 c[kSgRows], g[kSgRows];
 #pragma unroll
-  for (int r = 0; r < kSgRows; ++r) {
-    const int row = first + t0 + r;
-    in[r] = page_ok && row < len;
-    c[r] = g[r] = make_uint4(0u, 0u, 0u, 0u);
-    if (!in[r]) continue;
-    const size_t at = static_cast<size_t>(page) * kPage + row % kPage;
-    if (live) c[r] = __ldg(reinterpret_cast<const uint4*>(p.c_pool + at * p.d_c) + lane);
-    if (p.gate) {
-      int id = __ldg(p.id_pool + at);
-      if (static_cast<unsigned>(id) >= static_cast<unsigned>(p.vocab)) {
-        bad = true;
-        id = 0;
-      }
-      if (live) g[r] = __ldg(reinterpret_cast<const uint4*>(p.gate_table + static_cast<size_t>(id) * p.d_c) + lane);
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < kSgRows; ++r) {
-    uint4 out = c[r];
-    if (p.gate && in[r]) {
-      float x[8];
-      const uint32_t cw[4] = {c[r].x, c[r].y, c[r].z, c[r].w}, gw[4] = {g[r].x, g[r].y, g[r].z, g[r].w};
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float cv = __uint_as_float(i & 1 ? cw[i / 2] & 0xffff0000u : cw[i / 2] << 16);
-        const float gv = __uint_as_float(i & 1 ? gw[i / 2] & 0xffff0000u : gw[i / 2] << 16);
-        x[i] = p.gate_add ? cv + gv : cv * gv;
-        sum += x[i];
-      }
-      if (p.gate_ln) {
-        const float inv_n = 1.f / static_cast<float>(p.d_c);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float mu = sum * inv_n;
-        float sq = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] -= mu;
-          sq = fmaf(x[i], x[i], sq);
+    for (int r = 0; r < kSgRows; ++r) {
+      const size_t row = base + (r < live_rows ? off + r : 0);
+      c[r] = __ldg(reinterpret_cast<const uint4*>(p.c_pool + row * p.d_c + at));
+      if (GATE) {
+        int id = __ldg(p.id_pool + row);
+        if (static_cast<unsigned>(id) >= static_cast<unsigned>(p.vocab)) {
+          bad |= r < live_rows;
+          id = 0;
         }
-        if (!live) sq = 0.f;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        const float rstd = rsqrtf(fmaf(sq, inv_n, p.eps));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= rstd;
+        g[r] = __ldg(reinterpret_cast<const uint4*>(p.gate_table + static_cast<size_t>(id) * p.d_c + at));
       }
-      out = p.gate_ln ? make_uint4(sh_pack_as<true>(x[0], x[1]), sh_pack_as<true>(x[2], x[3]),
-                                   sh_pack_as<true>(x[4], x[5]), sh_pack_as<true>(x[6], x[7]))
-                      : make_uint4(sh_pack(x[0], x[1]), sh_pack(x[2], x[3]), sh_pack(x[4], x[5]), sh_pack(x[6], x[7]));
     }
-    if (live) *(reinterpret_cast<uint4*>(p.z + static_cast<size_t>(t0 + r) * p.d_c) + lane) = out;
+    uint16_t* z = p.z + static_cast<size_t>(t0) * p.d_c + at;
+    if constexpr (GATE) {
+      const float inv_n = 1.f / static_cast<float>(p.d_c);
+      float2 x[kSgRows][4];
+      float s[kSgRows];
+#pragma unroll
+      for (int r = 0; r < kSgRows; ++r) {
+        if (GATE_ADD) {
+          float2 t[4];
+          U::widen(c[r], x[r]);
+          U::widen(g[r], t);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[r][e] = __fadd2_rn(x[r][e], t[e]);
+        } else {
+          U::mul(c[r], g[r], x[r]);
+        }
+        const float2 sum = __fadd2_rn(__fadd2_rn(x[r][0], x[r][1]), __fadd2_rn(x[r][2], x[r][3]));
+        s[r] = live ? sum.x + sum.y : 0.f;
+      }
+      if (GATE_LN) {
+        warp_sums(s, lane);
+#pragma unroll
+        for (int r = 0; r < kSgRows; ++r) {
+          const float2 mu = make_float2(-s[r] * inv_n, -s[r] * inv_n);
+          float2 sq = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[r][e] = __fadd2_rn(x[r][e], mu);
+            sq = __ffma2_rn(x[r][e], x[r][e], sq);
+          }
+          s[r] = live ? sq.x + sq.y : 0.f;
+        }
+        warp_sums(s, lane);
+#pragma unroll
+        for (int r = 0; r < kSgRows; ++r) {
+          const float rstd = rsqrtf(fmaf(s[r], inv_n, p.eps));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[r][e] = __fmul2_rn(x[r][e], make_float2(rstd, rstd));
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < kSgRows; ++r)
+        c[r] = make_uint4(sh_pack_as<GATE_LN>(x[r][0].x, x[r][0].y), sh_pack_as<GATE_LN>(x[r][1].x, x[r][1].y),
+                          sh_pack_as<GATE_LN>(x[r][2].x, x[r][2].y), sh_pack_as<GATE_LN>(x[r][3].x, x[r][3].y));
+    }
+#pragma unroll
+    for (int r = 0; r < kSgRows; ++r)
+      if (live) *reinterpret_cast<uint4*>(z + r * p.d_c) = r < live_rows ? c[r] : make_uint4(0u, 0u, 0u, 0u);
+    if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
   }
-  if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
   grid_dependency_wait();
 }
 
@@ -638,14 +651,17 @@ cudaError_t launch_shared_gate(const SharedArgs& a, cudaStream_t st) {
   g.vocab = d.vocab;
   g.num_pages = d.num_pages;
   g.max_len = a.max_prefix_len;
-  g.gate = d.gate;
-  g.gate_add = d.gate_add;
-  g.gate_ln = d.gate_ln;
   g.eps = d.eps;
   g.status = d.status;
   const int rows = static_cast<int>(shared_z_rows(a.max_prefix_len, d.gate != 0));
-  return launch_chained(shared_gate_kernel, dim3((rows + kSgWarps * kSgRows - 1) / (kSgWarps * kSgRows)),
-                        dim3(32 * kSgWarps), 0, st, g);
+  auto launch = [&](auto kernel) {
+    return launch_chained(kernel, dim3((rows + kSgWarps * kSgRows - 1) / (kSgWarps * kSgRows)), dim3(32 * kSgWarps), 0, st,
+                          g);
+  };
+  if (!d.gate) return launch(shared_gate_kernel<EG_MLA_GATE_NONE>);
+  if (d.gate_add) return launch(shared_gate_kernel<EG_MLA_GATE_ADD_LN>);
+  if (d.gate_ln) return launch(shared_gate_kernel<EG_MLA_GATE_MUL_LN>);
+  return launch(shared_gate_kernel<EG_MLA_GATE_MUL>);
 }
 
 cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cudaStream_t st) {
