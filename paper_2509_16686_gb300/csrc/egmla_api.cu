@@ -439,6 +439,7 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       // the queries, and the schedule for what will be left of the sequences; then the pages
       extra.q32 = sparse->q;
       extra.sparse = sparse->lens;
+      extra.chain = 1;
       DecodeArgs part = a;
       part.seq_lens = sparse->select.seq_lens;
       part.block_table = nullptr;
@@ -666,7 +667,7 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
   s.keep_last = keep_last;
   s.width = sl.width;
   s.scale = resolve_scale(dims);
-  egmla::select_blocks(s);
+  s.chunks = egmla::select_chunks(max_seq_len, batch, budget, keep_first, keep_last, dims->d_c, dims->d_rope);
   if (static_cast<int64_t>(s.chunks) * batch > INT32_MAX) return EG_MLA_ERR_UNSUPPORTED;
   const int64_t most = static_cast<int64_t>(sl.width) * dims->page_size;
   return decode_impl(dims, q, c_pool, krope_pool, id_pool, s.sel_table, sl.width, sp.lens.lens,

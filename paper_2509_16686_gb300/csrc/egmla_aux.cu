@@ -462,8 +462,9 @@ prologue_f32_kernel(const float* __restrict__ q, const float* __restrict__ w_uk,
   __shared__ __align__(16) float red[kPfParts][kPfBatch][kPfFeat];
   const int nfc = (d_c + kPfFeat - 1) / kPfFeat, nbg = (batch + kPfBatch - 1) / kPfBatch;
   const int nabs = H * nfc * nbg;
-  grid_launch_dependents();
+  if (sparse.lens == nullptr) grid_launch_dependents();
   grid_dependency_wait();
+  if (sparse.lens != nullptr) grid_launch_dependents();   // the selection, which runs beside this kernel at first
   if (blockIdx.x == 0) {
     if (sparse.lens != nullptr) {
       selected_lengths(sparse, seq_lens, batch);

@@ -303,10 +303,10 @@ struct SelectArgs {
   int32_t* status;
   int H, d_c, d_r, batch, max_pages, max_seq_len, num_pages;
   int budget, keep_first, keep_last, width;
-  int chunks, rounds;     // blocks per sequence, groups of pages per block: set by select_blocks
+  int chunks;             // select_chunks(): blocks per sequence
   float scale;
 };
-void select_blocks(SelectArgs& a);
+int select_chunks(int max_seq_len, int batch, int budget, int keep_first, int keep_last, int d_c, int d_r);
 cudaError_t launch_select_pages(const SelectArgs& a, cudaStream_t st);
 
 // R0 decode (egmla_r0.cu): bf16, 16 heads, d_n = d_v = 128, d_r = 64,

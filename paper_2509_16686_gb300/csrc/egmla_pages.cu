@@ -438,21 +438,26 @@ __global__ void __launch_bounds__(32 * kSumWarps, NU == 1 ? 4 : NU == 2 ? 3 : 2)
 
 // ============================================================================ 3. page selection
 // score(b, p) = max_h scale (q^_bh . m^c_p + q^R_bh . m^R_p), fp32 products and sums.
-// One launch: a block scores 8 PP pages of a sequence, `rounds` times (its queries in
-// shared memory, a warp PP pages at a time, so that a query value read serves PP
-// products; lanes share a row, the heads' sums take one transposing reduction); the last
-// block of a sequence to finish selects its pages.  The lengths that are left do not
+// One launch: a block scores groups of 32 pages of a sequence (its queries in shared
+// memory, a warp four pages at a time, so that a query value read serves four products; lanes
+// share a row, the heads' sums take one transposing reduction); the last block of a
+// sequence to finish selects its pages.  The lengths that are left do not
 // depend on the choice, so the split-KV schedule is already made (selected_lengths).
 //
 // The selection: scores as whole numbers of the same order (no number comes last); the
 // want-th largest by up to four passes over a histogram of eight bits each; then, in
 // order, the pages above it and the first of those equal to it, between the pages that
 // are always kept.
-constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32, kScHeads = 16;
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kScHeads = 16;
+constexpr int kSelPages = 32;    // pages of a block at a time
+constexpr int kSelRounds = 4;    // times, at most
+constexpr int kWideRounds = 2;   // of rows in two parts
 constexpr int kSelKeys = 4096;   // scores kept in shared memory; of more the rest is read again
 
-// pages of a warp at a time, by the row's 16-byte units per lane
-__host__ __device__ constexpr int score_pages(int nu) { return nu <= 3 ? 4 : 2; }
+// Pages and heads of a warp (32 sums): two warps share a group of four pages.  A row's
+// 16-byte units go over the lanes, three of a lane at a time.
+constexpr int kScPP = 4, kScHH = 8, kScShare = kScHeads / kScHH, kScUnits = 3;
+static_assert(kSelWarps / kScShare * kScPP == kSelPages && kScPP * kScHH == 32, "pages of a block");
 
 // v[i] summed over the warp's lanes, value t returned to lane t
 __device__ __forceinline__ float sum32_transpose(float (&v)[32], int lane) {
@@ -493,18 +498,22 @@ __device__ __forceinline__ bool last_to_finish(int32_t* count, int of, int* flag
   return last;
 }
 
-template <int NU>
-__global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const SelectArgs p) {
-  constexpr int PP = score_pages(NU);
+// PARTS: of a row, three units of a lane each
+template <int PARTS>
+__global__ void __launch_bounds__(kSelThreads, 1) select_pages_kernel(const SelectArgs p) {
+  constexpr int PP = kScPP, HH = kScHH, kShare = kScShare, NU = kScUnits;
   extern __shared__ __align__(16) uint8_t sel_smem[];
   __shared__ int hist[256];
   __shared__ int ws[32], flag, digit, above;
+  __shared__ float bests[kSelRounds][kShare][kSelPages];
   float4* sq = reinterpret_cast<float4*>(sel_smem);            // [kScHeads][units]
   uint2* keys = reinterpret_cast<uint2*>(sel_smem);            // afterwards: (key, page id)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.x / p.chunks, j = blockIdx.x - b * p.chunks;
   const int D = p.d_c + p.d_r, units = D / 4;
-  grid_dependency_wait();
+  // lengths, block table and summaries are no work of the absorption, beside which this
+  // kernel starts: they are read before the wait for its queries
+  beside_acquire();
   const int given = __ldg(p.seq_lens + b);
   const int L = min(max(given, 0), p.max_seq_len), np = (L + kPage - 1) / kPage;
   const int32_t* table = p.block_table + static_cast<size_t>(b) * p.max_pages;
@@ -512,9 +521,33 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const Sele
   // of a longer sequence the pages lo .. hi - 1 are ranked, `want` of them taken
   const int lo = p.keep_first, hi = np - p.keep_last, want = p.budget - p.keep_first - p.keep_last;
   const bool ranked = np > p.budget && want > 0;
-  const int per = kSelWarps * PP * p.rounds, blocks = ranked ? (hi - lo + per - 1) / per : 1;
-  if (j >= blocks) return;
+  // groups of pages j, j + chunks, .. are this block's: a short sequence's go to as many blocks
+  const int groups = (hi - lo + kSelPages - 1) / kSelPages, blocks = ranked ? min(groups, p.chunks) : 1;
+  if (j >= blocks) return;   // (without the wait: those that have work stay for it)
   if (given != L && j == 0 && tid == 0) report_status(p.status, kStatusOutOfRange);
+  float4 m[PP][NU];
+  bool bad = false;
+  // part `part` of the mean keys of the warp's pages w0 .. w0 + PP - 1
+  auto load_pages = [&](int w0, int part) {
+#pragma unroll
+    for (int k = 0; k < PP; ++k) {
+      int page = __ldg(table + min(w0 + k, hi - 1));
+      if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) {
+        bad = true;
+        page = 0;
+      }
+      const float4* row = reinterpret_cast<const float4*>(p.summary + static_cast<size_t>(page) * D);
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        const int u = lane + 32 * (NU * part + i);
+        m[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (u < units) m[k][i] = __ldg(row + u);
+      }
+    }
+  };
+  const int row0 = warp / kShare * PP, h0 = warp % kShare * HH;   // the warp's pages of a group, its heads
+  if (ranked) load_pages(lo + j * kSelPages + row0, 0);
+  grid_dependency_wait();
   if (ranked) {
     const float* q = p.q + static_cast<size_t>(b) * p.q_stride;
     for (int h = warp; h < kScHeads; h += kSelWarps)
@@ -527,46 +560,25 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const Sele
         else
           copy16_async(dst, q + p.H * p.d_c + h * p.d_r + 4 * u - p.d_c);
       }
-    bool bad = false, staged = false;
-    for (int r = 0; r < p.rounds; ++r) {
-      const int w0 = lo + ((j * p.rounds + r) * kSelWarps + warp) * PP;
-      if (staged && w0 >= hi) break;
-      float4 m[PP][NU];
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    for (int r = 0; r < kSelRounds; ++r) {
+      const int w0 = lo + (j + r * p.chunks) * kSelPages + row0;
+      if (w0 >= hi) break;
+      float acc[32];   // [page][head]
 #pragma unroll
-      for (int k = 0; k < PP; ++k) {
-        int page = __ldg(table + min(w0 + k, hi - 1));
-        if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) {
-          bad = true;
-          page = 0;
-        }
-        const float4* row = reinterpret_cast<const float4*>(p.summary + static_cast<size_t>(page) * D);
+      for (int e = 0; e < 32; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        if (r > 0 || part > 0) load_pages(w0, part);
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-          m[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (lane + 32 * i < units) m[k][i] = __ldg(row + lane + 32 * i);
-        }
-      }
-      if (!staged) {   // (every warp comes here once)
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncthreads();
-        staged = true;
-        if (w0 >= hi) break;
-      }
-      // the heads in passes of HH, 32 sums a pass: [page][head]
-      constexpr int HH = 32 / PP;
-      float best = -INFINITY;   // lane l: of page l / HH
-#pragma unroll
-      for (int h0 = 0; h0 < kScHeads; h0 += HH) {
-        float acc[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-          const bool in = lane + 32 * i < units;   // (past the row both are zero)
+          const int u = lane + 32 * (NU * part + i);
+          const bool in = u < units;   // (past the row both are zero)
 #pragma unroll
           for (int h = 0; h < HH; ++h) {
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (in) x = sq[(h0 + h) * units + lane + 32 * i];
+            if (in) x = sq[(h0 + h) * units + u];
 #pragma unroll
             for (int k = 0; k < PP; ++k) {
               float& a = acc[k * HH + h];
@@ -577,15 +589,23 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const Sele
             }
           }
         }
-        const float t = sum32_transpose(acc, lane);
-        if (h0 + lane % HH < p.H) best = fmaxf(best, t);
       }
+      float best = sum32_transpose(acc, lane);   // lane l: of page l / HH
+      if (h0 + lane % HH >= p.H) best = -INFINITY;
 #pragma unroll
       for (int o = HH / 2; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-      const int lp = w0 + lane / HH;
-      if (lane % HH == 0 && lp < hi) scores[lp] = best * p.scale;
+      if (lane % HH == 0) bests[r][warp % kShare][row0 + lane / HH] = best;
     }
     if (bad && lane == 0) report_status(p.status, kStatusOutOfRange);
+    __syncthreads();
+    for (int i = tid; i < kSelRounds * kSelPages; i += kSelThreads) {
+      const int r = i / kSelPages, k = i % kSelPages, lp = lo + (j + r * p.chunks) * kSelPages + k;
+      if (lp >= hi) continue;
+      float s = bests[r][0][k];
+#pragma unroll
+      for (int e = 1; e < kShare; ++e) s = fmaxf(s, bests[r][e][k]);
+      scores[lp] = s * p.scale;
+    }
     if (blocks > 1 && !last_to_finish(p.counters + b, blocks, &flag)) return;
   }
   __syncthreads();   // (the scores of this block's warps; sq is read no more)
@@ -618,7 +638,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const Sele
     int left = want, shift = 32;
     for (bool all = false; shift > 0 && !all;) {
       shift -= 8;
-      hist[tid] = 0;
+      if (tid < 256) hist[tid] = 0;
       __syncthreads();
       for (int i0 = 0; i0 < n; i0 += kSelThreads) {   // the equal digits of a warp counted once
         const uint32_t k = i0 + tid < n ? key(i0 + tid) : 0u;
@@ -664,7 +684,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) select_pages_kernel(const Sele
       const uint32_t k = i < n ? key(i) >> shift : 0u, t = prefix >> shift;
       const bool up = i < n && k > t, tie = i < n && k == t;
       int total;
-      const int incl = block_scan((up ? 1 : 0) + (tie ? 1 << 16 : 0), ws, total);   // (256 of each at most)
+      const int incl = block_scan((up ? 1 : 0) + (tie ? 1 << 16 : 0), ws, total);   // (512 of each at most)
       const int ups = larger + (incl & 0xffff) - (up ? 1 : 0), ties = equal + (incl >> 16) - (tie ? 1 : 0);
       if (up || (tie && ties < left)) {
         const int pos = lo + ups + min(ties, left);
@@ -728,37 +748,35 @@ cudaError_t launch_page_summary(const SummaryArgs& a, cudaStream_t st) {
 }
 
 namespace {
-int units_per_lane(int d_c, int d_r) { return ((d_c + d_r) / 4 + 31) / 32 <= 3 ? 3 : 5; }
+int row_parts(int d_c, int d_r) { return ((d_c + d_r) / 4 + 32 * kScUnits - 1) / (32 * kScUnits); }
 
-template <int NU>
+template <int PARTS>
 cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
   auto bytes = [](int D) {
     const size_t q = static_cast<size_t>(kScHeads) * D * 4, keys = kSelKeys * sizeof(uint2);
     return q > keys ? q : keys;
   };
-  const cudaError_t e = allow_smem(select_pages_kernel<NU>, bytes(kSumMaxDc + kSumMaxDr));
+  const cudaError_t e = allow_smem(select_pages_kernel<PARTS>, bytes(kSumMaxDc + kSumMaxDr));
   if (e != cudaSuccess) return e;
-  return launch_chained(select_pages_kernel<NU>, dim3(static_cast<unsigned>(a.chunks) * a.batch), dim3(kSelThreads),
+  return launch_chained(select_pages_kernel<PARTS>, dim3(static_cast<unsigned>(a.chunks) * a.batch), dim3(kSelThreads),
                         bytes(a.d_c + a.d_r), st, a);
 }
 }  // namespace
 
-// Two rounds per block where one would leave more blocks than fit at once (two per SM):
-// the second round's queries are already in shared memory.
-void select_blocks(SelectArgs& a) {
-  const int pages = (a.max_seq_len + kPage - 1) / kPage, ranked = pages - a.keep_first - a.keep_last;
-  a.chunks = a.rounds = 1;
-  if (pages <= a.budget || a.budget <= a.keep_first + a.keep_last) return;
-  const int per = kSelWarps * score_pages(units_per_lane(a.d_c, a.d_r));
-  const int64_t groups = static_cast<int64_t>((ranked + per - 1) / per) * a.batch;
-  a.rounds = groups > 2 * kSms ? 2 : 1;
-  const int64_t all = static_cast<int64_t>(per) * a.rounds;
-  a.chunks = static_cast<int>((ranked + all - 1) / all);
+// Fewer blocks than groups of pages where those are more than SMs (one block fits on
+// each): a block's further rounds find the queries in shared memory.
+int select_chunks(int max_seq_len, int batch, int budget, int keep_first, int keep_last, int d_c, int d_r) {
+  const int pages = (max_seq_len + kPage - 1) / kPage, ranked = pages - keep_first - keep_last;
+  if (pages <= budget || budget <= keep_first + keep_last) return 1;
+  const int64_t groups = (ranked + kSelPages - 1) / kSelPages, all = groups * batch;
+  const int most = row_parts(d_c, d_r) == 1 ? kSelRounds : kWideRounds;
+  const int64_t rounds = all > most * kSms ? most : (all + kSms - 1) / kSms;
+  return static_cast<int>((groups + rounds - 1) / rounds);
 }
 
 cudaError_t launch_select_pages(const SelectArgs& a, cudaStream_t st) {
-  static_assert((kSumMaxDc + kSumMaxDr) / 4 <= 5 * 32, "a row's units over the lanes");
-  return units_per_lane(a.d_c, a.d_r) == 3 ? launch_select<3>(a, st) : launch_select<5>(a, st);
+  static_assert((kSumMaxDc + kSumMaxDr) / 4 <= 2 * kScUnits * 32, "a row's units over the lanes");
+  return row_parts(a.d_c, a.d_r) == 1 ? launch_select<1>(a, st) : launch_select<2>(a, st);
 }
 
 }  // namespace egmla
