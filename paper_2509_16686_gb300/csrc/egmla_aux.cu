@@ -201,13 +201,14 @@ __device__ void selected_lengths(const SparseLens& s, const int32_t* seq_lens, i
 // page prefix sums and the splits' start records.  `smem` (`words` ints): the
 // prefix sums in shared memory too where they fit, so that the splits'
 // searches read them there; `wsum`: eight more ints.
+template <bool EXTRA>
 __device__ void schedule_block(const int32_t* seq_lens, int batch, int page_size, int32_t* cu, uint32_t* seq_done,
                                int num_splits, const AbsorbExtra& extra, const int32_t* block_table, int max_pages,
                                SplitStart* starts, int32_t* smem, int words, int32_t* wsum) {
   // With a shared prefix the own tokens are cut for a part of the splits: each thread
   // weighs some of the choices, the cheapest (of equals the fewest own splits) is written.
   auto cut_for = [&](int units) {
-    if (extra.prefix_len == nullptr) return num_splits;
+    if (!EXTRA || extra.prefix_len == nullptr) return num_splits;
     const int len = min(max(__ldg(extra.prefix_len), 0), extra.max_prefix_len);
     const bool both = len > 0 && num_splits > 1;
     unsigned long long best = ~0ull;
@@ -279,6 +280,10 @@ __host__ __device__ constexpr uint32_t pm_smem(int nk, int nt) {
 
 static_assert(pm_smem(kPmMaxNope / 64, kPmMaxSeq) <= kSmemMost, "shared memory");
 
+// EXTRA: with what AbsorbExtra asks for.  A form of its own: as branches of one form
+// that, and the decode kernel's for a shared prefix, made a layer of 8K tokens 98.1 us
+// instead of 96.2 and a ragged step 66.8 instead of 66.1.
+template <bool EXTRA>
 __global__ void __launch_bounds__(kPmThreads)
 prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap qmap,
                     const __nv_bfloat16* __restrict__ q, const float* __restrict__ gamma,
@@ -293,20 +298,23 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   const int mt = (d_c + kPmTile - 1) / kPmTile, nbg = (batch + nt - 1) / nt;
   const int ntiles = q != nullptr ? H * mt * nbg : 0;   // (the cache-read test entry: the schedule only)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool chain = EXTRA && extra.chain != 0;
   if (blockIdx.x == 0 || blockIdx.x > static_cast<unsigned>(ntiles)) {
-    if (!extra.chain) grid_launch_dependents();
+    if (!chain) grid_launch_dependents();
     grid_dependency_wait();
-    if (extra.chain) grid_launch_dependents();
+    if (chain) grid_launch_dependents();
     if (blockIdx.x == 0) {
       int32_t* words = reinterpret_cast<int32_t*>(smem);
       constexpr int kWords = 4096;
       static_assert(pm_smem(1, 16) >= 1024 + (kWords + 8) * 4, "schedule area");
-      if (extra.sparse.lens != nullptr) {
+      const int32_t* lens = seq_lens;
+      if (EXTRA && extra.sparse.lens != nullptr) {
         selected_lengths(extra.sparse, seq_lens, batch);
         __syncthreads();
+        lens = extra.sparse.lens;
       }
-      schedule_block(extra.sparse.lens != nullptr ? extra.sparse.lens : seq_lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
-                       words + 8, kWords, words);
+      schedule_block<EXTRA>(lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
+                            words + 8, kWords, words);
     } else {
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);
@@ -342,9 +350,9 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
-  if (!extra.chain) grid_launch_dependents();
+  if (!chain) grid_launch_dependents();
   grid_dependency_wait();
-  if (extra.chain) grid_launch_dependents();
+  if (chain) grid_launch_dependents();
   if (warp == 0) {
     if (elect_one()) {
       const uint64_t keep = policy_evict_last(), once = policy_evict_first();
@@ -380,7 +388,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
       const uint4 x = *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + j) * H + h) * qrow + d_nope + r);
       *reinterpret_cast<uint4*>(qprep + static_cast<size_t>(b0 + j) * qstride + qprep_lat_bytes(d_c) + qop_offset(h, r)) =
           x;
-      if (extra.q32 != nullptr) {
+      if (EXTRA && extra.q32 != nullptr) {
         float4* qf = reinterpret_cast<float4*>(extra.q32 + static_cast<size_t>(b0 + j) * H * (d_c + d_rope) + H * d_c +
                                                h * d_rope + r);
         qf[0] = make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u),
@@ -413,13 +421,13 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         part[16 + j] = v[j] * bt;
         if (c0 + j < nb) *reinterpret_cast<__nv_bfloat16*>(qb + j * qstride) = bq;
       }
-      if (extra.q32 != nullptr) {
+      if (EXTRA && extra.q32 != nullptr) {
         float* qf = extra.q32 + static_cast<size_t>(b0 + c0) * H * (d_c + d_rope) + h * d_c + f;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (c0 + j < nb) qf[static_cast<size_t>(j) * H * (d_c + d_rope)] = v[j];
       }
-      if (extra.q16 != nullptr) {
+      if (EXTRA && extra.q16 != nullptr) {
         uint8_t* qh = extra.q16 + static_cast<size_t>(b0 + c0) * qprep_lat_bytes(d_c) + qop_offset(h, f);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -566,8 +574,8 @@ struct MergeShared {
   float wts[kMergeMaxSeq][kCombineSlots];
   float inv_l[kMergeMaxSeq];
   int slots[kMergeMaxSeq], slot0[kMergeMaxSeq];
-  int own[kMergeMaxSeq], prefix0[kMergeMaxSeq];   // with a shared prefix: the slots before it, its first partial
   float4 red[T];
+  int own[kMergeMaxSeq], prefix0[kMergeMaxSeq];   // with a shared prefix: the slots before it, its first partial
 };
 
 // the fewest sequences per block (a power of two up to `most`) that leave at most
@@ -1324,10 +1332,14 @@ cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const
   const int tiles = a.q != nullptr ? 16 * mt * ((a.batch + nt - 1) / nt) : 0;
   const int blocks = tiles + 1 + (ap.batch + kPmThreads / 32 - 1) / (kPmThreads / 32);
   const size_t smem = pm_smem(nk, nt);
-  const cudaError_t e = allow_smem(prologue_tc_kernel, pm_smem(kPmMaxNope / 64, kPmMaxSeq));
+  const bool more = extra.chain || extra.q16 != nullptr || extra.q32 != nullptr || extra.prefix_len != nullptr ||
+                    extra.sparse.lens != nullptr;
+  const auto kern = more ? prologue_tc_kernel<true> : prologue_tc_kernel<false>;
+  const size_t most = pm_smem(kPmMaxNope / 64, kPmMaxSeq);
+  const cudaError_t e = more ? allow_smem(prologue_tc_kernel<true>, most) : allow_smem(prologue_tc_kernel<false>, most);
   if (e != cudaSuccess) return e;
   return launch_chained(
-      prologue_tc_kernel, dim3(blocks), dim3(kPmThreads), smem, st, maps[0], maps[1],
+      kern, dim3(blocks), dim3(kPmThreads), smem, st, maps[0], maps[1],
       static_cast<const __nv_bfloat16*>(a.q), gamma, beta, a.seq_lens, a.batch, a.d_nope, a.d_rope, a.d_c,
       a.page_size, ws + wl.off_qprep, wl.qprep_stride, reinterpret_cast<int32_t*>(ws + wl.off_cu),
       reinterpret_cast<uint32_t*>(ws + wl.off_done), a.num_splits, a.block_table, a.max_pages,

@@ -191,7 +191,7 @@ struct TcParams {
   __nv_bfloat16* out;
   uint32_t* seq_done;   // [b]: the split partials of sequence b stored
   int d_v;
-  int fuse, early, beside;
+  int fuse, early;
   // limit of every wait (ns); a test entry lowers it, together with a
   // withheld page copy (stall_cta, stall_tile; stall_cta < 0: none)
   uint64_t wait_ns;
@@ -628,12 +628,13 @@ __device__ void fused_combine(const TcParams& p, uint8_t* smem, Bars& bars) {
 
 // GM: gate mode (0 none, 1 LN(c (*) g), 2 c (*) g, 3 LN(c + g): eg_mla_gate_mode)
 // DBG: 0 the decode, 1 the cache-read dump (raw pages and gate rows, no
-// attention), 2 the decode with the pipeline trace
+// attention), 2 the decode with the pipeline trace, 3 the decode beside the attention
+// over a shared prefix
 template <int D_C, int GM, int DBG>
 __global__ void __launch_bounds__(kThreads, 1)
     decode_tc_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap krmap,
                      const TcParams p) {
-  constexpr bool DUMP = DBG == 1;
+  constexpr bool DUMP = DBG == 1, BESIDE = DBG == 3;
   using Tracer = TracerT<DBG == 2>;
   constexpr bool GATE = GM != 0;
   constexpr bool GATE_ADD = GM == 3;             // ablation: c + g
@@ -660,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   phase_mark<DBG == 2>(p, 0);
   // beside the attention over a shared prefix most of the grid has no work: out of the
   // way at once (what comes before that kernel, the schedule with it, is complete)
-  if (p.beside) {
+  if constexpr (BESIDE) {
     beside_acquire();
     if (p.starts[blockIdx.x].done) {
       grid_dependency_wait();
@@ -713,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // Everything above touches only this CTA's shared and tensor memory; what
   // follows reads the query-absorption kernel's outputs (prepared queries,
   // split schedule, zeroed counters) and the cache it may have appended to.
-  if (!p.beside) grid_dependency_wait();
+  if constexpr (!BESIDE) grid_dependency_wait();
 
   // an issuer's wait, the choice of the thread that issues, and the warp's joining after it
   auto issuer_wait = [&](uint64_t& bar, uint32_t parity) {
@@ -1568,10 +1569,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   phase_mark<DBG == 2>(p, 2);
   if (warp == kMmaWarp) tmem_dealloc(tmem, C::TMEM_COLS);
   if (threadIdx.x == 0 && bars.abort) report_status(p.status, kStatusTimeout);
-  if constexpr (!DUMP && D_C <= 256) {
+  if constexpr (!DUMP && !BESIDE && D_C <= 256) {
     if (p.fuse) fused_combine<D_C, DBG == 2>(p, smem, bars);
   }
-  if (p.beside) grid_dependency_wait();
+  if constexpr (BESIDE) grid_dependency_wait();
   phase_mark<DBG == 2>(p, 3);
 }
 
@@ -1646,12 +1647,11 @@ cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_
   p.seq_done = reinterpret_cast<uint32_t*>(ws + wl.off_done);
   p.d_v = a.d_v;
   p.early = a.early;
-  p.beside = a.beside;
   p.wait_ns = a.wait_ns;
   p.stall_cta = a.stall_cta;
   p.stall_tile = a.stall_tile;
   // (the fused combine holds kCombineRowsPerWarp rows of W_UV,h per warp)
-  p.fuse = DBG != 1 && !a.apart && D_C <= 256 && a.batch > 0 && kHeads * a.batch <= a.num_splits &&
+  p.fuse = DBG != 1 && DBG != 3 && !a.apart && D_C <= 256 && a.batch > 0 && kHeads * a.batch <= a.num_splits &&
            a.d_v <= kCombineRowsPerWarp * (kThreads / 32) &&
            a.num_splits <= resident_ctas<decode_tc_kernel<D_C, GM, DBG>>(C::SMEM);
   if (fused) *fused = p.fuse != 0;
@@ -1695,6 +1695,11 @@ cudaError_t launch_mode(const DecodeArgs& a, const CUtensorMap* maps, cudaStream
       if (a.d_c == 256) return launch_one<256, GM, 2>(a, maps, st, fused);
       return cudaErrorInvalidValue;
     }
+  }
+  if (a.beside) {
+    if (a.d_c == 192) return launch_one<192, GM, 3>(a, maps, st, fused);
+    if (a.d_c == 256) return launch_one<256, GM, 3>(a, maps, st, fused);
+    return cudaErrorInvalidValue;
   }
   if (a.d_c == 192) return launch_one<192, GM, 0>(a, maps, st, fused);
   if (a.d_c == 256) return launch_one<256, GM, 0>(a, maps, st, fused);
