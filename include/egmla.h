@@ -20,6 +20,11 @@
  *     the query and latent projections (Eqs. 1, 8-10), the latent's RMSNorm
  *     and the rotary embedding, the append and the decode above, and the
  *     output projection (Eq. 14).
+ *   - around the decode of a serving loop: eg_mla_page_plan makes a step's block
+ *     tables, lengths and cache slots on the device; eg_mla_decode_shared decodes
+ *     sequences that share a prefix, which is read once for eight of them;
+ *     eg_mla_page_summary keeps the mean key of every full page, by which
+ *     eg_mla_decode_sparse decodes over the pages that matter most to the query.
  *
  * Conventions shared by every call:
  *   - Every pointer argument except `dims`, `bytes_out` and `out_splits` is a

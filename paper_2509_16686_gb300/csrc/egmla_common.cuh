@@ -143,8 +143,8 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
 // all such cuts the one whose longer side is shortest, by what was measured (in 10 ns):
 // a prefix unit, a page of own tokens with and without a gate, and what a CTA of either
 // kind takes besides (its queries, first scores and partial), the prefix's again for a
-// second row tile.  One after the other on all SMs, 64 sequences over 32K tokens took
-// 59.5 us a call, beside each other 57.0.
+// second row tile.  64 sequences over 32K tokens took 59.5 us a call with the two one
+// after the other on all SMs and 57.0 beside each other (53 with the later steps).
 constexpr int kSharedTile = 8;
 constexpr int kShUnitCost = 70, kShOwnGated = 137, kShOwnPlain = 93, kShFixed = 700, kShOwnFixed = 500;
 
