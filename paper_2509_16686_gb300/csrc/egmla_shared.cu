@@ -205,8 +205,8 @@ constexpr float kSaLazyLog2 = 8.f;              // how far a row's maximum runs 
 
 struct SaBars {
   uint64_t full[8], empty[8];
-  uint64_t sfull[2], pfull[2];
-  uint64_t qfull, qfree, odone, drain;
+  uint64_t sfull[2], pfull[2], odone[2];
+  uint64_t qfull, qfree, drain;
   uint32_t tmem_base;
   int abort;
 };
@@ -284,10 +284,10 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     for (int x = 0; x < 2; ++x) {
       mbar_init(smem_u32(&bars.sfull[x]), 1);
       mbar_init(smem_u32(&bars.pfull[x]), kSaSoftWarps);
+      mbar_init(smem_u32(&bars.odone[x]), 1);
     }
     mbar_init(smem_u32(&bars.qfull), kSaSoftWarps);
     mbar_init(smem_u32(&bars.qfree), kSaSoftWarps);
-    mbar_init(smem_u32(&bars.odone), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     bars.abort = 0;
     fence_mbar_init();
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
           mma_bf16_ts(tmem, tmem + C::kColS + kPage * (i & 1) + 8 * ks, vd + ((ks * 2048) >> 4), idesc_o,
                       (!first || ks > 0) ? 1u : 0u);
         mma_commit(smem_u32(&bars.empty[s]));
-        mma_commit(smem_u32(&bars.odone));
+        mma_commit(smem_u32(&bars.odone[i & 1]));
       };
       while (ok && walk.next(t, lp0, lp1)) {
         ok = mbar_wait(smem_u32(&bars.qfull), seg & 1, abort_flag, p.wait_ns);
@@ -429,6 +429,13 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     uint8_t* stage = smem + (warp - 2) * 2048;
     int n = 0, seg = 0;
     bool ok = true;
+    // O has taken page i, whose scores this warp has had.  Its scores came after O had page
+    // i - 2, and O cannot have page i + 2 before this warp has given weights for it, so the
+    // parity of every other page's barrier is that of page i; with one barrier for all, a
+    // warp ahead of the others would take page i - 2's completion for it.
+    auto o_has = [&](int i) {
+      return sh_warp_wait(smem_u32(&bars.odone[i & 1]), (i >> 1) & 1, abort_flag, p.wait_ns);
+    };
     while (ok && walk.next(t, lp0, lp1)) {
       // (the last partial has left that memory)
       if (seg > 0 && !sh_warp_wait(smem_u32(&bars.qfree), (seg - 1) & 1, abort_flag, p.wait_ns)) break;
@@ -535,8 +542,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
           }
         }
         if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-          // O has taken the page before (completion n of odone is page n's)
-          ok = sh_warp_wait(smem_u32(&bars.odone), (n - 1) & 1, abort_flag, p.wait_ns);
+          ok = o_has(n - 1);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -573,7 +579,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
         for (int e = 0; e < 2; ++e) l[e] = fmaf(l[e], alpha[e], rs[e].x + rs[e].y);
       }
       // ---- the partial
-      if (ok) ok = sh_warp_wait(smem_u32(&bars.odone), (n - 1) & 1, abort_flag, p.wait_ns);
+      if (ok) ok = o_has(n - 1);
       if (!ok) break;
       tc_fence_after();
 #pragma unroll

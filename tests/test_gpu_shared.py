@@ -232,3 +232,18 @@ def test_bad_pages_ids_and_lengths_are_reported(gpu_lib, gate_op):
             s.dc.id_pool[int(s.prefix_table[1]), 5] = s.dc.dims.vocab
         s.run()
         assert s.dc.read_status() == _lib.EG_MLA_ERR_OUT_OF_RANGE, bad
+
+
+@pytest.mark.parametrize("gate_op", ["none", "mul", "mul_ln"])
+@pytest.mark.parametrize("d_c", [192, 256])
+@pytest.mark.parametrize("prefix,splits", [(385, 0), (256, 3), (640, 4), (900, 0)])
+def test_short_ranges_repeat_bit_for_bit(gpu_lib, prefix, splits, d_c, gate_op):
+    """Ranges of a few pages, where a warp may be two pages ahead of another at a range's
+    end: the same bits forty times."""
+    case = make(prefix, (3, 0, 66), d_c=d_c, gate_op=gate_op)
+    s = Shared(case, splits=splits)
+    first = s.run()
+    check(first, reference(case))
+    for _ in range(40):
+        assert np.array_equal(s.run(), first)
+    assert s.dc.read_status() == 0
