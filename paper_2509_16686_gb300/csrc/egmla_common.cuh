@@ -145,11 +145,16 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
 // kind takes besides (its queries, first scores and partial), the prefix's again for a
 // second row tile.  64 sequences over 32K tokens took 59.5 us a call with the two one
 // after the other on all SMs and 57.0 beside each other (53 with the later steps).
-constexpr int kSharedTile = 8;
+// A CTA takes two pages at least: the second costs 0.7 us, the partials that it saves the
+// merge more (eight sequences over 2K tokens 21.2 us with one, 20.7 with two, 21.4 with
+// three).
+constexpr int kSharedTile = 8, kShMinPages = 2;
 constexpr int kShUnitCost = 70, kShOwnGated = 137, kShOwnPlain = 93, kShFixed = 700, kShOwnFixed = 500;
 
 struct alignas(16) SharedSchedule {
   int32_t pages, chunk, parts, own_splits;
+
+  static __host__ __device__ int at_least(int x, int least) { return x > least ? x : least; }
 
   // for `own` of `splits` CTAs; cost: of the longer side.  own_units: of the own
   // tokens' schedule (its cu[batch])
@@ -160,12 +165,12 @@ struct alignas(16) SharedSchedule {
     s.pages = (prefix_len + kPage - 1) / kPage;
     s.own_splits = own;
     const int ctas = splits > own ? splits - own : 1, units = tiles * s.pages;
-    s.chunk = split_chunk(units, ctas);
+    s.chunk = at_least(split_chunk(units, ctas), kShMinPages);
     s.parts = tiles > 0 ? ctas / tiles : 0;
     int64_t pre = static_cast<int64_t>(s.chunk) * kShUnitCost + kShFixed;
     if (s.pages % s.chunk != 0 && tiles > 1) pre += kShFixed;
     if (s.parts > 0) {
-      const int chunk = split_chunk(s.pages, s.parts);
+      const int chunk = at_least(split_chunk(s.pages, s.parts), kShMinPages);
       if (static_cast<int64_t>(chunk) * kShUnitCost + kShFixed <= pre) {
         s.chunk = chunk;
         pre = static_cast<int64_t>(chunk) * kShUnitCost + kShFixed;
