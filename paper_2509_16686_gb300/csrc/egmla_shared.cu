@@ -245,7 +245,7 @@ struct SharedAttnParams {
 struct SaWalk {
   int pages, u, u1;   // pages of the prefix; the next unit and the range's end
   __device__ SaWalk(const SharedAttnParams& p) {
-    const int4 v = __ldg(reinterpret_cast<const int4*>(p.sched));
+    const int4 v = *reinterpret_cast<const int4*>(p.sched);
     const SharedSchedule s = {v.x, v.y, v.z, v.w};
     pages = s.pages;
     s.range(p.batch, static_cast<int>(blockIdx.x), u, u1);
@@ -442,7 +442,8 @@ __global__ void __launch_bounds__(kSaThreads, 1)
       ++seg;
       // the tile's queries (every MMA that read the last tile's is complete).  A lane
       // takes its row of the quadrant, this warp one half of its latent features
-      // (the A operand in tensor memory) and of its RoPE part (shared memory).
+      // (the A operand in tensor memory) and of its RoPE part (shared memory).  Plain
+      // loads: this kernel may have started before the absorption had stored them.
       {
         const int row = 32 * quad + lane, h = row & 15, b = t * kSaSeqs + row / 16;
         const size_t bs = static_cast<size_t>(min(b, p.batch - 1));
@@ -455,7 +456,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
         for (int u = 0; u < 4; ++u) {
           xr[u] = make_uint4(0u, 0u, 0u, 0u);
           if (live)
-            xr[u] = __ldg(reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C) + qop_offset(h, 8 * (4 * sub + u))));
+            xr[u] = *reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C) + qop_offset(h, 8 * (4 * sub + u)));
         }
 #pragma unroll
         for (int u8 = 0; u8 < kHalf; u8 += 8) {
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
           for (int u = 0; u < 8; ++u) {
             x[u] = make_uint4(0u, 0u, 0u, 0u);
             if (live && u8 + u < kHalf)
-              x[u] = __ldg(reinterpret_cast<const uint4*>(lat + qop_offset(h, 8 * (sub * kHalf + u8 + u))));
+              x[u] = *reinterpret_cast<const uint4*>(lat + qop_offset(h, 8 * (sub * kHalf + u8 + u)));
           }
 #pragma unroll
           for (int u0 = 0; u0 < 8 && u8 + u0 < kHalf; u0 += 4) {
@@ -504,7 +505,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int c = 0; c < D_C / kSumFeatures; ++c) bias[e] += __ldg(sums + c * 32 + 16 + r0 + 8 * e);
+          for (int c = 0; c < D_C / kSumFeatures; ++c) bias[e] += sums[c * 32 + 16 + r0 + 8 * e];
       }
       float m_ref[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
       for (int lp = lp0; ok && lp < lp1; ++lp, ++n) {
