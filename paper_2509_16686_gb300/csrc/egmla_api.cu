@@ -431,7 +431,6 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
         extra.prefix_len = prefix->len;
         extra.max_prefix_len = prefix->max_len;
         extra.gate = a.gate;
-        extra.cols = a.d_c / 64;
         extra.sched = const_cast<egmla::SharedSchedule*>(parts.sched);
       }
       e = egmla::launch_prologue_tc(a, app, amaps, st, extra);

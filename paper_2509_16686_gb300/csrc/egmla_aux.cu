@@ -226,9 +226,7 @@ __device__ void schedule_block(const int32_t* seq_lens, int batch, int page_size
     const int own = both ? static_cast<int>(best & 0xffffffffu) : num_splits;
     if (threadIdx.x == 0) {
       int cost;
-      SharedSchedule s = SharedSchedule::make(batch, len, num_splits, own, units, extra.gate != 0, cost);
-      s.slice(batch, num_splits, extra.cols);
-      *extra.sched = s;
+      *extra.sched = SharedSchedule::make(batch, len, num_splits, own, units, extra.gate != 0, cost);
     }
     return own;
   };

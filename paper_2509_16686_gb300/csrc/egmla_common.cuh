@@ -148,14 +148,11 @@ __device__ inline int find_sequence(const int32_t* cu, int batch, int g) {
 // A CTA takes two pages at least: the second costs 0.7 us, the partials that it saves the
 // merge more (eight sequences over 2K tokens 21.2 us with one, 20.7 with two, 21.4 with
 // three).
-// Where the prefix leaves CTAs without work, `slices` of them take a range together: each
-// has all its scores, and 64-feature columns of the output of its own (a partial of all
-// columns takes 2.8 us to leave an SM).
 constexpr int kSharedTile = 8, kShMinPages = 2;
 constexpr int kShUnitCost = 70, kShOwnGated = 137, kShOwnPlain = 93, kShFixed = 700, kShOwnFixed = 500;
 
 struct alignas(16) SharedSchedule {
-  int32_t pages, chunk, parts, own_splits, slices;
+  int32_t pages, chunk, parts, own_splits;
 
   static __host__ __device__ int at_least(int x, int least) { return x > least ? x : least; }
 
@@ -167,7 +164,6 @@ struct alignas(16) SharedSchedule {
     const int tiles = (batch + kSharedTile - 1) / kSharedTile;
     s.pages = (prefix_len + kPage - 1) / kPage;
     s.own_splits = own;
-    s.slices = 1;
     const int ctas = splits > own ? splits - own : 1, units = tiles * s.pages;
     s.chunk = at_least(split_chunk(units, ctas), kShMinPages);
     s.parts = tiles > 0 ? ctas / tiles : 0;
@@ -188,16 +184,7 @@ struct alignas(16) SharedSchedule {
     cost = static_cast<int>(most < INT32_MAX ? most : INT32_MAX);
     return s;
   }
-  // `splits` CTAs in all, `cols` columns of the output
-  __host__ __device__ void slice(int batch, int splits, int cols) {
-    if (pages == 0) return;
-    const int tiles = (batch + kSharedTile - 1) / kSharedTile;
-    if (parts > 0) parts = (pages + chunk - 1) / chunk;   // (the others had none)
-    const int busy = parts > 0 ? tiles * parts : (tiles * pages + chunk - 1) / chunk;
-    const int each = busy > 0 ? (splits - own_splits) / busy : 1;
-    slices = each < 1 ? 1 : each < cols ? each : cols;
-  }
-  // the units of range c
+  // the units of CTA c
   __host__ __device__ void range(int batch, int c, int& u0, int& u1) const {
     const int units = (batch + kSharedTile - 1) / kSharedTile * pages;
     if (parts > 0) {
@@ -210,7 +197,7 @@ struct alignas(16) SharedSchedule {
       u1 = u0 + chunk < units ? u0 + chunk : units;
     }
   }
-  // the ranges c0 .. c0 + n - 1 that leave a partial of row tile t
+  // the CTAs c0 .. c0 + n - 1 that leave a partial of row tile t
   __host__ __device__ int ctas_of(int t, int& c0) const {
     c0 = 0;
     if (pages == 0) return 0;

@@ -203,7 +203,7 @@ struct AbsorbExtra {
   // a shared prefix, whose attention takes a part of the SMs (null: none): its length,
   // and where the schedule of both is written
   const int32_t* prefix_len;
-  int max_prefix_len, gate, cols;   // (cols: 64-feature columns of the latent)
+  int max_prefix_len, gate;
   SharedSchedule* sched;
 };
 cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const CUtensorMap* maps, cudaStream_t st,

@@ -176,8 +176,7 @@ __global__ void __launch_bounds__(32 * kSgWarps, 4) shared_gate_kernel(const Sha
 
 // ============================================================================ 2. attention over the prefix
 // A unit is (row tile of 8 sequences, prefix page); a CTA takes a range of them
-// (SharedSchedule) and leaves one partial per row tile that its range meets; a range may
-// have several CTAs, each with columns of the output of its own.
+// (SharedSchedule) and leaves one partial per row tile that its range meets.
 //
 // Tensor memory (512 columns): O [128 x D_C] fp32, two score buffers [128 x 64]
 // (P in bf16 written over the first half of each), and the latent part of the
@@ -244,16 +243,12 @@ struct SharedAttnParams {
 
 // the range of one CTA: row tile by row tile
 struct SaWalk {
-  int pages, u, u1;        // pages of the prefix; the next unit and the range's end
-  int c, col0, ncols;      // the range; this CTA's 64-feature columns of the output
-  __device__ SaWalk(const SharedAttnParams& p, int cols) {
-    const SharedSchedule s = *p.sched;
+  int pages, u, u1;   // pages of the prefix; the next unit and the range's end
+  __device__ SaWalk(const SharedAttnParams& p) {
+    const int4 v = *reinterpret_cast<const int4*>(p.sched);
+    const SharedSchedule s = {v.x, v.y, v.z, v.w};
     pages = s.pages;
-    c = static_cast<int>(blockIdx.x) / s.slices;
-    const int slice = static_cast<int>(blockIdx.x) - c * s.slices;
-    col0 = slice * cols / s.slices;
-    ncols = (slice + 1) * cols / s.slices - col0;
-    s.range(p.batch, c, u, u1);
+    s.range(p.batch, static_cast<int>(blockIdx.x), u, u1);
   }
   // row tile t, pages lp0 .. lp1 - 1; false at the end
   __device__ bool next(int& t, int& lp0, int& lp1) {
@@ -317,7 +312,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
   const int len = min(max(__ldg(p.prefix_len), 0), p.max_len);   // (an input too)
   grid_dependency_wait();
   grid_launch_dependents();   // the own tokens' split-KV kernel, beside this one
-  SaWalk walk(p, C::kCols);
+  SaWalk walk(p);
   int t, lp0, lp1;
 
   if (warp == 0) {
@@ -362,13 +357,12 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     // ---- MMAs
     constexpr uint32_t idesc_r = idesc_bf16(kSaRows, kPage, 0, 0);   // RoPE part
     constexpr uint32_t idesc_s = F16 ? idesc_f16(kSaRows, kPage, 0, 0) : idesc_r;
-    const int n_o = 64 * walk.ncols;
-    const uint32_t idesc_o = F16 ? idesc_f16(kSaRows, n_o, 0, 1) : idesc_bf16(kSaRows, n_o, 0, 1);
+    constexpr uint32_t idesc_o = F16 ? idesc_f16(kSaRows, D_C, 0, 1) : idesc_bf16(kSaRows, D_C, 0, 1);
     const uint64_t qrdesc = smem_desc(sbase, 16, 1024, kSwizzle128B);
     const uint64_t kdesc = smem_desc(sbase + C::kOffRing, 16, 1024, kSwizzle128B);
     // Z [keys x features] as the MN-major B operand: 64-feature columns 8 KB apart,
     // groups of 8 keys 1 KB apart
-    const uint64_t vdesc = smem_desc(sbase + C::kOffRing + walk.col0 * kSaCol, kSaCol, 1024, kSwizzle128B);
+    const uint64_t vdesc = smem_desc(sbase + C::kOffRing, kSaCol, 1024, kSwizzle128B);
     if (elect_one()) {
       bool ok = true, issued = false;
       int n = 0, seg = 0;   // pages and row tiles before this row tile
@@ -554,7 +548,6 @@ __global__ void __launch_bounds__(kSaThreads, 1)
           tc_fence_after();
 #pragma unroll
           for (int g = 0; g < C::kCols; ++g) {
-            if (g >= walk.ncols) break;
             float o[32];
             tmem_ld_16x256b_x8(lane_base + 64 * g, o);
             tmem_wait_ld();
@@ -596,8 +589,8 @@ __global__ void __launch_bounds__(kSaThreads, 1)
         l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
       }
       const int b = t * kSaSeqs + seq;
-      const size_t row = (static_cast<size_t>(walk.c + t) * kSaSeqs + seq) * 16 + r0;   // and row + 8
-      if (b < p.batch && (lane & 3) == 0 && walk.col0 == 0) {
+      const size_t row = (static_cast<size_t>(blockIdx.x + t) * kSaSeqs + seq) * 16 + r0;   // and row + 8
+      if (b < p.batch && (lane & 3) == 0) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           *reinterpret_cast<float2*>(p.part_ml + (row + 8 * e) * 2) =
@@ -605,18 +598,16 @@ __global__ void __launch_bounds__(kSaThreads, 1)
       }
 #pragma unroll
       for (int g = 0; g < C::kCols; ++g) {
-        if (g >= walk.ncols) break;
         float o[32];
         tmem_ld_16x256b_x8(lane_base + 64 * g, o);
         tmem_wait_ld();
-        const int f0 = 64 * (walk.col0 + g);
         if (b >= p.batch) continue;   // uniform in the warp
         // 32 columns at a time through shared memory, so that a store covers whole lines
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
           for (int k = 4 * half; k < 4 * half + 4; ++k) {
-            const int f = f0 + 8 * k + c2;
+            const int f = 64 * g + 8 * k + c2;
             const float2 gm = *reinterpret_cast<const float2*>(affine + f);
             const float2 bt = *reinterpret_cast<const float2*>(affine + D_C + f);
 #pragma unroll
@@ -631,7 +622,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
           for (int i = 0; i < 4; ++i) {
             const int rr = 4 * i + (lane >> 3), u = lane & 7;
             const float4 x = *reinterpret_cast<const float4*>(stage + rr * 128 + ((u ^ (rr & 7)) << 4));
-            *reinterpret_cast<float4*>(p.part_o + (row - r0 + rr) * D_C + f0 + 32 * half + 4 * u) = x;
+            *reinterpret_cast<float4*>(p.part_o + (row - r0 + rr) * D_C + 64 * g + 32 * half + 4 * u) = x;
           }
           __syncwarp();
         }
