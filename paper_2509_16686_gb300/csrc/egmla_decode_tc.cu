@@ -664,7 +664,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (BESIDE) {
     beside_acquire();
     if (p.starts[blockIdx.x].done) {
-      grid_launch_dependents();   // (the combine's set-up may begin: eight sequences over 2K tokens 20.6 -> 20.4 us)
       grid_dependency_wait();
       return;
     }
@@ -794,9 +793,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // sequences 69.8 us against 68.2).  128 at d_c 512 119.7 -> 118.5 us, 32 x
       // 4K 37.7 -> 37.2, 64 x 8K layer 102.4 -> 101.5 (against a trigger at the
       // start), at d_c 192 91.3 -> 90.8; outside layers d_c 192 lost (67.7 ->
-      // 67.9, 32 x 4K 33.7 -> 33.9).  Beside a shared prefix it pays at d_c 192 too (30.4 ->
-      // 30.1), and this kernel's start stands for the kernel before the call.
-      if (!p.fuse && (BESIDE || D_C > 192 || p.early)) grid_launch_dependents();
+      // 67.9, 32 x 4K 33.7 -> 33.9).
+      if (!p.fuse && (D_C > 192 || p.early)) grid_launch_dependents();
       // drain: every copy this thread issued must land before the CTA exits,
       // also after an abort (own flag: the wait is bounded but not cut short)
       volatile int own = 0;
