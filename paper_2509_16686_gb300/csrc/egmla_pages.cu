@@ -776,7 +776,7 @@ cudaError_t launch_select(const SelectArgs& a, cudaStream_t st) {
 // each): a block's further rounds find the queries in shared memory.
 int select_chunks(int max_seq_len, int batch, int budget, int keep_first, int keep_last, int d_c, int d_r) {
   const int pages = (max_seq_len + kPage - 1) / kPage, ranked = pages - keep_first - keep_last;
-  if (pages <= budget || budget <= keep_first + keep_last) return 1;
+  if (batch == 0 || pages <= budget || budget <= keep_first + keep_last) return 1;
   const int64_t groups = (ranked + kSelPages - 1) / kSelPages, all = groups * batch;
   const int most = row_parts(d_c, d_r) == 1 ? kSelRounds : kWideRounds;
   const int64_t rounds = all > most * kSms ? most : (all + kSms - 1) / kSms;

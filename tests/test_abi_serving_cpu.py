@@ -1,6 +1,9 @@
 """Refusals of the serving calls (page plan, summaries, sparse and shared decode) that
 come before any launch, and their workspace sizes: no GPU is needed."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -105,6 +108,25 @@ def test_sparse_refusals(lib):
     raw = lib.eg_mla_decode_sparse_workspace_size
     d = ctypes.byref(dims())
     assert raw(d, -1, 40, 8, 152) == 0 and raw(d, 3, 0, 8, 152) == 0 and raw(d, 3, 40, 0, 152) == 0
+
+
+def test_sparse_decode_of_no_sequence_returns():
+    """Nothing to do, whatever the bounds: in a process of its own, which a division by
+    the number of blocks would end."""
+    code = """
+import ctypes
+from paper_2509_16686_gb300 import _lib
+lib, F = _lib.load(), 0x10000
+for d in (_lib.make_dims(16, 128, 64, 128, 256, 32000), _lib.make_dims(16, 128, 64, 128, 512, 32000, gate=False),
+          _lib.make_dims(4, 32, 16, 32, 64, 1000, dtype="fp32")):
+    for pages in (1, 40, 100000):
+        rc = lib.eg_mla_decode_sparse(ctypes.byref(d), F, F, F, F, F, pages, F, 64 * pages, 0, 99, F, 8, 1, 2, F, None,
+                                      None, F, F, F, None, 152, F, 1 << 30, None, None)
+        assert rc == 0, (pages, rc)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert done.returncode == 0, (done.returncode, done.stderr)
 
 
 SUMMARY = dict(dims=dims(), c_pool=FAKE, krope_pool=FAKE, id_pool=FAKE, block_table=FAKE, max_pages=40, seq_lens=FAKE,
