@@ -142,8 +142,9 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
     E[p.batch] = total_need;
     cum[p.batch] = R;
   }
-  const int avail = min(F + R, p.num_pages);
-  if (avail < F + R) bad = true;   // more pages released than there are
+  // more pages released than there is room for: the rest is dropped (R may be near 2^31, F + R above it)
+  const int avail = F + min(R, p.num_pages - F);
+  if (avail - F < R) bad = true;
   __syncthreads();
   cluster_sync();
   // pages released, in the order of the batch

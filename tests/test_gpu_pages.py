@@ -529,3 +529,22 @@ def test_sparse_reports_bad_lengths_and_pages(gpu_lib):
     p.dc.block_table[5, 7] = -3
     p.run(5)
     assert p.dc.read_status() == _lib.EG_MLA_ERR_OUT_OF_RANGE
+
+
+def test_plan_drops_what_the_stack_cannot_hold_whatever_the_sum(gpu_lib):
+    """Stale lengths that give back nearly 2^31 pages to a stack of 200,000."""
+    B, width, num_pages, free = 16384, 131071, 200000, 160000
+    table = torch.zeros((B, width), dtype=torch.int32, device="cuda")
+    table[0, :num_pages - free] = torch.arange(free, num_pages, dtype=torch.int32, device="cuda")
+    stack = torch.arange(num_pages, dtype=torch.int32, device="cuda")
+    stack[free:] = -1
+    lens, new = dev([width * P] * (B - 1) + [0]), dev([-1] * (B - 1) + [1])
+    assert (B - 1) * width + free > 2 ** 31 - 1
+    lens_out, left, cu, pos, slots, status = dev([-9] * B), dev([-9]), dev([0] * (B + 1)), dev([0] * B), dev([0] * 2), dev([0])
+    _lib.eg_mla_page_plan(new, lens, lens_out, table, stack, dev([free]), left, cu, pos, slots, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == _lib.EG_MLA_ERR_OUT_OF_RANGE
+    assert left.tolist() == [num_pages - 1]
+    assert stack.tolist() == list(range(num_pages))
+    assert lens_out.tolist() == [0] * (B - 1) + [1] and int(cu[B].item()) == 1 and pos.tolist() == [-1] * (B - 1) + [0]
+    assert int(table[B - 1, 0].item()) == num_pages - 1 and slots.tolist() == [(num_pages - 1) * P, -1]
