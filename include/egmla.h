@@ -249,6 +249,10 @@ int eg_mla_step(const eg_mla_dims* dims, void* c_pool, void* krope_pool, int32_t
  *                   max_prefix_len, num_splits) bytes, 256-byte aligned: that of
  *                   eg_mla_decode, the gated prefix (with the gate off one page)
  *                   and the prefix's partial results
+ * With a LayerNorm gate the prefix is met in f16: the normalised latent, the softmax
+ * weights and q^ (*) gamma, kept at a power of two that follows softmax_scale.  An
+ * element of q^ (*) gamma that gives a score of about 2^20 and more for each unit of the
+ * normalised latent is taken as one that gives 2^20 (one that is infinite stays so).
  * A sequence without any token gets u = 0.  Device errors: as for eg_mla_decode;
  * a *prefix_len outside 0 .. max_prefix_len is reported as
  * EG_MLA_ERR_OUT_OF_RANGE and taken as the nearer bound.

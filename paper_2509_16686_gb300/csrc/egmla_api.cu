@@ -422,7 +422,10 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
       if (prefix->max_len > 0 && !encode_shared_maps(smaps, dims, a, sh)) return EG_MLA_ERR_CUDA;
     }
     egmla::AbsorbExtra extra = {};
-    if (prefix != nullptr && a.gate_ln) extra.q16 = static_cast<uint8_t*>(workspace) + sh.wl.off_q;
+    if (prefix != nullptr && a.gate_ln) {
+      extra.q16 = static_cast<uint8_t*>(workspace) + sh.wl.off_q;
+      extra.q_scale = sh.q_scale = egmla::shared_q_scale(resolve_scale(dims));
+    }
     const bool with_prefix = prefix != nullptr && prefix->max_len > 0;
     cudaError_t e = cudaSuccess;
     if (sparse == nullptr) {

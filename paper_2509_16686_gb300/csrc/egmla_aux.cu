@@ -432,7 +432,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           // (a finite value beyond f16's range stays finite, an infinite one or NaN what it is)
-          float x = v[j] * gm * kShQScale;
+          float x = v[j] * gm * extra.q_scale;
           if (fabsf(x) < INFINITY) x = fminf(fmaxf(x, -65504.f), 65504.f);
           if (c0 + j < nb) *reinterpret_cast<__half*>(qh + j * qprep_lat_bytes(d_c)) = __float2half_rn(x);
         }

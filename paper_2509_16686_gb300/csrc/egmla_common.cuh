@@ -12,6 +12,7 @@
 // is c + b: the CTA ranges of consecutive sequences overlap in at most one CTA,
 // so these slots never collide and there are at most num_splits + batch of them.
 #pragma once
+#include <cmath>
 #include <cstddef>
 #include <cstdint>
 
@@ -214,11 +215,15 @@ struct alignas(16) SharedSchedule {
 // meet the prefix in f16, whose three more bits of significand than bf16's make the
 // roundings of z', of the softmax weights and of q^ gamma small against the output's
 // (rel-L2 against 64 bits of the emulated arithmetic, 8 and 17 sequences of a few
-// tokens after 64: 3.0e-3 in bf16, 1.9e-3 in f16).  q^ gamma is kept 2^-kShQShift
-// times its value: it may reach 1.6e7, and its smallest step, 1.5e-5, moves a score
-// by about 1e-5.
-constexpr int kShQShift = 8;
-constexpr float kShQScale = 1.f / (1 << kShQShift);
+// tokens after 64: 3.0e-3 in bf16, 1.9e-3 in f16).  q^ gamma is kept 2^k times its
+// value, with the k that puts softmax_scale 2^-k between 16 and 32 (-8 for the usual
+// scale of 128 + 64 dimensions): f16's smallest step, 2^-24, then moves a score by
+// about 1e-5 whatever the scale, and an element clamped to its largest value, 65504, is
+// one that gives a score of 2^20 and more for each unit of z'.
+inline float shared_q_scale(float softmax_scale) {
+  const int k = std::ilogb(softmax_scale) - 4;
+  return std::ldexp(1.f, k < -100 ? -100 : k > 100 ? 100 : k);
+}
 
 // rows of the gated prefix: whole pages; with the gate off only the last page
 __host__ __device__ inline size_t shared_z_rows(int max_prefix_len, bool gate) {

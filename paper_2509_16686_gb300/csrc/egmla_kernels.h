@@ -197,6 +197,7 @@ struct SparseLens {
 // `extra`: the absorbed queries in other forms too.  a.q null: the schedule only
 struct AbsorbExtra {
   uint8_t* q16;     // q^ gamma in f16, for the attention over a shared prefix (null: none)
+  float q_scale;    // times this (shared_q_scale)
   float* q32;       // per sequence q^ [H, d_c], then q^R [H, d_rope], in fp32, for the page scores (null: none)
   SparseLens sparse;
   int chain;        // the kernel after this one runs beside it (see launch_chained)
@@ -243,6 +244,7 @@ bool tc_supported(int d_c, int gate);
 struct SharedArgs {
   const DecodeArgs* dec;
   SharedLayout wl;
+  float q_scale = 1.f;   // of q^ gamma in f16 (AbsorbExtra)
   const int32_t* prefix_table;
   const int32_t* prefix_len;
   int max_prefix_len;

@@ -227,7 +227,7 @@ struct SaCfg {
 struct SharedAttnParams {
   const uint8_t* qprep;   // the prepared query blocks: q^R, the sums of q^ . beta and (bf16) q^ gamma
   size_t qstride;
-  const uint8_t* q16;     // q^ gamma in f16
+  const uint8_t* q16;     // q^ gamma in f16, q_scale times its value
   const int32_t* table;
   const int32_t* prefix_len;
   const SharedSchedule* sched;
@@ -236,7 +236,7 @@ struct SharedAttnParams {
   float* part_ml;
   float* part_o;
   int batch, max_len, num_pages, gate;
-  float scale_log2;
+  float scale_log2, q_scale;
   uint64_t wait_ns;
   int32_t* status;
 };
@@ -261,7 +261,7 @@ struct SaWalk {
   }
 };
 
-// F16: the latent's products in f16 (q^ 2^-kShQShift times its value, q^R likewise),
+// F16: the latent's products in f16 (q^ q_scale times its value, a power of two, q^R likewise),
 // and the weights 2^kPShift times theirs, so that they reach from 2^-32 to 2^15 of the
 // reference; otherwise in bf16 (a latent of any magnitude), unscaled.
 template <int D_C, bool F16>
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
     const int seq = 2 * quad + sub;                         // of the tile
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(32 * quad + 16 * sub) << 16);
     const int r0 = lane >> 2, c2 = 2 * (lane & 3);
-    const float sl2 = p.scale_log2 * (F16 ? 1.f / kShQScale : 1.f);
+    const float sl2 = F16 ? p.scale_log2 / p.q_scale : p.scale_log2;
     // a partial leaves through the memory of q^R, which is read no more by then: 2 KB a warp
     uint8_t* stage = smem + (warp - 2) * 2048;
     int n = 0, seg = 0;
@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(kSaThreads, 1)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           if constexpr (F16) {   // exact: the exponent alone changes
-            const __nv_bfloat162 f = __float2bfloat162_rn(kShQScale);
+            const __nv_bfloat162 f = __float2bfloat162_rn(p.q_scale);
             __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&xr[u]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = __hmul2(w[i], f);
@@ -697,6 +697,7 @@ cudaError_t launch_shared_attn(const SharedArgs& a, const CUtensorMap* maps, cud
   p.num_pages = d.num_pages;
   p.gate = d.gate;
   p.scale_log2 = d.scale_log2;
+  p.q_scale = a.q_scale;
   p.wait_ns = d.wait_ns;
   p.status = d.status;
   if (d.gate_ln) return d.d_c == 256 ? launch_attn<256, true>(a, maps, p, st) : launch_attn<192, true>(a, maps, p, st);

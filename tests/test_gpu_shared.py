@@ -247,3 +247,22 @@ def test_short_ranges_repeat_bit_for_bit(gpu_lib, prefix, splits, d_c, gate_op):
     for _ in range(40):
         assert np.array_equal(s.run(), first)
     assert s.dc.read_status() == 0
+
+
+@pytest.mark.parametrize("gate_op", ["mul_ln", "add_ln", "mul", "none"])
+@pytest.mark.parametrize("power", [10, 40, -10, -40])
+def test_softmax_scales_and_queries_of_any_size(gpu_lib, power, gate_op):
+    """A softmax scale 2^power times the usual one with queries 2^-power times theirs: every
+    score stays as it is, and so does every bit of the result."""
+    def scaled(by):
+        def change(case):
+            case.dims.softmax_scale = float(np.float32(192 ** -0.5)) * 2.0 ** by
+            case.q[:] = synth.f32_to_bf16_bits(synth.bf16_bits_to_f32(case.q) * np.float32(2.0 ** -by))
+        return make(300, (2, 70, 1), gate_op=gate_op, change=change)
+
+    case = scaled(power)
+    s, usual = Shared(case), Shared(scaled(0))
+    got, want = s.run(), usual.run()
+    assert s.dc.read_status() == 0
+    check(got, reference(case))
+    assert np.array_equal(got, want)
