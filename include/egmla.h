@@ -357,9 +357,10 @@ int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void*
  *   score_b(p) = max_h scale (q^_b,h . m^c_p + q^R_b,h . m^R_p),
  * [m^c_p ; m^R_p] = summary[page p] (eg_mla_page_summary): a page is as important
  * as its mean key is to the head that wants it most.  Equal scores: the earlier
- * page first; a score that is no number comes last.  Scores are computed and
- * compared in fp32.  The result is eg_mla_decode's over the chosen pages' tokens.
- * One selection serves all heads, which share the latent.
+ * page first.  A head whose product is no number is left out of the maximum; a page
+ * that no head has a number for comes last, after one of minus infinity.  Scores are
+ * computed and compared in fp32.  The result is eg_mla_decode's over the chosen pages'
+ * tokens.  One selection serves all heads, which share the latent.
  *
  *   summary      [num_pages, d_c + d_rope] fp32, 16-byte aligned; read for the
  *                pages that are ranked, all of which are full

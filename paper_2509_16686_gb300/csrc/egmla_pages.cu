@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) select_pages_kernel(const Sele
         }
       }
       float best = sum32_transpose(acc, lane);   // lane l: of page l / HH
-      if (h0 + lane % HH >= p.H) best = -INFINITY;
+      if (h0 + lane % HH >= p.H) best = NAN;   // no head: left out, as a head without a number is
 #pragma unroll
       for (int o = HH / 2; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
       if (lane % HH == 0) bests[r][warp % kShare][row0 + lane / HH] = best;

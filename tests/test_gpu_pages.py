@@ -548,3 +548,23 @@ def test_plan_drops_what_the_stack_cannot_hold_whatever_the_sum(gpu_lib):
     assert stack.tolist() == list(range(num_pages))
     assert lens_out.tolist() == [0] * (B - 1) + [1] and int(cu[B].item()) == 1 and pos.tolist() == [-1] * (B - 1) + [0]
     assert int(table[B - 1, 0].item()) == num_pages - 1 and slots.tolist() == [(num_pages - 1) * P, -1]
+
+
+@pytest.mark.parametrize("name", ["gate256", "none512", "fp32_64", "fp32_132", "fp32_none", "fp32_512"])
+def test_a_page_without_a_number_comes_after_the_lowest_score(gpu_lib, name):
+    """Whatever the number of heads: a page whose every head has no number ranks after one
+    of minus infinity; heads without a number are left out where others have one."""
+    p = Sparse(make(name, (64 * 20,)))
+    d, n = p.case.dims, 20
+    p.summary.fill_(0.0)
+    p.dc.q[0, :, d.d_nope] = 1.0
+    p.dc.q[0, :, d.d_nope + 1] = 1.0
+    p.dc.q[0, 0, d.d_nope + 1] = 0.0
+    page = [int(x) for x in p.case.block_table[0]]
+    p.summary[page[5]] = float("nan")
+    p.summary[page[9], d.d_c] = -float("inf")
+    assert p.run(n - 1)[0].tolist() == [i for i in range(n) if i != 5]
+    assert p.run(n - 2)[0].tolist() == [i for i in range(n) if i not in (5, 9)]
+    # head 0 has 0 times infinity, the others infinity: the page is the best
+    p.summary[page[12], d.d_c + 1] = float("inf")
+    assert p.run(3)[0].tolist() == [0, 12, n - 1]
