@@ -484,8 +484,9 @@ __device__ __forceinline__ float sum32_transpose(float (&v)[32], int lane) {
   return v[0];
 }
 
+// scores as whole numbers of the same order: no number last, +0 and -0 (a score that underflows) the same
 __device__ __forceinline__ uint32_t score_key(float s) {
-  const uint32_t u = __float_as_uint(s);
+  const uint32_t u = s == 0.f ? 0u : __float_as_uint(s);
   return s != s ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 

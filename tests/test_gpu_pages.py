@@ -568,3 +568,15 @@ def test_a_page_without_a_number_comes_after_the_lowest_score(gpu_lib, name):
     # head 0 has 0 times infinity, the others infinity: the page is the best
     p.summary[page[12], d.d_c + 1] = float("inf")
     assert p.run(3)[0].tolist() == [0, 12, n - 1]
+
+
+@pytest.mark.parametrize("name", ["gate256", "fp32_64"])
+def test_a_score_that_underflows_equals_zero(gpu_lib, name):
+    """Scores of +0 and of -0 (a small negative one times a small scale) are equal: by position."""
+    case = make(name, (64 * 20,))
+    case = dataclasses.replace(case, dims=dataclasses.replace(case.dims, softmax_scale=1e-30))
+    p = Sparse(case)
+    p.summary.fill_(0.0)
+    p.dc.q[0, :, case.dims.d_nope] = 1.0
+    p.summary[int(case.block_table[0, 3]), case.dims.d_c] = -1e-30
+    assert p.run(6)[0].tolist() == [0, 1, 2, 3, 4, 19]
