@@ -204,12 +204,13 @@ __device__ void selected_lengths(const SparseLens& s, const int32_t* seq_lens, i
 template <bool EXTRA>
 __device__ void schedule_block(const int32_t* seq_lens, int batch, int page_size, int32_t* cu, uint32_t* seq_done,
                                int num_splits, const AbsorbExtra& extra, const int32_t* block_table, int max_pages,
-                               SplitStart* starts, int32_t* smem, int words, int32_t* wsum) {
+                               SplitStart* starts, int32_t* smem, int words, int32_t* wsum, int32_t* status) {
   // With a shared prefix the own tokens are cut for a part of the splits: each thread
   // weighs some of the choices, the cheapest (of equals the fewest own splits) is written.
   auto cut_for = [&](int units) {
     if (!EXTRA || extra.prefix_len == nullptr) return num_splits;
-    const int len = min(max(__ldg(extra.prefix_len), 0), extra.max_prefix_len);
+    const int given = __ldg(extra.prefix_len), len = min(max(given, 0), extra.max_prefix_len);
+    if (given != len && threadIdx.x == 0) report_status(status, kStatusOutOfRange);
     const bool both = len > 0 && num_splits > 1;
     unsigned long long best = ~0ull;
     for (int own = 1 + threadIdx.x; both && own < num_splits; own += blockDim.x) {
@@ -314,7 +315,7 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         lens = extra.sparse.lens;
       }
       schedule_block<EXTRA>(lens, batch, page_size, cu, seq_done, num_splits, extra, block_table, max_pages, starts,
-                            words + 8, kWords, words);
+                            words + 8, kWords, words, status);
     } else {
       const int b = (static_cast<int>(blockIdx.x) - (ntiles + 1)) * (kPmThreads / 32) + warp;
       if (b < app.batch) append_row(app, b, lane, 32);

@@ -92,8 +92,7 @@ __global__ void __launch_bounds__(32 * kSgWarps, 4) shared_gate_kernel(const Sha
   // beside the query absorption (nothing here needs it): its wait comes at the end
   grid_launch_dependents();
   beside_acquire();
-  const int given = __ldg(p.prefix_len), len = min(max(given, 0), p.max_len);
-  if (given != len && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, kStatusOutOfRange);
+  const int len = min(max(__ldg(p.prefix_len), 0), p.max_len);   // (reported by the schedule)
   const int first = GATE ? 0 : len / kPage * kPage;   // the row that z begins with
   const int rows = (len + kPage - 1) / kPage * kPage - first;
   const int t0 = (blockIdx.x * kSgWarps + warp) * kSgRows;

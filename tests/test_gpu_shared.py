@@ -266,3 +266,14 @@ def test_softmax_scales_and_queries_of_any_size(gpu_lib, power, gate_op):
     assert s.dc.read_status() == 0
     check(got, reference(case))
     assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("gate_op", ["none", "mul_ln"])
+@pytest.mark.parametrize("length", [1, -1, 2 ** 31 - 1])
+def test_a_prefix_where_the_bound_is_zero_is_reported(gpu_lib, length, gate_op):
+    case = make(0, (3, 0, 200), gate_op=gate_op)
+    s = Shared(case, max_prefix=0)
+    s.prefix_len.fill_(length)
+    got = s.run()
+    assert s.dc.read_status() == _lib.EG_MLA_ERR_OUT_OF_RANGE
+    check(got, reference(case))   # taken as 0
