@@ -232,8 +232,8 @@ int eg_mla_step(const eg_mla_dims* dims, void* c_pool, void* krope_pool, int32_t
  * rows of one matrix product; the own tokens go through eg_mla_decode's kernel,
  * and the partial results of both are merged by log-sum-exp.
  *
- * Supported: bf16 with d_c in {192, 256}, every gate mode
- * (EG_MLA_ERR_UNSUPPORTED otherwise).
+ * Supported: bf16 with d_c in {192, 256}, every gate mode; max_prefix_len and
+ * max_seq_len at most 2^31 - 64 (EG_MLA_ERR_UNSUPPORTED otherwise).
  *
  *   prefix_table    [ceil(max_prefix_len / page_size)] int32 on the device: the
  *                   prefix's physical pages in order (may be NULL with
@@ -332,7 +332,7 @@ int eg_mla_page_plan(const int32_t* new_tokens, const int32_t* seq_lens, int32_t
  *   c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens,
  *   max_seq_len, batch, num_pages, gate_table, ln_gamma, ln_beta: as for
  *                   eg_mla_decode (the same dims are supported; row sizes in bytes
- *                   must be multiples of 16)
+ *                   must be multiples of 16, max_seq_len at most 2^31 - 64)
  *   new_tokens      [batch] int32 or NULL (all tokens); negative: none
  *   max_new_tokens  host-side bound of new_tokens (ignored with NULL)
  *   summary         [num_pages, d_c + d_rope] fp32, 16-byte aligned; the rows of
@@ -373,7 +373,7 @@ int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void*
  *                that of eg_mla_decode, the absorbed queries in fp32, a score per
  *                page and the selected block table
  *   the others   as for eg_mla_decode; every dims that it supports with d_rope a
- *                multiple of 4
+ *                multiple of 4, max_seq_len at most 2^31 - 64
  * Device errors: as for eg_mla_decode; a length outside 0 .. max_seq_len is
  * reported as EG_MLA_ERR_OUT_OF_RANGE and taken as the nearer bound.
  */

@@ -48,6 +48,9 @@ int check_dims(const eg_mla_dims* d) {
   return EG_MLA_ERR_INVALID_ARG;
 }
 
+// tokens whose pages can be counted as (tokens + page - 1) / page in 32 bits
+bool countable(int32_t tokens) { return tokens <= INT32_MAX - egmla::kPage + 1; }
+
 int resolve_splits(int32_t num_splits, int32_t* out) {
   if (num_splits < 0) return EG_MLA_ERR_INVALID_ARG;
   if (num_splits > 0) {
@@ -353,6 +356,7 @@ int shared_workspace(const eg_mla_dims* d, int32_t batch, int32_t max_prefix_len
   if (rc != EG_MLA_OK) return rc;
   if (!is_tc_path(d) || !egmla::shared_supported(d->d_c)) return EG_MLA_ERR_UNSUPPORTED;
   if (batch < 0 || max_prefix_len < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (!countable(max_prefix_len)) return EG_MLA_ERR_UNSUPPORTED;
   // the schedule counts row tiles x pages in 32 bits
   if ((static_cast<int64_t>(batch) / egmla::kSharedTile + 1) * (max_prefix_len / d->page_size + 1) > INT32_MAX / 2)
     return EG_MLA_ERR_UNSUPPORTED;
@@ -381,6 +385,7 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     const int rc = shared_workspace(dims, batch, prefix->max_len, num_splits, &sh.wl, &splits);
     if (rc != EG_MLA_OK) return rc;
     if (prefix->len == nullptr || (prefix->table == nullptr && prefix->max_len > 0)) return EG_MLA_ERR_INVALID_ARG;
+    if (!countable(max_seq_len)) return EG_MLA_ERR_UNSUPPORTED;
     if (workspace_bytes < sh.wl.total) return EG_MLA_ERR_WORKSPACE;
   }
   DecodeArgs a;
@@ -631,7 +636,7 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
     return EG_MLA_ERR_INVALID_ARG;
   if (keep_first < 0 || keep_last < 1 || budget < keep_last || budget - keep_last < keep_first)
     return EG_MLA_ERR_INVALID_ARG;
-  if (dims->d_rope % 4 != 0) return EG_MLA_ERR_UNSUPPORTED;
+  if (dims->d_rope % 4 != 0 || !countable(max_seq_len)) return EG_MLA_ERR_UNSUPPORTED;
   if (block_table == nullptr || seq_lens == nullptr || summary == nullptr || !aligned(summary, 16))
     return EG_MLA_ERR_INVALID_ARG;
   int32_t splits = 0;
@@ -690,7 +695,7 @@ int eg_mla_page_summary(const eg_mla_dims* dims, const void* c_pool, const void*
       static_cast<int64_t>(max_seq_len) > static_cast<int64_t>(max_pages_per_seq) * dims->page_size)
     return EG_MLA_ERR_INVALID_ARG;
   const int eb = elem_bytes(dims);
-  if (dims->d_c * eb % 16 || dims->d_rope * eb % 16) return EG_MLA_ERR_UNSUPPORTED;
+  if (dims->d_c * eb % 16 || dims->d_rope * eb % 16 || !countable(max_seq_len)) return EG_MLA_ERR_UNSUPPORTED;
   const bool gate = dims->gate_mode != EG_MLA_GATE_NONE;
   if (c_pool == nullptr || krope_pool == nullptr || block_table == nullptr || seq_lens == nullptr ||
       summary == nullptr || (gate && (id_pool == nullptr || gate_table == nullptr)))

@@ -168,6 +168,16 @@ def test_plan_refusals(lib):
         assert rc(**kw) == UNSUPPORTED, kw
 
 
+def test_lengths_within_a_page_of_32_bits_are_refused(lib):
+    """The pages of such a length are not counted in 32 bits."""
+    for most, rc in ((2 ** 31 - 1, UNSUPPORTED), (2 ** 31 - 63, UNSUPPORTED), (2 ** 31 - 64, WORKSPACE)):
+        assert call(lib.eg_mla_decode_sparse, SPARSE, max_pages=2 ** 25, max_seq_len=most, bytes=1) == rc
+        assert call(lib.eg_mla_decode_shared, SHARED, dims=dims(gate=False), max_prefix_len=most, bytes=1) == rc
+        assert call(lib.eg_mla_decode_shared, SHARED, max_pages=2 ** 25, max_seq_len=most, bytes=1) == rc
+    for most in (2 ** 31 - 1, 2 ** 31 - 63):
+        assert call(lib.eg_mla_page_summary, SUMMARY, max_pages=2 ** 25, max_seq_len=most) == UNSUPPORTED
+
+
 def test_no_pages_has_its_own_text(lib):
     assert b"page" in lib.eg_mla_status_string(_lib.EG_MLA_ERR_NO_PAGES)
     assert b"unknown" in lib.eg_mla_status_string(-9)
