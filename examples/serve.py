@@ -41,8 +41,8 @@ class Layer:
         self.free = torch.arange(num_pages, dtype=torch.int32, device="cuda")
         self.free_count = torch.full((1,), num_pages, dtype=torch.int32, device="cuda")
         self.cu, self.positions, self.status = self.ints(sequences + 1), self.ints(sequences), self.ints(1)
-        self.slots = self.ints(max_pages * PAGE)
-        self.longest = 0   # the host's bound of every length
+        self.slots = self.ints(max(max_pages * PAGE, sequences))
+        self.most = [0] * sequences   # the host's bound of every length
 
     @staticmethod
     def ints(*shape):
@@ -62,7 +62,7 @@ class Layer:
     def plan(self, new):
         """Pages for new[b] tokens of every sequence (negative: it leaves), in place."""
         self.new = torch.tensor(new, dtype=torch.int32, device="cuda")
-        self.longest += max(0, *new)
+        self.most = [m + n if n >= 0 else 0 for m, n in zip(self.most, new)]
         _lib.eg_mla_page_plan(self.new, self.lens, self.lens, self.table, self.free, self.free_count, self.free_count,
                               self.cu, self.positions, self.slots, dev_status=self.status)
 
@@ -83,8 +83,9 @@ class Layer:
 
     def summarise(self):
         """Mean keys of the pages that the planned tokens completed."""
-        _lib.eg_mla_page_summary(self.dims, *self.cache(), self.table, self.lens, self.longest, *self.gate, self.summary,
-                                 new_tokens=self.new, max_new_tokens=self.longest, dev_status=self.status)
+        longest = max(self.most)
+        _lib.eg_mla_page_summary(self.dims, *self.cache(), self.table, self.lens, longest, *self.gate, self.summary,
+                                 new_tokens=self.new, max_new_tokens=longest, dev_status=self.status)
 
     @staticmethod
     def bytes(n):
@@ -115,20 +116,18 @@ def main(document=1000, sequences=12, steps=70, budget=8):
     # the questions: a token each per step, over the document and their own tokens
     prefix = layer.table[0, :pages_of(document)].contiguous()
     prefix_len = torch.full((1,), document, dtype=torch.int32, device="cuda")
-    layer.longest = 0
     out = torch.empty((sequences, HEADS, D_NOPE), dtype=torch.bfloat16, device="cuda")
     ws = layer.bytes(_lib.eg_mla_decode_shared_workspace_size(layer.dims, sequences, document))
     for _ in range(steps):
         layer.plan([0] + [1] * sequences)
         q = layer.append()[1:].contiguous()
         _lib.eg_mla_decode_shared(layer.dims, q, *layer.cache(), prefix, prefix_len, document,
-                                  layer.table[1:].contiguous(), layer.lens[1:].contiguous(), layer.longest, *layer.gate,
-                                  layer.w_uk, layer.w_uv, out, ws, dev_status=layer.status)
+                                  layer.table[1:].contiguous(), layer.lens[1:].contiguous(), max(layer.most[1:]),
+                                  *layer.gate, layer.w_uk, layer.w_uv, out, ws, dev_status=layer.status)
     joint = torch.cat([prefix.expand(sequences, -1), layer.table[1:, :pages_of(steps)]], 1).contiguous()
-    shared = apart(out, layer.dense(q, joint, layer.lens[1:] + document, document + layer.longest))
+    shared = apart(out, layer.dense(q, joint, layer.lens[1:] + document, document + steps))
 
     # the document's own sequence goes on, over its best pages
-    layer.longest = document
     one = torch.empty((1, HEADS, D_NOPE), dtype=torch.bfloat16, device="cuda")
     chosen = layer.ints(1, budget)
     ws = layer.bytes(_lib.eg_mla_decode_sparse_workspace_size(layer.dims, 1, max_pages, budget))
@@ -136,7 +135,7 @@ def main(document=1000, sequences=12, steps=70, budget=8):
         layer.plan([1] + [0] * sequences)
         q = layer.append()[:1].contiguous()
         layer.summarise()
-        _lib.eg_mla_decode_sparse(layer.dims, q, *layer.cache(), layer.table[:1], layer.lens[:1], layer.longest,
+        _lib.eg_mla_decode_sparse(layer.dims, q, *layer.cache(), layer.table[:1], layer.lens[:1], layer.most[0],
                                   layer.summary, budget, 1, 1, *layer.gate, layer.w_uk, layer.w_uv, one, ws,
                                   selected=chosen, dev_status=layer.status)
     kept = chosen[0][chosen[0] >= 0].long()

@@ -177,3 +177,10 @@ def alternating(which, graph, rounds=60):
 @pytest.mark.parametrize("which", ["shared", "sparse"])
 def test_calls_in_turn_on_one_workspace(gpu_lib, which, graph):
     alternating(which, graph)
+
+
+@pytest.mark.parametrize("kw", [dict(document=30, sequences=3, steps=5), dict(document=1, sequences=1, steps=70, budget=2),
+                                dict(document=130, sequences=2, steps=1, budget=64)])
+def test_example_with_a_short_document(gpu_lib, kw):
+    shared, sparse, all_free, status = example().main(**kw)
+    assert shared <= 1e-2 and sparse == 0.0 and all_free and status == 0
