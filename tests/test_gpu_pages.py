@@ -580,3 +580,98 @@ def test_a_score_that_underflows_equals_zero(gpu_lib, name):
     p.dc.q[0, :, case.dims.d_nope] = 1.0
     p.summary[int(case.block_table[0, 3]), case.dims.d_c] = -1e-30
     assert p.run(6)[0].tolist() == [0, 1, 2, 3, 4, 19]
+
+
+def test_plan_can_be_captured(gpu_lib):
+    """A captured plan serves the lengths that its inputs hold at each replay."""
+    cases = [plan_case(seed, 700, 900, spare=spare, width=30) for seed, spare in ((21, -20), (22, 5), (23, 0))]
+    slots = max(sum(max(n, 0) for n in c[0]) for c in cases)
+    most = max(len(c[3]) for c in cases)
+    cases = [(*c[:3], np.concatenate([c[3], np.full(most - len(c[3]), 77)]), c[4]) for c in cases]
+    new, lens, table, stack, free = (dev(x) for x in (*cases[0][:4], [0]))
+    lens_out, left, cu, pos, at, status = dev([0] * 700), dev([0]), dev([0] * 701), dev([0] * 700), dev([0] * slots), dev([0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _lib.eg_mla_page_plan(new, lens, lens_out, table, stack, free, left, cu, pos, at, dev_status=status)
+    for case in cases:
+        for dst, src in zip((new, lens, table, stack, free, status), (*case[:4], [case[4]], [0])):
+            dst.copy_(dev(src))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, st = plan_reference(*case, slots)
+        got = dict(seq_lens=lens_out, table=table, stack=stack, free=left, cu=cu, positions=pos, slots=at)
+        assert_plan({k: v.cpu().numpy() for k, v in got.items()}, want)
+        assert int(status.item()) == st
+
+
+class Wide(Sparse):
+    """Long sequences over a few physical pages, whose summaries are drawn."""
+
+    def __init__(self, name, lens, seed=1):
+        small = make(name, (64 * 9, 64 * 6))
+        super().__init__(small)
+        d, r, B = small.dims, np.random.default_rng(seed), len(lens)
+        held = small.block_table[:, :6].reshape(-1)
+        q = r.standard_normal((B, d.num_heads, d.d_nope + d.d_rope)).astype(np.float32)
+        self.case = dataclasses.replace(
+            small, block_table=held[r.integers(0, len(held), (B, pages_of(max(lens))))].astype(np.int32),
+            seq_lens=np.array(lens, np.int32), q=synth.f32_to_bf16_bits(q) if d.dtype == "bf16" else q)
+        dc = self.dc
+        dc.q = device.to_device_array(self.case.q, d.dtype, "cuda")
+        dc.block_table, dc.seq_lens = dev(self.case.block_table).view(B, -1), dev(lens)
+        dc.out = torch.empty((B, d.num_heads, d.d_v), dtype=dc.out.dtype, device="cuda")
+        self.summary = torch.from_numpy(r.standard_normal((small.num_pages, d.d_c + d.d_rope)).astype(np.float32)).cuda()
+        self.longest = max(lens)
+
+    def check(self, budget, first, last, splits=0):
+        """The selection; of pages with the same summary the first ones; the decode's bits."""
+        case, dc = self.case, self.dc
+        sel = self.run(budget, first, last, splits)
+        assert dc.read_status() == 0
+        check_selection(case, sel, self.summary.cpu().numpy().astype(np.float64), budget, first, last)
+        for b, L in enumerate(case.seq_lens):
+            n, taken = pages_of(int(L)), set(sel[b].tolist())
+            if n <= budget:
+                continue
+            left = {}
+            for i in range(first, n - last):
+                page = int(case.block_table[b, i])
+                if i not in taken:
+                    left[page] = i
+                else:
+                    assert page not in left, (b, i, left[page])
+        count = (sel >= 0).sum(1)
+        table = np.where(sel >= 0, np.take_along_axis(case.block_table, np.maximum(sel, 0), 1), 0)
+        lens = [int(L) - (pages_of(int(L)) - int(k)) * P for L, k in zip(case.seq_lens, count)]
+        ws = torch.empty(_lib.eg_mla_decode_workspace_size(dc.dims, case.batch, splits), dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(dc.out)
+        _lib.eg_mla_decode(dc.dims, dc.q, dc.c_pool, dc.kr_pool, dc.id_pool, dev(table).view(table.shape), dev(lens),
+                           max(lens), dc.gate_table, dc.ln_gamma, dc.ln_beta, dc.w_uk, dc.w_uv, out, ws, splits,
+                           dc.status)
+        torch.cuda.synchronize()
+        assert dc.read_status() == 0 and torch.equal(out, dc.out)
+
+
+@pytest.mark.parametrize("name", ["gate256", "none512", "fp32_132", "fp32_512"])
+@pytest.mark.parametrize("budget,first,last", [(9, 1, 1), (64, 0, 2)])
+def test_selection_in_several_rounds_and_blocks(gpu_lib, name, budget, first, last):
+    """More groups of pages than blocks: 32 sequences of up to 512 pages (four rounds of a
+    block, two where a row is read in two parts), and fewer, of 900 (two)."""
+    r = np.random.default_rng(6)
+    long = [int(x) for x in r.integers(400 * P, 512 * P, 31)] + [512 * P]
+    Wide(name, long).check(budget, first, last)
+    Wide(name, long[:20] + [7 * P, 70 * P + 1, 0, 140 * P - 3], seed=2).check(budget, first, last)
+    Wide(name, [900 * P, 899 * P + 1, 200 * P, 13] * 3, seed=3).check(budget, first, last)
+
+
+@pytest.mark.parametrize("name", ["gate192", "none512", "fp32_132"])
+@pytest.mark.parametrize("budget", [20, 2100, 4250, 4600])
+def test_selection_from_more_pages_than_shared_memory_holds(gpu_lib, name, budget):
+    """More than 4,096 ranked pages, with equal scores on both sides of that number."""
+    Wide(name, [4700 * P - 5, 4300 * P, 100 * P]).check(budget, 1, 2)
+
+
+@pytest.mark.parametrize("name", ["gate192", "gate256", "none512", "fp32_64"])
+@pytest.mark.parametrize("splits", [1, 3, 40, 300])
+def test_sparse_decode_with_a_number_of_splits(gpu_lib, name, splits):
+    Wide(name, [30 * P, 1, 41 * P - 7, 8 * P]).check(9, 1, 1, splits)

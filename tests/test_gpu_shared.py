@@ -277,3 +277,59 @@ def test_a_prefix_where_the_bound_is_zero_is_reported(gpu_lib, length, gate_op):
     got = s.run()
     assert s.dc.read_status() == _lib.EG_MLA_ERR_OUT_OF_RANGE
     check(got, reference(case))   # taken as 0
+
+
+def exact(case, q, prefix, table, lens):
+    """The definition in 64 bits from the cached rows: `prefix` rows of the cache, then
+    each sequence's own."""
+    d = case.dims
+    c, kr, ids = orc.appended_pools(case)
+    rows = [torch.from_numpy(orc.widen(a, "bf16").reshape(-1, a.shape[-1])).cuda() for a in (c, kr)]
+    if d.gate:
+        g = torch.from_numpy(orc.widen(case.gate_table, "bf16")).cuda()[torch.from_numpy(ids.reshape(-1)).long().cuda().clamp(0, d.vocab - 1)]
+        x = rows[0] + g if d.gate_op == "add_ln" else rows[0] * g
+        if d.gate_op != "mul":
+            x = x - x.mean(-1, keepdim=True)
+            x = x / (x.square().mean(-1, keepdim=True) + d.ln_eps).sqrt()
+            x = x * torch.from_numpy(case.ln_gamma).cuda().double() + torch.from_numpy(case.ln_beta).cuda().double()
+        rows[0] = x
+    w_uk, w_uv = (torch.from_numpy(orc.widen(w, "bf16")).cuda() for w in (case.w_uk, case.w_uv))
+    q = q.double()
+    qa = torch.cat([torch.einsum("bhd,hdc->bhc", q[..., :d.d_nope], w_uk), q[..., d.d_nope:]], -1)
+    out = []
+    for b, n in enumerate(lens):
+        at = torch.cat([prefix, table[b, torch.arange(n) // 64].long().cpu() * 64 + torch.arange(n) % 64]).cuda()
+        z = rows[0][at]
+        p = (qa[b] @ torch.cat([z, rows[1][at]], -1).T * orc.softmax_scale(d)).softmax(-1)
+        out.append(torch.einsum("hc,hdc->hd", p @ z, w_uv))
+    return torch.stack(out).cpu().numpy()
+
+
+@pytest.mark.parametrize("d_c,gate_op", [(192, "none"), (256, "mul_ln"), (256, "mul")])
+@pytest.mark.parametrize("batch,prefix,splits", [(3, 600 * 64 - 17, 0), (3, 600 * 64, 400), (1, 300 * 64 + 1, 200),
+                                                 (70, 310 * 64 - 1, 0), (70, 100 * 64 + 5, 1000)])
+def test_long_prefixes_and_many_partials(gpu_lib, batch, prefix, splits, d_c, gate_op):
+    """Prefixes of hundreds of pages (a few physical ones, many times), up to 300 partials
+    of a sequence."""
+    case = make(15 * 64, (100,) * 2, d_c=d_c, gate_op=gate_op)
+    r = np.random.default_rng(prefix + batch)
+    s = Shared(case)
+    dc = s.dc
+    pages = (prefix + 63) // 64
+    held = s.prefix_table.cpu()
+    prefix_table = held[torch.from_numpy(r.integers(0, 15, pages))]
+    lens = [int(x) for x in r.integers(0, 130, batch)]
+    table = held[torch.from_numpy(r.integers(0, 15, (batch, 3)))]
+    gen = torch.Generator(device="cuda").manual_seed(batch)
+    q = torch.randn((batch, 16, 192), generator=gen, device="cuda").bfloat16()
+    out = torch.full((batch, 16, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((_lib.eg_mla_decode_shared_workspace_size(dc.dims, batch, prefix, splits),), 255,
+                    dtype=torch.uint8, device="cuda")
+    n = torch.tensor([prefix], dtype=torch.int32, device="cuda")
+    _lib.eg_mla_decode_shared(dc.dims, q, dc.c_pool, dc.kr_pool, dc.id_pool, prefix_table.cuda(), n, prefix,
+                              table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), 192, dc.gate_table,
+                              dc.ln_gamma, dc.ln_beta, dc.w_uk, dc.w_uv, out, ws, splits, dc.status)
+    torch.cuda.synchronize()
+    assert dc.read_status() == 0
+    at = torch.arange(prefix)
+    check(device.output_f64(out), exact(case, q, prefix_table[at // 64].long() * 64 + at % 64, table, lens))
