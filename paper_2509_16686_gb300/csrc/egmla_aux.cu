@@ -299,6 +299,9 @@ prologue_tc_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
   const int mt = (d_c + kPmTile - 1) / kPmTile, nbg = (batch + nt - 1) / nt;
   const int ntiles = q != nullptr ? H * mt * nbg : 0;   // (the cache-read test entry: the schedule only)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // `chain`: the trigger comes after the wait, in every block.  The next kernel, the one
+  // after it and, in the shared-prefix decode, the combine's copy of W_UV read inputs
+  // before their own waits, and this order alone completes what came before the call.
   const bool chain = EXTRA && extra.chain != 0;
   if (blockIdx.x == 0 || blockIdx.x > static_cast<unsigned>(ntiles)) {
     if (!chain) grid_launch_dependents();

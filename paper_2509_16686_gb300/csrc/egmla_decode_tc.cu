@@ -786,9 +786,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (lane == 0) {
       // The split combine may take its place once every CTA's last page is
-      // requested, a few microseconds before this kernel ends.  Never before this
-      // kernel's wait: the combine copies W_UV before its own, and only this wait
-      // stands for the kernel before the call, which may write W_UV.  (At the start it
+      // requested, a few microseconds before this kernel ends.  Never before the
+      // kernel before the call, which may write W_UV, is complete: the combine copies
+      // W_UV before its own wait.  This kernel's wait stands for that; beside the
+      // attention over a shared prefix, where the wait comes at the end, the
+      // absorption's does, after which alone it let the gate (and that the attention,
+      // and that this kernel) start.  (At the start it
       // would crowd its blocks onto the first SMs to free up: 128 ragged
       // sequences 69.8 us against 68.2).  128 at d_c 512 119.7 -> 118.5 us, 32 x
       // 4K 37.7 -> 37.2, 64 x 8K layer 102.4 -> 101.5 (against a trigger at the

@@ -23,13 +23,17 @@ namespace egmla {
 //    the split combine copies W_UV, the fp32 one brings it to L2, the projection
 //    GEMM copies its weights.  The caller's kernel before the call may write
 //    W_UV: the combine must not start before that one is complete, so the bf16
-//    split-KV kernel triggers a separate combine only after its own wait.  (An
+//    split-KV kernel triggers a separate combine only after its own wait, or, beside
+//    the attention over a shared prefix, knows it complete when it starts (below).  (An
 //    L2 prefetch reads nothing that could be old.  The first projection's weights
 //    must not be written by the kernel directly before the layer call.)
 //  - a kernel may stand beside the one before it where it needs nothing of that one:
 //    that one lets it start only after its own wait (so that all before it is
 //    complete), and it waits at its end instead of its start (`beside`), so that its
-//    completion stands for both.
+//    completion stands for both.  In the shared-prefix decode the absorption triggers
+//    after its wait, and gate, attention and split-KV kernel each start after the
+//    trigger of the one before: whatever came before the call is complete when any of
+//    them starts.  The combine's early copy of W_UV rests on that too.
 // A kernel lets its successor start early (grid_launch_dependents) where that was
 // measured to pay: mostly where the successor's blocks take a whole SM each, since
 // smaller blocks, started early, crowd onto the first SMs to free up (the R0
