@@ -191,8 +191,8 @@ __global__ void __launch_bounds__(32 * kSgWarps, 4) shared_gate_kernel(const Sha
 // S(j + 1) overwrites P(j - 1) after the MMA that reads it.
 //
 // Bound by the tensor pipe in steady state: 0.705 us for a page (9.4 MFLOP; over all SMs
-// as fast as the measured bf16 peak).  64 sequences over 32K tokens at d_c 256: 36 us
-// (cold, alone; tensor pipe 45 % of it), since the own tokens' kernel has a part of the
+// as fast as the measured bf16 peak).  64 sequences over 32K tokens at d_c 256: 37 us
+// (cold, alone; tensor pipe 43 % of it), since the own tokens' kernel has a part of the
 // SMs, and a CTA takes 7 us besides its pages: queries into tensor memory, the first
 // pages and scores, the partial.
 constexpr int kSaSoftWarps = 8;
