@@ -675,3 +675,24 @@ def test_selection_from_more_pages_than_shared_memory_holds(gpu_lib, name, budge
 @pytest.mark.parametrize("splits", [1, 3, 40, 300])
 def test_sparse_decode_with_a_number_of_splits(gpu_lib, name, splits):
     Wide(name, [30 * P, 1, 41 * P - 7, 8 * P]).check(9, 1, 1, splits)
+
+
+@pytest.mark.parametrize("name", ["gate256", "none512", "fp32_none"])
+def test_pages_past_32_bits_of_a_pool(gpu_lib, name):
+    """Pages whose elements and bytes lie past 2^31 and 2^32 in the latent pool: the same bits."""
+    p = Sparse(make(name, LENS))
+    dc, n = p.dc, p.case.num_pages
+    summary = torch.from_numpy(p.summarise())
+    sel = p.run(9, 1, 1)
+    out = dc.out.clone()
+    shift = 2 ** 31 // (P * p.case.dims.d_c) + 1
+    for pool in ("c_pool", "kr_pool", "id_pool"):
+        small = getattr(dc, pool)
+        big = torch.zeros((shift + n, *small.shape[1:]), dtype=small.dtype, device="cuda")
+        big[shift:] = small
+        setattr(dc, pool, big)
+    dc.block_table = dc.block_table + shift
+    p.summary = torch.full((shift + n, p.summary.shape[1]), -77.0, device="cuda")
+    assert torch.equal(torch.from_numpy(p.summarise()[shift:]), summary)
+    assert np.array_equal(p.run(9, 1, 1), sel) and torch.equal(dc.out, out)
+    assert dc.read_status() == 0

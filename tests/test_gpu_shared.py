@@ -333,3 +333,21 @@ def test_long_prefixes_and_many_partials(gpu_lib, batch, prefix, splits, d_c, ga
     assert dc.read_status() == 0
     at = torch.arange(prefix)
     check(device.output_f64(out), exact(case, q, prefix_table[at // 64].long() * 64 + at % 64, table, lens))
+
+
+@pytest.mark.parametrize("gate_op", ["none", "mul_ln"])
+def test_pages_past_32_bits_of_a_pool(gpu_lib, gate_op):
+    """Pages whose elements and bytes lie past 2^31 and 2^32 in the latent pool: the same bits."""
+    s = Shared(make(333, (4, 90, 0), gate_op=gate_op))
+    dc = s.dc
+    want, n = s.run(), dc.c_pool.shape[0]
+    shift = 2 ** 31 // (64 * 256) + 1
+    for pool in ("c_pool", "kr_pool", "id_pool"):
+        small = getattr(dc, pool)
+        big = torch.zeros((shift + n, *small.shape[1:]), dtype=small.dtype, device="cuda")
+        big[shift:] = small
+        setattr(dc, pool, big)
+    s.prefix_table, s.table = s.prefix_table + shift, s.table + shift
+    s.out.fill_(float("nan"))
+    assert np.array_equal(s.run(), want)
+    assert dc.read_status() == 0
