@@ -25,6 +25,10 @@
  *     sequences that share a prefix, which is read once for eight of them;
  *     eg_mla_page_summary keeps the mean key of every full page, by which
  *     eg_mla_decode_sparse decodes over the pages that matter most to the query.
+ *   - between the projections and the cache: eg_mla_rope rotates the queries and keys of
+ *     packed tokens; eg_mla_append_latent_q8 writes tokens into a cache that holds the
+ *     latent in 8 bits, eg_mla_read_latent_q8 reads them back as rows, and
+ *     eg_mla_decode_q8 decodes over it.
  *
  * Conventions shared by every call:
  *   - Every pointer argument except `dims`, `bytes_out` and `out_splits` is a
@@ -395,6 +399,145 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
                          const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
                          const void* w_uv, void* out, int32_t* selected, int32_t num_splits, void* workspace,
                          size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_rope - the rotary embedding of packed tokens' queries and keys (Appendix C
+ * Eqs. 9-10; the listing of Appendix E): what eg_mla_prefill, eg_mla_decode and the
+ * appends take as already rotated.
+ *
+ * Packed token k is token k - cu_seqlens[b] of the sequence b with cu_seqlens[b] <= k <
+ * cu_seqlens[b + 1], at position t = positions[b] + k - cu_seqlens[b] (as
+ * eg_mla_page_plan writes both); with cu_seqlens NULL sequence k has the one token k, at
+ * positions[k].  The last d_rope entries of every head of q, and k, are turned pair by
+ * pair, i < d_rope / 2:
+ *   (x, y) -> m (x cos t f_i - y sin t f_i,  x sin t f_i + y cos t f_i)
+ * Pairs are entries (2i, 2i + 1) (EG_MLA_ROPE_INTERLEAVED, the paper's) or (i, i +
+ * d_rope / 2) (EG_MLA_ROPE_HALF).  The first d_nope entries of a head are copied.
+ * f_i = theta^(-2i / d_rope), scaled for contexts s = `factor` times the trained one:
+ *   EG_MLA_ROPE_UNSCALED  as it is
+ *   EG_MLA_ROPE_LINEAR    f_i / s (position interpolation, arXiv 2306.15595)
+ *   EG_MLA_ROPE_NTK       theta s^(d_rope / (d_rope - 2)) in place of theta
+ *   EG_MLA_ROPE_YARN      f_i ((1 - g) / s + g) with g = (original_len f_i / (2 pi) -
+ *                         beta_slow) / (beta_fast - beta_slow) kept within 0 and 1:
+ *                         "NTK by parts" (YaRN, arXiv 2309.00071, Section 3.2)
+ * `inverse` turns the other way (times m): the transposed matrix, which takes the
+ * gradients of the rotated rows to those of q and k.
+ */
+typedef enum { EG_MLA_ROPE_INTERLEAVED = 0, EG_MLA_ROPE_HALF = 1 } eg_mla_rope_layout;
+typedef enum {
+  EG_MLA_ROPE_UNSCALED = 0,
+  EG_MLA_ROPE_LINEAR = 1,
+  EG_MLA_ROPE_NTK = 2,
+  EG_MLA_ROPE_YARN = 3
+} eg_mla_rope_scaling;
+
+typedef struct {
+  int32_t layout;        /* eg_mla_rope_layout */
+  int32_t scaling;       /* eg_mla_rope_scaling */
+  int32_t inverse;       /* nonzero: turn back */
+  int32_t original_len;  /* YARN: the trained context, > 0 */
+  float theta;           /* <= 0 selects 10000; else >= 1 */
+  float factor;          /* s >= 1; ignored for UNSCALED */
+  float beta_fast;       /* YARN: <= 0 selects 32 */
+  float beta_slow;       /* YARN: <= 0 selects 1; below beta_fast */
+  float magnitude;       /* m; <= 0 selects 1, with YARN 0.1 ln s + 1 */
+} eg_mla_rope_dims;
+
+/*
+ *   dims         num_heads, d_nope (>= 0), d_rope (even, at most 256) and dtype are used
+ *   q, q_out     [tokens, num_heads, d_nope + d_rope], model dtype, tokens q_stride and
+ *                q_out_stride elements apart (>= num_heads (d_nope + d_rope)); both NULL:
+ *                no queries.  q_out may be q (then with the same stride: only the
+ *                rotated entries are written); they must not overlap otherwise
+ *   k, k_out     [tokens, d_rope], tokens k_stride and k_out_stride elements apart, likewise
+ *   cu_seqlens   [batch + 1] int32, non-decreasing from 0, or NULL (then tokens = batch)
+ *   positions    [batch] int32: of each sequence's first token; a negative one leaves
+ *                the sequence's rows of q_out and k_out as they were.  NULL: 0 (not with
+ *                cu_seqlens NULL)
+ *   tokens       rows of q and k; those from cu_seqlens[batch] on are left as they were
+ * Angles are reduced as 64-bit fractions of a turn, which keeps them to 2^-32 of a turn
+ * at any position; sums are fp32, rounded once.  16-byte alignment of rows, heads and
+ * pointers is not needed but faster.  Device errors: EG_MLA_ERR_OUT_OF_RANGE for
+ * cu_seqlens that begin above 0 or decrease (rows that belong to no sequence are left).
+ */
+int eg_mla_rope(const eg_mla_dims* dims, const eg_mla_rope_dims* rope, const void* q, int64_t q_stride, void* q_out,
+                int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride,
+                const int32_t* cu_seqlens, const int32_t* positions, int32_t batch, int32_t tokens,
+                int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_append_latent_q8 - new tokens written into a paged cache that holds the latent
+ * in 8 bits: d_c + 4 bytes a token for c^KV instead of 2 d_c (bf16), with k^R and the id
+ * as in eg_mla_append_latent's cache.
+ *
+ * For a latent row c with a = max_f |c_f|:
+ *   scale = 2^e, e the least integer with a <= 448 2^e, at least -100 (at most 119)
+ *   code_f = e4m3(c_f / scale), to the nearest, ties to even
+ * (448 is e4m3's largest number).  A power of two costs a floating format no precision and
+ * makes scale x code exact in bf16 and in fp32.  A row with an infinity or a NaN has the
+ * scale NaN and reads back as NaN; magnitudes above 448 2^119 as 448 2^119.
+ *
+ *   dims         page_size 64, d_c (a multiple of 16, at most 512), d_rope (at most 256,
+ *                rows a multiple of 16 bytes) and dtype are used
+ *   c8_pool      [num_pages, 64, d_c] e4m3 bytes, written; 16-byte aligned
+ *   scale_pool   [num_pages, 64] fp32, written; 16-byte aligned for eg_mla_decode_q8
+ *   krope_pool   [num_pages, 64, d_rope] model dtype, written; 16-byte aligned
+ *   id_pool      [num_pages, 64] int32, written; may be NULL (then ids_new is ignored)
+ *   c_new        [tokens, d_c], tokens c_stride elements apart; krope_new [tokens, d_rope],
+ *                krope_stride apart: model dtype, rows 16-byte aligned; ids_new [tokens]
+ *                int32, may be NULL (then id_pool is left as it was)
+ *   cu_seqlens, positions, batch, tokens: as for eg_mla_rope: prompts, or with cu_seqlens
+ *                NULL a token per sequence.  Packed token k is written at its position's
+ *                slot; a negative positions[b] skips the sequence
+ *   block_table  [batch, max_pages_per_seq] int32
+ * Device errors: a position past max_pages_per_seq pages or a page id outside [0,
+ * num_pages) (that token is skipped), or cu_seqlens as for eg_mla_rope, as
+ * EG_MLA_ERR_OUT_OF_RANGE.  Two tokens of one call must not share a slot.
+ */
+int eg_mla_append_latent_q8(const eg_mla_dims* dims, void* c8_pool, float* scale_pool, void* krope_pool,
+                            int32_t* id_pool, const void* c_new, int64_t c_stride, const void* krope_new,
+                            int64_t krope_stride, const int32_t* ids_new, const int32_t* cu_seqlens,
+                            const int32_t* positions, const int32_t* block_table, int32_t max_pages_per_seq,
+                            int32_t batch, int32_t tokens, int32_t num_pages, int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_read_latent_q8 - cached tokens read back as packed rows, in the form that
+ * eg_mla_append_latent and eg_mla_prefill take: c = scale x code (exact), k^R and ids.
+ * Row k is the token of sequence b at logical position positions[b] + k - cu_seqlens[b]
+ * (positions NULL: each sequence from its start).
+ *
+ *   c_out        [tokens, d_c] model dtype, tokens c_stride elements apart, written
+ *   krope_out    [tokens, d_rope], krope_stride apart, written; may be NULL
+ *   ids_out      [tokens] int32, written; may be NULL
+ *   the others   as for eg_mla_append_latent_q8.  Rows from cu_seqlens[batch] on, of a
+ *                sequence with a negative position and of tokens that a device error
+ *                skips are left as they were
+ */
+int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const float* scale_pool,
+                          const void* krope_pool, const int32_t* id_pool, const int32_t* cu_seqlens,
+                          const int32_t* positions, const int32_t* block_table, int32_t max_pages_per_seq,
+                          void* c_out, int64_t c_stride, void* krope_out, int64_t krope_stride, int32_t* ids_out,
+                          int32_t batch, int32_t tokens, int32_t num_pages, int32_t* dev_status, void* stream);
+
+/*
+ * eg_mla_decode_q8 - eg_mla_decode over a cache in 8 bits: the latent of token j is
+ * scale_j x code_j.  The result is eg_mla_decode's over a cache of the values that
+ * eg_mla_read_latent_q8 gives, to the bit.
+ *
+ *   dims         those of eg_mla_decode with d_c a multiple of 16; max_seq_len at most
+ *                2^31 - 64
+ *   c8_pool, scale_pool: as eg_mla_append_latent_q8 writes them (a scale that is not a
+ *                power of two between 2^-100 and 2^119 or NaN is not supported, nor are
+ *                NaN codes under another scale than NaN); both 16-byte aligned
+ *   the others   as for eg_mla_decode, workspace too (eg_mla_decode_workspace_size)
+ * Device errors: as for eg_mla_decode.
+ */
+int eg_mla_decode_q8(const eg_mla_dims* dims, const void* q, const void* c8_pool, const float* scale_pool,
+                     const void* krope_pool, const int32_t* id_pool, const int32_t* block_table,
+                     int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, int32_t batch,
+                     int32_t num_pages, const void* gate_table, const float* ln_gamma, const float* ln_beta,
+                     const void* w_uk, const void* w_uv, void* out, int32_t num_splits, void* workspace,
+                     size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* Size of the static device scratch array behind eg_mla_decode_static. */
 #define EG_MLA_STATIC_SCRATCH_BYTES ((size_t)16 << 20)

@@ -35,6 +35,8 @@ EG_MLA_GATE_NONE = 0
 EG_MLA_GATE_MUL_LN = 1
 EG_MLA_GATE_MUL = 2      # ablation: LayerNorm removed
 EG_MLA_GATE_ADD_LN = 3   # ablation: (*) replaced by +
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 GATE_MODES = {"mul_ln": EG_MLA_GATE_MUL_LN, "mul": EG_MLA_GATE_MUL, "add_ln": EG_MLA_GATE_ADD_LN}
 
 EXPORTED = [
@@ -49,6 +51,10 @@ EXPORTED = [
     "eg_mla_decode_sparse",
     "eg_mla_page_plan",
     "eg_mla_page_summary",
+    "eg_mla_rope",
+    "eg_mla_append_latent_q8",
+    "eg_mla_read_latent_q8",
+    "eg_mla_decode_q8",
     "eg_mla_step",
     "eg_mla_decode_r0_workspace_size",
     "eg_mla_decode_r0",
@@ -83,6 +89,20 @@ class EgMlaDims(ctypes.Structure):
         ("gate_mode", ctypes.c_int32),
         ("softmax_scale", ctypes.c_float),
         ("ln_eps", ctypes.c_float),
+    ]
+
+
+class EgMlaRopeDims(ctypes.Structure):
+    _fields_ = [
+        ("layout", ctypes.c_int32),
+        ("scaling", ctypes.c_int32),
+        ("inverse", ctypes.c_int32),
+        ("original_len", ctypes.c_int32),
+        ("theta", ctypes.c_float),
+        ("factor", ctypes.c_float),
+        ("beta_fast", ctypes.c_float),
+        ("beta_slow", ctypes.c_float),
+        ("magnitude", ctypes.c_float),
     ]
 
 
@@ -123,6 +143,15 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.eg_mla_page_plan.restype = ctypes.c_int
     lib.eg_mla_page_summary.argtypes = [D, P, P, P, P, I32, P, I32, P, I32, I32, I32, P, P, P, P, P, P]
     lib.eg_mla_page_summary.restype = ctypes.c_int
+    I64 = ctypes.c_int64
+    lib.eg_mla_rope.argtypes = [D, ctypes.POINTER(EgMlaRopeDims), P, I64, P, I64, P, I64, P, I64, P, P, I32, I32, P, P]
+    lib.eg_mla_rope.restype = ctypes.c_int
+    lib.eg_mla_append_latent_q8.argtypes = [D, P, P, P, P, P, I64, P, I64, P, P, P, P, I32, I32, I32, I32, P, P]
+    lib.eg_mla_append_latent_q8.restype = ctypes.c_int
+    lib.eg_mla_read_latent_q8.argtypes = [D, P, P, P, P, P, P, P, I32, P, I64, P, I64, P, I32, I32, I32, P, P]
+    lib.eg_mla_read_latent_q8.restype = ctypes.c_int
+    lib.eg_mla_decode_q8.argtypes = [D, P, P, P, P, P, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P, P]
+    lib.eg_mla_decode_q8.restype = ctypes.c_int
     lib.eg_mla_step.argtypes = [D, P, P, P, P, P, P, P, P, P, I32, P, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ,
                                 P, P]
     lib.eg_mla_step.restype = ctypes.c_int
@@ -222,6 +251,59 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _shaped(t: Optional[torch.Tensor], shape: tuple, name: str) -> None:
     if t is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {shape} expected, got {tuple(t.shape)}")
+
+
+_MODEL_DTYPES = {EG_MLA_BF16: torch.bfloat16, EG_MLA_FP32: torch.float32}
+
+
+def _typed(t: Optional[torch.Tensor], dtypes, name: str) -> None:
+    if t is not None and t.dtype not in dtypes:
+        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+
+
+def _token_rows(t: Optional[torch.Tensor], shape: tuple, dtype, name: str):
+    """Pointer and token stride of rows [tokens, ...] that are dense but for the first dimension."""
+    if t is None:
+        return None, 0
+    _shaped(t, shape, name)
+    _typed(t, (dtype,), name)
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    width = 1
+    for n, step in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
+        if n > 1 and step != width:
+            raise ValueError(f"{name}: rows that are dense expected")
+        width *= n
+    stride = t.stride(0) if shape[0] > 1 else width
+    if stride < width:
+        raise ValueError(f"{name}: rows that overlap")
+    return t.data_ptr(), stride
+
+
+def _packed(tokens: int, positions, cu_seqlens) -> tuple:
+    """(cu_seqlens, positions, batch) of packed tokens as pointers, their shapes checked."""
+    if cu_seqlens is None and positions is None:
+        raise ValueError("positions or cu_seqlens expected")
+    batch = cu_seqlens.shape[0] - 1 if cu_seqlens is not None else tokens
+    _shaped(positions, (batch,), "positions")
+    for name, t in (("positions", positions), ("cu_seqlens", cu_seqlens)):
+        _typed(t, (torch.int32,), name)
+    return _ptr(cu_seqlens), _ptr(positions), batch
+
+
+def _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table) -> tuple:
+    """Pointers of a cache in 8 bits, its shapes and types checked."""
+    pages = c8_pool.shape[0]
+    _shaped(c8_pool, (pages, dims.page_size, dims.d_c), "c8_pool")
+    _shaped(scale_pool, (pages, dims.page_size), "scale_pool")
+    _shaped(krope_pool, (pages, dims.page_size, dims.d_rope), "krope_pool")
+    _shaped(id_pool, (pages, dims.page_size), "id_pool")
+    _typed(c8_pool, (torch.float8_e4m3fn, torch.uint8), "c8_pool")
+    _typed(scale_pool, (torch.float32,), "scale_pool")
+    _typed(krope_pool, (_MODEL_DTYPES.get(dims.dtype),), "krope_pool")
+    for name, t in (("id_pool", id_pool), ("block_table", block_table)):
+        _typed(t, (torch.int32,), name)
+    return _ptr(c8_pool), _ptr(scale_pool), _ptr(krope_pool), _ptr(id_pool)
 
 
 def _stream(stream) -> int:
@@ -384,6 +466,76 @@ def eg_mla_page_plan(new_tokens, seq_lens, seq_lens_out, block_table, free_pages
         _ptr(free_pages), free_pages.shape[0], _ptr(free_count), _ptr(free_count_out), _ptr(cu_seqlens),
         _ptr(positions), _ptr(slots), slots.shape[0] if slots is not None else 0, _ptr(dev_status), _stream(stream))
     _check(code, "eg_mla_page_plan")
+
+
+def make_rope(layout: str = "interleaved", scaling: str = "none", theta: float = 10000.0, factor: float = 1.0,
+              original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: float = 0.0,
+              inverse: bool = False) -> EgMlaRopeDims:
+    """layout: "interleaved" or "half"; scaling: "none", "linear", "ntk" or "yarn" (see include/egmla.h)."""
+    return EgMlaRopeDims(ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], 1 if inverse else 0, original_len, theta, factor,
+                         beta_fast, beta_slow, magnitude)
+
+
+def eg_mla_rope(dims: EgMlaDims, rope: EgMlaRopeDims, q, q_out, k, k_out, positions=None, cu_seqlens=None,
+                dev_status=None, stream=None) -> None:
+    """Rotary embedding of packed tokens' queries [tokens, H, d_nope + d_rope] and keys [tokens, d_rope], whose
+    tokens may be apart (a slice of wider rows); q_out may be q, k_out k, and either pair None: see include/egmla.h."""
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
+        raise ValueError("q with q_out or k with k_out expected")
+    tokens = (q if q is not None else k).shape[0]
+    rows = []
+    for name, t, shape in (("q", q, (dims.num_heads, dims.d_nope + dims.d_rope)),
+                           ("q_out", q_out, (dims.num_heads, dims.d_nope + dims.d_rope)),
+                           ("k", k, (dims.d_rope,)), ("k_out", k_out, (dims.d_rope,))):
+        rows += _token_rows(t, (tokens, *shape), _MODEL_DTYPES.get(dims.dtype), name)
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
+    _check(load().eg_mla_rope(ctypes.byref(dims), ctypes.byref(rope), *rows, cu, pos, batch, tokens, _ptr(dev_status),
+                              _stream(stream)), "eg_mla_rope")
+
+
+def eg_mla_append_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_pool, c_new, krope_new, ids_new,
+                            block_table, positions, cu_seqlens=None, dev_status=None, stream=None) -> None:
+    """New tokens into a cache that holds the latent in 8 bits (c8_pool e4m3 or its bytes), a token per sequence
+    or packed by cu_seqlens; the rows of c_new and krope_new may be apart: see include/egmla.h."""
+    tokens, dtype = c_new.shape[0], _MODEL_DTYPES.get(dims.dtype)
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
+    rows = (*_token_rows(c_new, (tokens, dims.d_c), dtype, "c_new"),
+            *_token_rows(krope_new, (tokens, dims.d_rope), dtype, "krope_new"))
+    _shaped(ids_new, (tokens,), "ids_new")
+    _typed(ids_new, (torch.int32,), "ids_new")
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
+    _shaped(block_table, (batch, block_table.shape[1]), "block_table")
+    _check(load().eg_mla_append_latent_q8(
+        ctypes.byref(dims), *cache, *rows, _ptr(ids_new), cu, pos, _ptr(block_table), block_table.shape[1], batch, tokens,
+        c8_pool.shape[0], _ptr(dev_status), _stream(stream)), "eg_mla_append_latent_q8")
+
+
+def eg_mla_read_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_pool, block_table, c_out, krope_out,
+                          ids_out, positions=None, cu_seqlens=None, dev_status=None, stream=None) -> None:
+    """Cached tokens of a cache in 8 bits as packed rows (krope_out and ids_out may be None): see include/egmla.h."""
+    tokens, dtype = c_out.shape[0], _MODEL_DTYPES.get(dims.dtype)
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
+    rows = (*_token_rows(c_out, (tokens, dims.d_c), dtype, "c_out"),
+            *_token_rows(krope_out, (tokens, dims.d_rope), dtype, "krope_out"))
+    _shaped(ids_out, (tokens,), "ids_out")
+    _typed(ids_out, (torch.int32,), "ids_out")
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
+    _shaped(block_table, (batch, block_table.shape[1]), "block_table")
+    _check(load().eg_mla_read_latent_q8(
+        ctypes.byref(dims), *cache, cu, pos, _ptr(block_table), block_table.shape[1], *rows, _ptr(ids_out), batch, tokens,
+        c8_pool.shape[0], _ptr(dev_status), _stream(stream)), "eg_mla_read_latent_q8")
+
+
+def eg_mla_decode_q8(dims: EgMlaDims, q, c8_pool, scale_pool, krope_pool, id_pool, block_table, seq_lens, max_seq_len,
+                     gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, workspace, num_splits=0, dev_status=None,
+                     stream=None) -> None:
+    """eg_mla_decode over a cache in 8 bits: see include/egmla.h."""
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
+    _check(load().eg_mla_decode_q8(
+        ctypes.byref(dims), _ptr(q), *cache, _ptr(block_table), block_table.shape[1], _ptr(seq_lens), int(max_seq_len),
+        seq_lens.shape[0], c8_pool.shape[0], _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk), _ptr(w_uv),
+        _ptr(out), num_splits, _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dev_status),
+        _stream(stream)), "eg_mla_decode_q8")
 
 
 def make_layer_dims(n_embd: int, rope_theta: float = 10000.0, rms_eps: float = 0.0,

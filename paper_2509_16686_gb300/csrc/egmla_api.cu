@@ -14,6 +14,7 @@
 #include "egmla_common.cuh"
 #include "egmla_kernels.h"
 #include "egmla_ptx.cuh"
+#include "egmla_q8.cuh"
 
 namespace {
 
@@ -80,7 +81,8 @@ bool encode_decode_maps(CUtensorMap (&maps)[2], const eg_mla_dims* d, const void
   std::memset(maps, 0, sizeof(maps));
   const uint64_t rows = static_cast<uint64_t>(num_pages) * d->page_size, dc = d->d_c, dr = d->d_rope;
   const uint32_t tile = d->d_c <= 256 ? 64 : 32;
-  return encode_3d(&maps[0], c_pool, 64, rows, dc / 64, dc, 64, tile, static_cast<uint32_t>(dc / 64)) &&
+  // (a cache in 8 bits, c_pool null here, is copied without a map)
+  return (c_pool == nullptr || encode_3d(&maps[0], c_pool, 64, rows, dc / 64, dc, 64, tile, static_cast<uint32_t>(dc / 64))) &&
          encode_3d(&maps[1], krope_pool, dr, rows, 1, dr, rows * dr, tile, 1);
 }
 
@@ -370,7 +372,8 @@ int shared_workspace(const eg_mla_dims* d, int32_t batch, int32_t max_prefix_len
 
 // eg_mla_decode, preceded by the append of `app` when it is non-null (in the
 // query-absorption kernel's grid), and over the tokens of `prefix` too when that is
-// non-null, or over the pages that `sparse` selects when that is.  Every argument is
+// non-null, or over the pages that `sparse` selects when that is, or over a cache in 8 bits
+// with the scales `scale_pool` when that is.  Every argument is
 // checked before anything is launched (`launch` false: checked only).
 int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, const void* krope_pool,
                 const int32_t* id_pool, const int32_t* block_table, int32_t max_pages_per_seq,
@@ -378,7 +381,8 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
                 const void* gate_table, const float* ln_gamma, const float* ln_beta, const void* w_uk,
                 const void* w_uv, void* out, int32_t num_splits, void* workspace, size_t workspace_bytes,
                 int32_t* dev_status, const egmla::AppendArgs* app, cudaStream_t st, bool early = false,
-                bool launch = true, const Prefix* prefix = nullptr, const Sparse* sparse = nullptr) {
+                bool launch = true, const Prefix* prefix = nullptr, const Sparse* sparse = nullptr,
+                const float* scale_pool = nullptr) {
   egmla::SharedArgs sh;
   if (prefix != nullptr) {
     int32_t splits = 0;
@@ -405,10 +409,12 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
   a.w_uv = w_uv;
   a.out = out;
   a.early = early ? 1 : 0;
+  a.scale_pool = scale_pool;
   if (is_tc_path(dims)) {
     CUtensorMap maps[2];
-    if (!encode_decode_maps(maps, dims, c_pool, krope_pool, num_pages)) return EG_MLA_ERR_CUDA;
-    apply_trace(a);
+    if (!encode_decode_maps(maps, dims, scale_pool == nullptr ? c_pool : nullptr, krope_pool, num_pages))
+      return EG_MLA_ERR_CUDA;
+    if (scale_pool == nullptr) apply_trace(a);   // (no traced build over a cache in 8 bits)
     apply_fault(a);
     CUtensorMap amaps[2];
     if (!encode_absorb_maps(amaps, a, egmla::absorb_tile(a.d_c, a.batch))) return EG_MLA_ERR_CUDA;
@@ -577,6 +583,23 @@ int eg_mla_decode(const eg_mla_dims* dims, const void* q, const void* c_pool, co
   return decode_impl(dims, q, c_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens, max_seq_len,
                      batch, num_pages, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace,
                      workspace_bytes, dev_status, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+int eg_mla_decode_q8(const eg_mla_dims* dims, const void* q, const void* c8_pool, const float* scale_pool,
+                     const void* krope_pool, const int32_t* id_pool, const int32_t* block_table,
+                     int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_seq_len, int32_t batch,
+                     int32_t num_pages, const void* gate_table, const float* ln_gamma, const float* ln_beta,
+                     const void* w_uk, const void* w_uv, void* out, int32_t num_splits, void* workspace,
+                     size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  int rc = check_dims(dims);
+  if (rc == EG_MLA_OK) rc = egmla::q8_check_dims(dims);
+  if (rc != EG_MLA_OK) return rc;
+  if (!countable(max_seq_len)) return EG_MLA_ERR_UNSUPPORTED;
+  if (scale_pool == nullptr || !aligned(scale_pool, 16)) return EG_MLA_ERR_INVALID_ARG;
+  return decode_impl(dims, q, c8_pool, krope_pool, id_pool, block_table, max_pages_per_seq, seq_lens, max_seq_len,
+                     batch, num_pages, gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, num_splits, workspace,
+                     workspace_bytes, dev_status, nullptr, static_cast<cudaStream_t>(stream), false, true, nullptr,
+                     nullptr, scale_pool);
 }
 
 int eg_mla_step(const eg_mla_dims* dims, void* c_pool, void* krope_pool, int32_t* id_pool, const void* c_new,

@@ -22,6 +22,7 @@
 #include "egmla_common.cuh"
 #include "egmla_kernels.h"
 #include "egmla_ptx.cuh"
+#include "egmla_q8.cuh"
 
 namespace egmla {
 
@@ -1023,9 +1024,10 @@ __host__ __device__ constexpr size_t f32_smem_floats(int d_c, int d_rope) {
 static_assert(f32_smem_floats(512, kF32MaxRope) * sizeof(float) <= kSmemMost, "shared memory");
 
 // NV: 16-byte units of a latent row per lane (d_c <= 128 NV)
-template <int NV>
+// Q8: c_pool holds codes (egmla_q8.cuh), scale_pool their scales
+template <int NV, bool Q8>
 __global__ void __launch_bounds__(kF32Threads, 1)
-decode_f32_kernel(const float* __restrict__ c_pool, const float* __restrict__ kr_pool,
+decode_f32_kernel(const void* __restrict__ c_pool, const float* __restrict__ scale_pool, const float* __restrict__ kr_pool,
                   const int32_t* __restrict__ id_pool, const int32_t* __restrict__ block_table,
                   int max_pages, const int32_t* __restrict__ seq_lens, int batch, int num_pages,
                   const float* __restrict__ gate_table, const float* __restrict__ gamma,
@@ -1125,7 +1127,14 @@ decode_f32_kernel(const float* __restrict__ c_pool, const float* __restrict__ kr
             z[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
             gv[k][i] = z[k][i];
             if (t < ntok && u < ncol) {
-              z[k][i] = __ldg(reinterpret_cast<const float4*>(c_pool + (row0 + t) * d_c) + u);
+              if constexpr (Q8) {
+                const float s = __ldg(scale_pool + row0 + t);
+                float x[4];
+                q8_decode4(__ldg(static_cast<const uint32_t*>(c_pool) + (row0 + t) * ncol + u), x);
+                z[k][i] = make_float4(s * x[0], s * x[1], s * x[2], s * x[3]);
+              } else {
+                z[k][i] = __ldg(static_cast<const float4*>(c_pool) + (row0 + t) * ncol + u);
+              }
               if (gate) gv[k][i] = __ldg(reinterpret_cast<const float4*>(gate_table + static_cast<size_t>(id[k]) * d_c) + u);
             }
           }
@@ -1351,19 +1360,27 @@ cudaError_t launch_prologue_tc(const DecodeArgs& a, const AppendArgs* app, const
 }
 
 namespace {
-template <int NV>
+template <int NV, bool Q8>
 cudaError_t launch_decode_f32_t(const DecodeArgs& a, const WorkspaceLayout& wl, cudaStream_t st) {
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   const size_t smem = f32_smem_floats(a.d_c, a.d_rope) * sizeof(float);
-  const cudaError_t e = allow_smem(decode_f32_kernel<NV>, f32_smem_floats(128 * NV, kF32MaxRope) * sizeof(float));
+  const cudaError_t e = allow_smem(decode_f32_kernel<NV, Q8>, f32_smem_floats(128 * NV, kF32MaxRope) * sizeof(float));
   if (e != cudaSuccess) return e;
   return launch_chained(
-      decode_f32_kernel<NV>, dim3(a.num_splits), dim3(kF32Threads), smem, st,
-      static_cast<const float*>(a.c_pool), static_cast<const float*>(a.kr_pool), a.id_pool, a.block_table,
+      decode_f32_kernel<NV, Q8>, dim3(a.num_splits), dim3(kF32Threads), smem, st,
+      a.c_pool, a.scale_pool, static_cast<const float*>(a.kr_pool), a.id_pool, a.block_table,
       a.max_pages, a.seq_lens, a.batch, a.num_pages, static_cast<const float*>(a.gate_table), a.ln_gamma,
       a.ln_beta, ws + wl.off_qprep, wl.qprep_stride, reinterpret_cast<const int32_t*>(ws + wl.off_cu),
       reinterpret_cast<float*>(ws + wl.off_ml), reinterpret_cast<float*>(ws + wl.off_o), a.H, a.d_c, a.d_rope,
       a.vocab, a.gate, a.gate_add, a.gate_ln, a.scale_log2, a.eps, a.status);
+}
+
+template <bool Q8>
+cudaError_t launch_decode_f32_q(const DecodeArgs& a, cudaStream_t st) {
+  const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
+  if (a.d_c <= 128) return launch_decode_f32_t<1, Q8>(a, wl, st);
+  if (a.d_c <= 256) return launch_decode_f32_t<2, Q8>(a, wl, st);
+  return launch_decode_f32_t<4, Q8>(a, wl, st);
 }
 }  // namespace
 
@@ -1383,10 +1400,7 @@ cudaError_t launch_prologue_f32(const DecodeArgs& a, const AppendArgs* app, cuda
 }
 
 cudaError_t launch_decode_f32(const DecodeArgs& a, cudaStream_t st) {
-  const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, a.H, a.d_c, a.d_rope, false);
-  if (a.d_c <= 128) return launch_decode_f32_t<1>(a, wl, st);
-  if (a.d_c <= 256) return launch_decode_f32_t<2>(a, wl, st);
-  return launch_decode_f32_t<4>(a, wl, st);
+  return a.scale_pool != nullptr ? launch_decode_f32_q<true>(a, st) : launch_decode_f32_q<false>(a, st);
 }
 
 namespace {

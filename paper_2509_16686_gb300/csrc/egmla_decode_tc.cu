@@ -68,6 +68,7 @@
 #include "egmla_common.cuh"
 #include "egmla_kernels.h"
 #include "egmla_ptx.cuh"
+#include "egmla_q8.cuh"
 
 namespace egmla {
 
@@ -103,7 +104,11 @@ constexpr float kLazyLog2 = 8.f;
 constexpr int kNB = 4;
 constexpr int kNP = 4;
 
-template <int D_C, bool GATE>
+// Q8: the cache holds the latent in 8 bits (egmla_q8.cuh).  The page's codes, scales and
+// ids and its RoPE keys land in a ring of raw slots, from which the gate warps write the
+// bf16 tile into a ring of latent slots: a raw slot is held until the tile's score MMAs
+// are complete, a latent slot from the gate to its output MMAs.
+template <int D_C, bool GATE, bool Q8 = false>
 struct Cfg {
   static constexpr int NCH = D_C / 64;                  // 64-feature swizzle-atom columns
   // tokens per tile: a page, or half a page for the widest latent, whose pages
@@ -113,7 +118,10 @@ struct Cfg {
   static constexpr int TOK = D_C > 256 ? kPage / 2 : kPage;
   static constexpr uint32_t PCHUNK = TOK * 128;         // one atom column of a tile
   static constexpr uint32_t KR_OFF = NCH * PCHUNK;
-  static constexpr uint32_t SLOT = KR_OFF + PCHUNK;     // latent + RoPE key of one tile
+  static constexpr uint32_t SLOT = Q8 ? KR_OFF : KR_OFF + PCHUNK;   // latent (+ RoPE key) of one tile
+  // raw slots: RoPE key, codes; apart from them the ids and the scales
+  static constexpr uint32_t RSLOT = Q8 ? PCHUNK + TOK * D_C : 0;
+  static constexpr uint32_t RMETA = Q8 ? (GATE ? 2 : 1) * kPage * 4 : 0;
   static constexpr uint32_t STAT_BYTES = GATE ? 2 * kPage * 4 : 0;   // per slot: mu[64], r[64]
   static constexpr uint32_t QB_LAT = qprep_lat_bytes(D_C);
   static constexpr uint32_t QPREP = qprep_bytes_tc(D_C, kRope);
@@ -125,19 +133,25 @@ struct Cfg {
   // softmax exchange: tile maxima [4 warps][16], segment sums [4 warps][16][2],
   // with half pages the odd latent columns' scores [32 tokens][16]
   static constexpr uint32_t XCH = 1024 + (TOK < kPage ? TOK * kHeads * 4 : 0);
-  static constexpr uint32_t MISC = 1024;
+  static constexpr uint32_t MISC = Q8 ? 512 : 1024;
   static constexpr uint32_t FIXED = kNP * PBUF + GB_BYTES + XCH + MISC + 1024;
   // slots with two query buffers (the next segment's loaded while this one is
   // in use) or with one; one buffer when a second would cost a slot below five
   static constexpr int NS2 = (int)((kSmemLimit - FIXED - 2 * QBUF) / (SLOT + STAT_BYTES));
   static constexpr int NS1 = (int)((kSmemLimit - FIXED - QBUF) / (SLOT + STAT_BYTES));
-  static constexpr int NQ = (NS2 < 5 && NS1 > NS2) ? 1 : 2;
+  static constexpr int NQ = Q8 ? (D_C == 192 ? 2 : 1) : (NS2 < 5 && NS1 > NS2) ? 1 : 2;
   static constexpr int NS_FIT = NQ == 2 ? NS2 : NS1;
-  static constexpr int NS = NS_FIT > 6 ? 6 : NS_FIT;
-  static constexpr uint32_t OFF_QBUF = NS * SLOT;
+  static constexpr int NS = Q8 ? 4 : NS_FIT > 6 ? 6 : NS_FIT;
+  // raw slots: what is left beside the latent slots
+  static constexpr int NR_FIT =
+      Q8 ? (int)((kSmemLimit - FIXED - NQ * QBUF - NS * (SLOT + STAT_BYTES)) / (RSLOT + RMETA + (Q8 ? 0 : 1))) : 0;
+  static constexpr int NR = NR_FIT > 6 ? 6 : NR_FIT;
+  static constexpr uint32_t OFF_RAW = NS * SLOT;
+  static constexpr uint32_t OFF_QBUF = OFF_RAW + NR * RSLOT;
   static constexpr uint32_t OFF_PBUF = OFF_QBUF + NQ * QBUF;
   static constexpr uint32_t OFF_STAT = OFF_PBUF + kNP * PBUF;
-  static constexpr uint32_t OFF_GB = OFF_STAT + NS * STAT_BYTES;
+  static constexpr uint32_t OFF_META = OFF_STAT + NS * STAT_BYTES;
+  static constexpr uint32_t OFF_GB = OFF_META + NR * RMETA;
   static constexpr uint32_t OFF_XCH = OFF_GB + GB_BYTES;
   static constexpr uint32_t OFF_MISC = OFF_XCH + XCH;
   static constexpr uint32_t SMEM = OFF_MISC + MISC + 1024;
@@ -147,9 +161,11 @@ struct Cfg {
   static constexpr uint32_t S_COLS = 32;
   static constexpr uint32_t COL_S = 0, COL_O = kNB * S_COLS;
   static constexpr uint32_t TMEM_COLS = 256;
-  static constexpr uint32_t PAGE_TX = SLOT;
+  static constexpr uint32_t PAGE_TX = Q8 ? RSLOT + TOK * 4 : SLOT;
   static constexpr uint32_t ID_TX = GATE ? kPage * 4 : 0;   // the page's token ids
-  static_assert(NS >= 3, "the ring needs three page slots");
+  static constexpr int RING = Q8 ? NR : NS;                 // slots that copies land in
+  static_assert(NS >= 3 && RING >= 3, "the ring needs three page slots");
+  static_assert(SLOT % 1024 == 0 && RSLOT % 1024 == 0, "swizzle atoms");
   static_assert(SMEM <= kSmemLimit, "shared memory");
   static_assert(D_C == 192 || D_C == 256 || (D_C == 512 && !GATE), "latent widths of this kernel");
   static_assert(COL_O + kHeads * NMC <= TMEM_COLS && NMC % 2 == 0, "tensor memory");
@@ -163,6 +179,8 @@ struct Cfg {
 };
 
 struct TcParams {
+  const uint8_t* c8;      // Q8: codes [num_pages, 64, d_c], scales [num_pages, 64]
+  const float* scales;
   const int32_t* id_pool;
   const int32_t* block_table;
   const int32_t* seq_lens;
@@ -238,7 +256,7 @@ __device__ __forceinline__ void phase_mark(const TcParams& p, int event) {
 
 // shared-memory barrier block (inside MISC)
 struct Bars {
-  uint64_t full[6], empty[6], zready[6];
+  uint64_t full[6], empty[6], zready[6], zfree[6];
   uint64_t qfull[2], qempty[2];
   uint64_t sready[kNB], sfree[kNB];
   uint64_t spdone[kNP], pfree[kNP];
@@ -629,17 +647,17 @@ __device__ void fused_combine(const TcParams& p, uint8_t* smem, Bars& bars) {
 // GM: gate mode (0 none, 1 LN(c (*) g), 2 c (*) g, 3 LN(c + g): eg_mla_gate_mode)
 // DBG: 0 the decode, 1 the cache-read dump (raw pages and gate rows, no
 // attention), 2 the decode with the pipeline trace, 3 the decode beside the attention
-// over a shared prefix
+// over a shared prefix, 4 the decode over a cache in 8 bits
 template <int D_C, int GM, int DBG>
 __global__ void __launch_bounds__(kThreads, 1)
     decode_tc_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap krmap,
                      const TcParams p) {
-  constexpr bool DUMP = DBG == 1, BESIDE = DBG == 3;
+  constexpr bool DUMP = DBG == 1, BESIDE = DBG == 3, Q8 = DBG == 4;
   using Tracer = TracerT<DBG == 2>;
   constexpr bool GATE = GM != 0;
   constexpr bool GATE_ADD = GM == 3;             // ablation: c + g
   constexpr bool GATE_LN = GM == 1 || GM == 3;   // LayerNorm after the gate
-  using C = Cfg<D_C, GATE>;
+  using C = Cfg<D_C, GATE, Q8>;
   // The MMA issuers: one thread of the warp, or (d_c 192 gated with a product) the
   // whole warp waiting together and electing a thread for each tile's MMAs.  Steps
   // replayed 24 to a graph, one thread / whole warp: d_c 192 with c (*) g 65.7 / 65.1
@@ -673,10 +691,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (p.early && p.fuse) grid_launch_dependents();
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::NS; ++s) {
+    for (int s = 0; s < C::RING; ++s) {
       mbar_init(smem_u32(&bars.full[s]), 1);
       mbar_init(smem_u32(&bars.empty[s]), DUMP ? kGateWarps : 1);
+    }
+    for (int s = 0; s < C::NS; ++s) {
       mbar_init(smem_u32(&bars.zready[s]), kGateWarps);
+      if (Q8) mbar_init(smem_u32(&bars.zfree[s]), 1);
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&bars.qfull[s]), 1);
@@ -703,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_relinquish();
   }
   if (warp == kTmaWarp && lane == 0) {
-    prefetch_tensormap(&cmap);
+    if (!Q8) prefetch_tensormap(&cmap);
     prefetch_tensormap(&krmap);
   }
   tc_fence_before();
@@ -745,10 +766,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok_loop = true;
     while (ok_loop && w.next(t)) {
       const int pg = pw.page(p, t, lane);
-      const int slot = it % C::NS;
+      const int slot = it % C::RING;
       if (lane == 0) {
         tr.mark(0, it);
-        if (!mbar_wait(smem_u32(&bars.empty[slot]), ((it / C::NS) & 1) ^ 1, abort_flag, wait_ns)) ok_loop = false;
+        if (!mbar_wait(smem_u32(&bars.empty[slot]), ((it / C::RING) & 1) ^ 1, abort_flag, wait_ns)) ok_loop = false;
         if (ok_loop) {
           tr.mark(1, it);
           const bool ok = pg >= 0 && pg < p.num_pages;
@@ -759,9 +780,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!withheld) {
             const uint32_t fb = smem_u32(&bars.full[slot]);
             mbar_arrive_expect_tx(fb, ok ? C::PAGE_TX + C::ID_TX : 0u);
-            if (ok) {
+            const int y = pg * kPage + t.tok0 % kPage;
+            if (Q8) {
+              if (ok) {
+                const uint32_t dst = sbase + C::OFF_RAW + slot * C::RSLOT, meta = sbase + C::OFF_META + slot * C::RMETA;
+                bulk_load_hint(dst + C::PCHUNK, p.c8 + static_cast<size_t>(y) * D_C, C::TOK * D_C, fb, pol_stream);
+                tma_load_3d(dst, &krmap, 0, y, 0, fb, pol_stream);
+                bulk_load_hint(meta, p.scales + y, C::TOK * 4, fb, pol_stream);
+                if (C::ID_TX)
+                  bulk_load_hint(meta + kPage * 4, p.id_pool + static_cast<size_t>(pg) * kPage, C::ID_TX, fb, pol_stream);
+              }
+            } else if (ok) {
               const uint32_t dst = sbase + slot * C::SLOT;
-              const int y = pg * kPage + t.tok0 % kPage;
               tma_load_3d(dst, &cmap, 0, y, 0, fb, pol_stream);
               tma_load_3d(dst + C::KR_OFF, &krmap, 0, y, 0, fb, pol_stream);
               // the page's token ids, into the half of the slot's statistics that
@@ -801,8 +831,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // drain: every copy this thread issued must land before the CTA exits,
       // also after an abort (own flag: the wait is bounded but not cut short)
       volatile int own = 0;
-      for (int s = 0; s < C::NS; ++s)
-        if (last_it[s] >= 0 && !mbar_wait(smem_u32(&bars.full[s]), (last_it[s] / C::NS) & 1, &own, wait_ns)) *abort_flag = 1;
+      for (int s = 0; s < C::RING; ++s)
+        if (last_it[s] >= 0 && !mbar_wait(smem_u32(&bars.full[s]), (last_it[s] / C::RING) & 1, &own, wait_ns)) *abort_flag = 1;
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
@@ -881,6 +911,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (issuer_one()) {
           mbar_arrive(smem_u32(&bars.sready[sb]));
           const uint64_t za = zdesc_k + ((slot * C::SLOT) >> 4);
+          const uint64_t ka = Q8 ? zdesc_k + ((C::OFF_RAW + js % C::RING * C::RSLOT) >> 4) : za + (C::KR_OFF >> 4);
           const uint64_t qb = qdesc0 + (((seg % C::NQ) * C::QBUF) >> 4);
           const uint32_t ds = tmem + C::COL_S + sb * C::S_COLS;
           if constexpr (C::TOK < kPage) {
@@ -891,7 +922,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                           qb2 + ((kk * 4 * kQGroupBytes) >> 4), IDESC_S2, kk > 0);
 #pragma unroll
             for (int kk = 0; kk < kRope / 16; ++kk)
-              mma_bf16_ss(ds, za + ((C::KR_OFF + kk * 32) >> 4),
+              mma_bf16_ss(ds, ka + ((kk * 32) >> 4),
                           qb + ((C::QB_LAT + kk * 2 * kQGroupBytes) >> 4), IDESC_S, 1);
           } else {
 #pragma unroll
@@ -900,10 +931,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                           qb + ((kk * 2 * kQGroupBytes) >> 4), IDESC_S, kk > 0);
 #pragma unroll
             for (int kk = 0; kk < kRope / 16; ++kk)
-              mma_bf16_ss(ds + kHeads, za + ((C::KR_OFF + kk * 32) >> 4),
+              mma_bf16_ss(ds + kHeads, ka + ((kk * 32) >> 4),
                           qb + ((C::QB_LAT + kk * 2 * kQGroupBytes) >> 4), IDESC_S, kk > 0);
           }
           mma_commit(smem_u32(&bars.sready[sb]));
+          if (Q8) mma_commit(smem_u32(&bars.empty[js % C::RING]));
           if (ts.last) mma_commit(smem_u32(&bars.qempty[seg % C::NQ]));
         }
         issuer_join();
@@ -960,7 +992,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int mc = 0; mc < C::NMC; ++mc)
               mma_bf16_ss(tmem + C::COL_O + kHeads * mc, za + (((C::mc_start(mc) / 64) * C::PCHUNK + ks * 2048) >> 4),
                           pb + ((ks * 512) >> 4), IDESC_O, ks > 0 ? 1u : keep);
-          mma_commit(smem_u32(&bars.empty[slot]));
+          mma_commit(smem_u32(Q8 ? &bars.zfree[slot] : &bars.empty[slot]));
           mma_commit(smem_u32(&bars.pfree[jo % kNP]));
         }
         issuer_join();
@@ -1000,7 +1032,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // id of this thread's row of tile jj, from the slot that holds its page (0
     // past the end of the page)
     auto slot_id = [&](int jj, const Tile& tt) -> int {
-      const int32_t* ids = reinterpret_cast<const int32_t*>(smem + C::OFF_STAT + (jj % C::NS) * C::STAT_BYTES + kPage * 4);
+      const int32_t* ids = reinterpret_cast<const int32_t*>(
+          smem + (Q8 ? C::OFF_META + (jj % C::RING) * C::RMETA : C::OFF_STAT + (jj % C::NS) * C::STAT_BYTES) + kPage * 4);
       return row < tt.ntok ? ids[row] : 0;
     };
     // this thread's part of the gate row of token id (row 0, reported, for an
@@ -1029,6 +1062,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     Tracer tr;
     tr.init(p, 2);
     if (threadIdx.x != kGateWarp0 * 32) tr.base = nullptr;
+    // Q8: this thread's row of the codes, its part of the row's 64-feature columns
+    // (qsub, qsub + kQSubs, ..: four lanes a row, eight with half pages), and 16 codes of
+    // each, which are the units 2 (lane % 4) and the next of the column's bf16 values
+    constexpr int kQSubs = kPage / C::TOK, kQCols = C::NCH / kQSubs;
+    const int qrow = gw * (C::TOK / kGateWarps) + lane / (4 * kQSubs), qsub = lane / 4 % kQSubs;
+    uint4 codes[Q8 ? kQCols : 1];
+    Q8Widen widen;
+    static_assert(!Q8 || (kGateWarps == 8 && (!GATE || kQSubs == 1)), "rows of the codes");
     Tile t, t1;
     bool have = w.next(t);
     bool have1 = have && w.next(t1);
@@ -1052,7 +1093,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // over the tile instead of one burst), otherwise after this tile.
       bool next_issued = false;
       const __nv_bfloat16* gsrc_next = p.gate_table;
-      if (GATE && have1 && warp_test(smem_u32(&bars.full[(j + 1) % C::NS]), ((j + 1) / C::NS) & 1)) {
+      if (GATE && have1 && warp_test(smem_u32(&bars.full[(j + 1) % C::RING]), ((j + 1) / C::RING) & 1)) {
         gsrc_next = g_row(slot_id(j + 1, t1));
         next_issued = true;
       }
@@ -1064,7 +1105,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             gnext[fc][0] = ldg_16_na_hint(gsrc_next + fc * 64, pol_keep);
         }
       };
-      if (!warp_wait(smem_u32(&bars.full[slot]), (j / C::NS) & 1, abort_flag, wait_ns)) break;
+      if (!warp_wait(smem_u32(&bars.full[j % C::RING]), (j / C::RING) & 1, abort_flag, wait_ns)) break;
       tr.mark(1, j);
       if (DUMP) id0 = slot_id(j, t);
       uint8_t* cpage = smem + slot * C::SLOT;
@@ -1092,7 +1133,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         warp_arrive(smem_u32(&bars.empty[slot]));
       } else {
         const bool full_page = t.ntok == C::TOK;   // uniform: no token masking needed
-        if (GATE) {
+        if constexpr (Q8) {
+          // the tile's codes into registers, and the latent slot of the tile (output
+          // MMAs of the tile NS before it complete)
+          const uint8_t* raw = smem + C::OFF_RAW + (j % C::RING) * C::RSLOT + C::PCHUNK;
+          const float* scales = reinterpret_cast<const float*>(smem + C::OFF_META + (j % C::RING) * C::RMETA);
+          raw += qrow * D_C + qsub * 64 + 16 * (lane % 4);
+#pragma unroll
+          for (int i = 0; i < kQCols; ++i) codes[i] = *reinterpret_cast<const uint4*>(raw + i * (C::NCH / kQCols) * 64);
+          widen.set(scales[qrow]);
+          if (!warp_wait(smem_u32(&bars.zfree[slot]), ((j / C::NS) & 1) ^ 1, abort_flag, wait_ns)) break;
+        }
+        if constexpr (Q8 && !GATE) {
+#pragma unroll
+          for (int i = 0; i < kQCols; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              // (of a row shared by eight lanes, the second four write their units in
+              // the other order, so that the eight meet different banks)
+              const int hh = kQSubs > 1 ? h ^ qsub : h;
+              const uint32_t w0 = hh ? codes[i].z : codes[i].x, w1 = hh ? codes[i].w : codes[i].y;
+              uint4 z;
+              widen.four(w0, z.x, z.y);
+              widen.four(w1, z.z, z.w);
+              if (qrow >= t.ntok) z = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(cpage + (i * (C::NCH / kQCols) + qsub) * C::PCHUNK + qrow * 128 +
+                                        (((2 * (lane % 4) + hh) ^ (qrow & 7)) << 4)) = z;
+            }
+          }
+        } else if (GATE) {
           float* st = reinterpret_cast<float*>(smem + C::OFF_STAT + slot * C::STAT_BYTES);
           // all shared-memory reads of this thread's units first (the in-place
           // stores below would otherwise order every later load behind them)
@@ -1100,7 +1169,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int fc = 0; fc < C::NCH; ++fc)
 #pragma unroll
-            for (int h = 0; h < kGateUnits; ++h) cv[fc][h] = *reinterpret_cast<const uint4*>(cpage + unit_off(fc, h));
+            for (int h = 0; h < kGateUnits; ++h) {
+              if constexpr (Q8) {
+                uint4& c = cv[fc][h];
+                widen.four(h ? codes[fc].z : codes[fc].x, c.x, c.y);
+                widen.four(h ? codes[fc].w : codes[fc].y, c.z, c.w);
+              } else {
+                cv[fc][h] = *reinterpret_cast<const uint4*>(cpage + unit_off(fc, h));
+              }
+            }
           tr.mark(5, j);
           const bool valid = row < t.ntok;
           if constexpr (GATE_ADD) {
@@ -1225,7 +1302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tr.mark(3, j);
       if (GATE && have1 && !next_issued) {
         // the next page landed only now
-        if (!warp_wait(smem_u32(&bars.full[(j + 1) % C::NS]), ((j + 1) / C::NS) & 1, abort_flag, wait_ns)) break;
+        if (!warp_wait(smem_u32(&bars.full[(j + 1) % C::RING]), ((j + 1) / C::RING) & 1, abort_flag, wait_ns)) break;
         load_g(slot_id(j + 1, t1), gnext);
       }
       ++j;
@@ -1600,13 +1677,15 @@ int resident_ctas(uint32_t smem) {
 
 template <int D_C, int GM, int DBG>
 cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_t st, bool* fused) {
-  using C = Cfg<D_C, GM != 0>;
+  using C = Cfg<D_C, GM != 0, DBG == 4>;
   auto kern = decode_tc_kernel<D_C, GM, DBG>;
   cudaError_t e = allow_smem(kern, C::SMEM);
   if (e != cudaSuccess) return e;
   const WorkspaceLayout wl = workspace_layout(a.batch, a.num_splits, kHeads, D_C, kRope, true);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   TcParams p;
+  p.c8 = static_cast<const uint8_t*>(a.c_pool);
+  p.scales = a.scale_pool;
   p.id_pool = a.id_pool;
   p.block_table = a.block_table;
   p.seq_lens = a.seq_lens;
@@ -1692,6 +1771,11 @@ bool tc_supported(int d_c, int gate) {
 // none and mul_ln (the others run untraced)
 template <int GM>
 cudaError_t launch_mode(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_t st, bool* fused) {
+  if (a.scale_pool != nullptr) {
+    if (a.d_c == 192) return launch_one<192, GM, 4>(a, maps, st, fused);
+    if (a.d_c == 256) return launch_one<256, GM, 4>(a, maps, st, fused);
+    return cudaErrorInvalidValue;
+  }
   if constexpr (GM <= 1) {
     if (a.trace != nullptr) {
       if (a.d_c == 192) return launch_one<192, GM, 2>(a, maps, st, fused);
@@ -1718,7 +1802,8 @@ cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool 
     return cudaErrorInvalidValue;
   }
   if (!a.gate) {
-    if (a.d_c == 512) return launch_one<512, 0, 0>(a, maps, st, fused);
+    if (a.d_c == 512)
+      return a.scale_pool != nullptr ? launch_one<512, 0, 4>(a, maps, st, fused) : launch_one<512, 0, 0>(a, maps, st, fused);
     return launch_mode<0>(a, maps, st, fused);
   }
   if (a.gate_add) return launch_mode<3>(a, maps, st, fused);

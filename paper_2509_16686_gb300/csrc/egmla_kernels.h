@@ -153,6 +153,7 @@ struct DecodeArgs {
   // tensors
   const void* q;
   const void* c_pool;
+  const float* scale_pool;  // non-null: c_pool holds the latent in 8 bits (egmla_q8.cuh)
   const void* kr_pool;
   const int32_t* id_pool;
   const int32_t* block_table;

@@ -1,0 +1,831 @@
+"""GPU parity of eg_mla_rope and of the calls on a cache that holds the latent in 8 bits.
+
+eg_mla_rope against its formula in extended precision.  Error of an entry x cos - y sin:
+the angle's (2^-32 of a turn, and the eight half-steps of its frequency in double precision,
+2^-50 of it, times the position), sine's and cosine's (2 ulp: 2^-23), and four fp32 roundings (2^-24 each), all on
+values of at most m (|x| + |y|); then the rounding of the output, half a step of its type.
+
+eg_mla_append_latent_q8 is whole numbers: codes and scales equal a search over e4m3's
+grid in 64 bits, bit for bit.  eg_mla_read_latent_q8 gives scale x code exactly.
+
+eg_mla_decode_q8 equals eg_mla_decode over the values read back, bit for bit, and is within
+the hot path's bounds of the oracle on them."""
+import dataclasses
+import importlib.util
+import math
+import os
+import threading
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import egmla_oracle as orc
+from paper_2509_16686_gb300 import _lib, device, synth
+
+pytestmark = pytest.mark.gpu
+P = 64
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+HALF_STEP = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
+RANGE = _lib.EG_MLA_ERR_OUT_OF_RANGE
+
+
+def ints(values):
+    return torch.tensor(np.asarray(values, np.int64).astype(np.int32), dtype=torch.int32, device="cuda")
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def offsets(lens):
+    return [0] + list(np.cumsum(np.asarray(lens, np.int64)))
+
+
+def normal(shape, dtype, seed, std=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(DT[dtype])
+
+
+# ------------------------------------------------------------------ rope
+def rates(d, scaling="none", theta=10000.0, factor=1.0, original_len=0, beta_fast=32.0, beta_slow=1.0, **_):
+    L = np.longdouble
+    i = np.arange(0, d, 2).astype(L) / L(d)
+    if scaling == "ntk":
+        theta = L(theta) * L(factor) ** (L(d) / L(d - 2))
+    f = L(theta) ** -i
+    if scaling == "linear":
+        f = f / L(factor)
+    if scaling == "yarn":
+        turns = L(original_len) * f / (2 * L("3.14159265358979323846264338327950288"))
+        g = np.clip((turns - L(beta_slow)) / L(beta_fast - beta_slow), 0, 1)
+        f = f * ((1 - g) / L(factor) + g)
+    return f
+
+
+def rope_reference(x, pos, d, kw):
+    """(rotated entries, bound without the output's rounding) of x [tokens, heads, dn + d], in 64 bits."""
+    f = rates(d, **kw)
+    m = kw.get("magnitude", 0.0) or (0.1 * math.log(kw.get("factor", 1.0)) + 1.0 if kw.get("scaling") == "yarn" else 1.0)
+    t = np.asarray(pos).astype(np.longdouble)[:, None] * f
+    two_pi = 2 * np.longdouble("3.14159265358979323846264338327950288")
+    t = (t - np.rint(t / two_pi) * two_pi).astype(np.float64)
+    cos, sin = m * np.cos(t)[:, None], m * np.sin(t)[:, None]
+    if kw.get("inverse"):
+        sin = -sin
+    x = x.double().cpu().numpy()
+    y, bound = x.copy(), np.zeros_like(x)
+    r = x[..., x.shape[-1] - d:]
+    a, b = (r[..., :d // 2], r[..., d // 2:]) if kw.get("layout") == "half" else (r[..., 0::2], r[..., 1::2])
+    ra, rb = a * cos - b * sin, a * sin + b * cos
+    angle = 2 * math.pi * 2.0 ** -32 + np.abs(np.asarray(pos, np.float64))[:, None] * f.astype(np.float64) * 2.0 ** -50
+    e = (np.abs(a) + np.abs(b)) * m * (angle[:, None] + 2.0 ** -23 + 4 * 2.0 ** -24)
+    out, eb = y[..., x.shape[-1] - d:], bound[..., x.shape[-1] - d:]
+    if kw.get("layout") == "half":
+        out[..., :d // 2], out[..., d // 2:] = ra, rb
+        eb[..., :d // 2], eb[..., d // 2:] = e, e
+    else:
+        out[..., 0::2], out[..., 1::2] = ra, rb
+        eb[..., 0::2], eb[..., 1::2] = e, e
+    return y, bound
+
+
+def positions_of(lens, firsts):
+    return np.concatenate([np.arange(f, f + n) for f, n in zip(firsts, lens)] + [np.zeros(0, np.int64)])
+
+
+def check_rope(got, x, pos, d, dtype, kw):
+    want, bound = rope_reference(x, pos, d, kw)
+    got = got.double().cpu().numpy()
+    over = float((np.abs(got - want) - bound - HALF_STEP[dtype] * np.abs(want)).max(initial=0.0))
+    assert over <= 0, over
+    n = x.shape[-1] - d
+    assert np.array_equal(got[..., :n], want[..., :n])   # the rest of the head is a copy
+
+
+ROPE_FORMS = [
+    dict(), dict(layout="half"), dict(inverse=True), dict(scaling="linear", factor=4.0),
+    dict(scaling="ntk", factor=8.0, layout="half"), dict(scaling="yarn", factor=32.0, original_len=4096),
+    dict(scaling="yarn", factor=1.0, original_len=2048, theta=500000.0, inverse=True, layout="half"),
+    dict(scaling="yarn", factor=16.0, original_len=8192, beta_fast=8.0, beta_slow=0.5, magnitude=0.75),
+    dict(theta=1.0, magnitude=2.0)]
+# heads, d_nope, d_rope: the workloads', one head, odd counts, sizes that no 16-byte unit divides
+ROPE_SHAPES = [(16, 128, 64), (1, 0, 64), (3, 32, 16), (5, 7, 10), (2, 64, 128), (7, 128, 256), (4, 8, 2), (64, 64, 32),
+               (12, 40, 48), (1, 3, 6)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", ROPE_SHAPES)
+@pytest.mark.parametrize("form", range(len(ROPE_FORMS)))
+def test_rope_matches_the_formula(gpu_lib, dtype, shape, form):
+    (H, dn, dr), kw = shape, ROPE_FORMS[form]
+    if kw.get("scaling") == "ntk" and dr == 2:
+        kw = dict(layout="half")
+    lens, firsts = [1, 0, 33, 5, 64], [7, 3, 0, 100000, 4090]
+    T = sum(lens)
+    dims = _lib.make_dims(H, dn, dr, 128, 256, 100, dtype=dtype)
+    q, k = normal((T, H, dn + dr), dtype, form), normal((T, dr), dtype, 50 + form)
+    qo, ko, st = torch.full_like(q, 77), torch.full_like(k, 77), status_word()
+    _lib.eg_mla_rope(dims, _lib.make_rope(**kw), q, qo, k, ko, ints(firsts), ints(offsets(lens)), st)
+    pos = positions_of(lens, firsts)
+    check_rope(qo, q, pos, dr, dtype, kw)
+    check_rope(ko[:, None], k[:, None], pos, dr, dtype, kw)
+    # in place: the same values
+    q2, k2 = q.clone(), k.clone()
+    _lib.eg_mla_rope(dims, _lib.make_rope(**kw), q2, q2, k2, k2, ints(firsts), ints(offsets(lens)), st)
+    assert torch.equal(q2, qo) and torch.equal(k2, ko) and int(st) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [1, 2, 7, 64, 300, 2500])
+def test_rope_of_one_token_per_sequence(gpu_lib, dtype, T):
+    r = np.random.default_rng(T)
+    pos = r.integers(0, 1 << 20, T)
+    dims = _lib.make_dims(16, 128, 64, 128, 256, 100, dtype=dtype)
+    q, k = normal((T, 16, 192), dtype, T), normal((T, 64), dtype, T + 1)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, qo, k, ko, ints(pos))
+    check_rope(qo, q, pos, 64, dtype, {})
+    check_rope(ko[:, None], k[:, None], pos, 64, dtype, {})
+
+
+def test_rope_at_the_farthest_positions(gpu_lib):
+    """Positions up to 2^31 - 1, and past it with a sequence's own offset."""
+    dims = _lib.make_dims(2, 0, 64, 128, 256, 100, dtype="fp32")
+    for firsts, lens in (([2 ** 31 - 1, 2 ** 30 + 1, 2 ** 31 - 1], [1, 5, 70]), ([2 ** 24 + 1], [3])):
+        T = sum(lens)
+        q, k = normal((T, 2, 64), "fp32", 5), normal((T, 64), "fp32", 6)
+        qo, ko, st = torch.empty_like(q), torch.empty_like(k), status_word()
+        for kw in (dict(), dict(scaling="yarn", factor=8.0, original_len=4096, inverse=True)):
+            _lib.eg_mla_rope(dims, _lib.make_rope(**kw), q, qo, k, ko, ints(firsts), ints(offsets(lens)), st)
+            check_rope(qo, q, positions_of(lens, firsts), 64, "fp32", kw)
+            check_rope(ko[:, None], k[:, None], positions_of(lens, firsts), 64, "fp32", kw)
+        assert int(st) == 0
+
+
+@pytest.mark.parametrize("dtype,shift", [("bf16", 0), ("bf16", 1), ("bf16", 4), ("fp32", 0), ("fp32", 1), ("fp32", 2)])
+def test_rope_between_wider_rows(gpu_lib, dtype, shift):
+    """Slices of projection rows, at any alignment, to dense rows, in place and to other slices; what lies
+    between stays."""
+    T, H, dn, dr = 41, 16, 128, 64
+    wide = normal((T, H * 192 + 256 + 64 + 8), dtype, 9)
+    dims = _lib.make_dims(H, dn, dr, 128, 256, 100, dtype=dtype)
+    cu, pos = ints([0, 41]), np.arange(41)
+
+    def parts(t):
+        return t[:, shift:shift + H * 192].unflatten(1, (H, 192)), t[:, -64 - shift:t.shape[1] - shift]
+
+    q, k = parts(wide)
+    qo, ko = torch.empty((T, H, 192), dtype=DT[dtype], device="cuda"), torch.empty((T, 64), dtype=DT[dtype], device="cuda")
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, qo, k, ko, None, cu)
+    check_rope(qo, q, pos, dr, dtype, {})
+    check_rope(ko[:, None], k[:, None], pos, dr, dtype, {})
+    other = wide.clone()
+    q2, k2 = parts(other)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q2, q2, k2, k2, None, cu)
+    assert torch.equal(q2, qo) and torch.equal(k2, ko)
+    q2.copy_(q)
+    k2.copy_(k)
+    assert torch.equal(other, wide)
+    third = torch.full_like(wide, 5)
+    q3, k3 = parts(third)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, q3, k, k3, None, cu)
+    assert torch.equal(q3, qo) and torch.equal(k3, ko)
+    q3.fill_(5)
+    k3.fill_(5)
+    assert bool((third == 5).all())
+
+
+def test_rope_of_queries_or_keys_alone(gpu_lib):
+    dims = _lib.make_dims(16, 128, 64, 128, 256, 100)
+    q, k, pos = normal((20, 16, 192), "bf16", 1), normal((20, 64), "bf16", 2), ints(range(100, 120))
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, qo, k, ko, pos)
+    a, b = torch.empty_like(q), torch.empty_like(k)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, a, None, None, pos)
+    _lib.eg_mla_rope(dims, _lib.make_rope(), None, None, k, b, pos)
+    assert torch.equal(a, qo) and torch.equal(b, ko)
+
+
+def test_rope_leaves_what_belongs_to_no_token(gpu_lib):
+    """Rows behind the last sequence, and of sequences with a negative position."""
+    dims = _lib.make_dims(16, 128, 64, 128, 256, 100)
+    lens, firsts = [3, 4, 0, 6], [5, -1, 2, 0]
+    q, k = normal((20, 16, 192), "bf16", 3), normal((20, 64), "bf16", 4)
+    qo, ko, st = torch.full_like(q, 9), torch.full_like(k, 9), status_word()
+    _lib.eg_mla_rope(dims, _lib.make_rope(), q, qo, k, ko, ints(firsts), ints(offsets(lens)), st)
+    for o, x in ((qo, q), (ko[:, None], k[:, None])):
+        assert bool((o[3:7] == 9).all()) and bool((o[13:] == 9).all())
+        check_rope(o[:3], x[:3], np.arange(5, 8), 64, "bf16", {})
+        check_rope(o[7:13], x[7:13], np.arange(6), 64, "bf16", {})
+    assert int(st) == 0
+
+
+def test_rope_offsets_that_make_no_sense_are_reported(gpu_lib):
+    dims = _lib.make_dims(2, 8, 16, 128, 256, 100, dtype="fp32")
+    q, k = normal((6, 2, 24), "fp32", 3), normal((6, 16), "fp32", 4)
+    for cu in ([4, 6], [0, 5, 2, 6], [2 ** 31 - 1, 2 ** 31 - 1], [-5, 6]):
+        qo, ko, st = torch.full_like(q, 9), torch.full_like(k, 9), status_word()
+        _lib.eg_mla_rope(dims, _lib.make_rope(), q, qo, k, ko, None, ints(cu), st)
+        torch.cuda.synchronize()
+        if cu == [4, 6]:   # tokens 0 to 3 belong to no sequence
+            assert int(st) == RANGE and bool((qo[:4] == 9).all())
+            check_rope(qo[4:], q[4:], np.arange(2), 16, "fp32", {})
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("scaling", ["none", "yarn"])
+def test_rope_inverse_is_the_gradient(gpu_lib, layout, scaling):
+    """Against the formula's (the transposed matrix) and against differences, in fp32."""
+    kw = dict(layout=layout, scaling=scaling, factor=4.0, original_len=64)
+    dims = _lib.make_dims(2, 4, 16, 128, 256, 100, dtype="fp32")
+    T = 9
+    pos, q, w = ints(range(50, 59)), normal((T, 2, 20), "fp32", 1), normal((T, 2, 20), "fp32", 2)
+    grad, moved = torch.empty_like(q), torch.empty_like(q)
+    _lib.eg_mla_rope(dims, _lib.make_rope(inverse=True, **kw), w, grad, None, None, pos)
+    check_rope(grad, w, np.arange(50, 59), 16, "fp32", dict(kw, inverse=True))
+
+    def value(x):
+        _lib.eg_mla_rope(dims, _lib.make_rope(**kw), x, moved, None, None, pos)
+        return moved.double().mul(w.double()).sum((1, 2))   # one value per token, of which each depends on its own
+
+    for f in range(20):
+        for h in range(2):
+            step = torch.zeros_like(q)
+            step[:, h, f] = 2.0   # the map is linear: differences have no error of their own
+            d = (value(q + step) - value(q - step)) / 4
+            m = 0.1 * math.log(4.0) + 1.0
+            # each value: 20 products of two numbers below 6, each off by 2^-21 of m (|x| + |y|) |w|
+            assert bool(((d - grad[:, h, f].double()).abs() <= 2 * 40 * m * 16 * 6 * 2.0 ** -21 / 4).all())
+    # turning there and back gives m^2 times the input
+    back = torch.empty_like(q)
+    value(q)
+    _lib.eg_mla_rope(dims, _lib.make_rope(inverse=True, **kw), moved, back, None, None, pos)
+    m = 0.1 * math.log(4.0) + 1.0 if scaling == "yarn" else 1.0
+    assert bool(((back[..., 4:] - m * m * q[..., 4:]).abs() <= 2 * 12 * m * m * 2.0 ** -21).all())
+
+
+# ------------------------------------------------------------------ the cache in 8 bits
+GRID = np.array([(c & 7) * 2.0 ** -9 if c < 8 else (8 + (c & 7)) * 2.0 ** ((c >> 3) - 10) for c in range(127)])
+
+
+def quantise(x):
+    """(bytes, scales) by the definition, in 64 bits, with a search over the 127 magnitudes."""
+    x = np.asarray(x, np.float64)
+    a = np.abs(x).max(-1)
+    ok = np.isfinite(x).all(-1)
+    e = np.full(a.shape, -100)
+    for i in np.argwhere(ok):
+        i = tuple(i)
+        if a[i] > 0:
+            e[i] = max(-100, math.frexp(a[i] / 448)[1] - 1)
+            while a[i] > 448 * 2.0 ** e[i]:
+                e[i] += 1
+    e = np.minimum(e, 119)
+    y = np.where(ok[..., None], np.nan_to_num(x, posinf=0, neginf=0), 0) / 2.0 ** e[..., None]
+    mag = np.minimum(np.abs(y), 448)
+    hi = np.searchsorted(GRID, mag).clip(1, 126)
+    below, above = mag - GRID[hi - 1], GRID[hi] - mag
+    code = np.where((above < below) | ((above == below) & (hi % 2 == 0)), hi, hi - 1)
+    code = code | np.where(np.signbit(y), 128, 0)
+    return code.astype(np.uint8), np.where(ok, 2.0 ** e, np.nan)
+
+
+class Cache:
+    """Pools of `pages` pages, filled with values that no call leaves."""
+
+    def __init__(self, pages, d_c, dtype, d_rope=64, ids=True):
+        self.c8 = torch.full((pages, P, d_c), 0x33, dtype=torch.uint8, device="cuda")
+        self.scale = torch.full((pages, P), 3.0, device="cuda")
+        self.kr = torch.full((pages, P, d_rope), 7, dtype=DT[dtype], device="cuda")
+        self.ids = torch.full((pages, P), -5, dtype=torch.int32, device="cuda") if ids else None
+
+    def all(self):
+        return self.c8, self.scale, self.kr, self.ids
+
+    def clone(self):
+        other = object.__new__(Cache)
+        other.c8, other.scale, other.kr = self.c8.clone(), self.scale.clone(), self.kr.clone()
+        other.ids = None if self.ids is None else self.ids.clone()
+        return other
+
+
+def tables(lens, firsts, seed, spare=3):
+    """(block table of shuffled pages, pool rows of the packed tokens, pages)."""
+    pages = [max(0, -(-(f + n) // P)) if f >= 0 else 1 for f, n in zip(firsts, lens)]
+    order = np.random.default_rng(seed).permutation(sum(pages) + spare)
+    table = np.full((len(lens), max(pages + [1])), 99999999, np.int64)
+    at = 0
+    for b, n in enumerate(pages):
+        table[b, :n] = order[at:at + n]
+        at += n
+    rows = [table[b, p // P] * P + p % P for b, (f, n) in enumerate(zip(firsts, lens)) for p in range(f, f + n) if f >= 0]
+    return table, np.asarray(rows, np.int64), len(order)
+
+
+def append_case(lens, firsts, d_c, dtype, seed=0, d_rope=64, x=None):
+    T = sum(lens)
+    c = normal((T, d_c), dtype, seed, 0.5) if x is None else x
+    kr, ids = normal((T, d_rope), dtype, seed + 1), torch.arange(100, 100 + T, dtype=torch.int32, device="cuda")
+    table, rows, pages = tables(lens, firsts, seed)
+    dims = _lib.make_dims(16, 128, d_rope, 128, d_c, 1000, dtype=dtype)
+    return dims, c, kr, ids, table, rows, Cache(pages, d_c, dtype, d_rope)
+
+
+def assert_cache(cache, before, rows, kept, c, kr, ids):
+    """The rows of the tokens `kept` hold them, all others what they did."""
+    code, scale = quantise(c[kept].double().cpu().numpy())
+    want = before.clone()
+    r = torch.as_tensor(rows, device="cuda")
+    c8 = want.c8.view(-1, want.c8.shape[-1])
+    c8[r] = torch.as_tensor(code, device="cuda")
+    want.scale.view(-1)[r] = torch.as_tensor(scale.astype(np.float32), device="cuda")
+    want.kr.view(-1, want.kr.shape[-1])[r] = kr[kept]
+    if ids is not None:
+        want.ids.view(-1)[r] = ids[kept]
+    nan = want.scale.view(-1).isnan()
+    got = cache.c8.view(-1, want.c8.shape[-1])
+    assert torch.equal(got[~nan], c8[~nan])
+    assert bool((got[nan] & 0x7f == 0x7f).all())
+    assert torch.equal(cache.scale.view(-1).isnan(), nan) and torch.equal(cache.scale.view(-1)[~nan], want.scale.view(-1)[~nan])
+    assert torch.equal(cache.kr, want.kr) and (ids is None or torch.equal(cache.ids, want.ids))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d_c,d_rope", [(256, 64), (192, 64), (512, 64), (16, 8), (64, 32), (272, 256), (496, 24)])
+@pytest.mark.parametrize("lens,firsts", [([1], [0]), ([64, 1, 0, 65, 200], [0, 63, 5, 10, 127]),
+                                         ([7, 3, 2, 0, 9], [100, -1, 3, -7, 0])])
+def test_append_and_read_back(gpu_lib, dtype, d_c, d_rope, lens, firsts):
+    dims, c, kr, ids, table, rows, cache = append_case(lens, firsts, d_c, dtype, d_rope=d_rope)
+    before, st = cache.clone(), status_word()
+    cu, pos, T = ints(offsets(lens)), ints(firsts), sum(lens)
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, ints(table), pos, cu, st)
+    kept = torch.as_tensor(np.repeat(np.asarray(firsts) >= 0, lens), device="cuda")
+    assert_cache(cache, before, rows, kept, c, kr, ids)
+    co, ko, io = torch.full_like(c, 9), torch.full_like(kr, 9), torch.full_like(ids, 9)
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), ints(table), co, ko, io, pos, cu, st)
+    code, scale = quantise(c.double().cpu().numpy())
+    value = np.where(code & 128, -1, 1) * GRID[code & 127] * scale[:, None]
+    assert np.array_equal(co[kept].double().cpu().numpy(), value[kept.cpu().numpy()])
+    assert torch.equal(ko[kept], kr[kept]) and torch.equal(io[kept], ids[kept])
+    assert bool((co[~kept] == 9).all()) and bool((ko[~kept] == 9).all()) and bool((io[~kept] == 9).all())
+    # the latents alone
+    only = torch.full_like(c, 9)
+    _lib.eg_mla_read_latent_q8(dims, cache.c8.view(torch.float8_e4m3fn), cache.scale, cache.kr, None, ints(table), only,
+                               None, None, pos, cu, st)
+    assert torch.equal(only, co) and int(st) == 0
+    # what is read and written again reads the same (the codes may be others: a largest
+    # magnitude between 224 and 232 scales rounds to 224, which half the scale holds as 448)
+    again, same_rows = cache.clone(), torch.full_like(c, 9)
+    _lib.eg_mla_append_latent_q8(dims, *again.all(), co, ko, io, ints(table), pos, cu, st)
+    _lib.eg_mla_read_latent_q8(dims, *again.all(), ints(table), same_rows, None, None, pos, cu, st)
+    assert torch.equal(same_rows, co) and torch.equal(again.kr, cache.kr) and torch.equal(again.ids, cache.ids)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_of_every_kind_of_number(gpu_lib, dtype):
+    """Borders of the scale, ties, subnormal codes, signed zeros, the smallest and largest numbers, rows with
+    infinities and NaN."""
+    rows, base = [], 2.0 ** np.arange(-12, 12)
+    for top in (448, 449.0 if dtype == "fp32" else 450, 447, 1, 1.75, 1.7578125, 2.0 ** -100, 448 * 2.0 ** -100,
+                450 * 2.0 ** -100, 2.0 ** -126, 2.0 ** -133, 448 * 2.0 ** 119, 1.9921875 * 2.0 ** 127, 0.0, 57344, 57600):
+        r = np.zeros(64)
+        r[0] = top
+        r[1:25] = -top / 448 * base
+        r[25:49] = top / 448 * base * 1.0625   # halfway between two codes of the same exponent
+        r[49:57] = top / 448 * 2.0 ** -9 * (np.arange(8) + 0.5)   # halfway between subnormal codes
+        r[57:60] = [-0.0, top, -top]
+        rows.append(np.clip(r, -abs(top), abs(top)))
+    for bad in (np.inf, -np.inf, np.nan):
+        r = np.linspace(-1, 1, 64)
+        r[17] = bad
+        rows.append(r)
+    x = torch.tensor(np.array(rows), device="cuda").to(DT[dtype])
+    T = len(rows)
+    dims, c, kr, ids, table, at, cache = append_case([T], [0], 64, dtype, x=x)
+    before, st = cache.clone(), status_word()
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, ints(table), ints([0]), ints([0, T]), st)
+    assert_cache(cache, before, at, torch.ones(T, dtype=torch.bool, device="cuda"), c, kr, ids)
+    out = torch.empty_like(c)
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), ints(table), out, None, None, None, ints([0, T]), st)
+    assert bool(out[-3:].isnan().all()) and bool(out[:-3].isfinite().all()) and int(st) == 0
+
+
+@pytest.mark.parametrize("batch", [1, 2, 31, 32, 33, 1023, 1024, 1025, 5000])
+def test_tokens_find_their_sequences(gpu_lib, batch):
+    """Batches around the powers of 32 that the search walks by, empty sequences among them, rows behind the last."""
+    r = np.random.default_rng(batch)
+    lens = r.integers(0, 4, batch)
+    firsts = r.integers(0, 130, batch)
+    T, spare = int(lens.sum()), 37
+    dims, c, kr, ids, table, rows, cache = append_case(list(lens) + [spare], list(firsts) + [-1], 64, "bf16", seed=batch)
+    before, st = cache.clone(), status_word()
+    table, cu, pos = ints(table[:-1]), ints(offsets(lens)), ints(firsts)
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, table, pos, cu, st)
+    kept = torch.arange(T + spare, device="cuda") < T
+    assert_cache(cache, before, rows, kept, c, kr, ids)
+    co, ko, io = torch.full_like(c, 9), torch.full_like(kr, 9), torch.full_like(ids, 9)
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), table, co, ko, io, pos, cu, st)
+    assert torch.equal(ko[:T], kr[:T]) and torch.equal(io[:T], ids[:T]) and bool((co[T:] == 9).all())
+    assert bool((ko[T:] == 9).all()) and bool((io[T:] == 9).all())
+    q, qo = normal((T + spare, 1, 8), "fp32", batch), torch.full((T + spare, 1, 8), 9.0, device="cuda")
+    rd = _lib.make_dims(1, 0, 8, 128, 256, 100, dtype="fp32")
+    _lib.eg_mla_rope(rd, _lib.make_rope(), q, qo, None, None, pos, cu, st)
+    check_rope(qo[:T], q[:T], positions_of(lens, firsts), 8, "fp32", {})
+    assert bool((qo[T:] == 9).all()) and int(st) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_of_one_token_per_sequence_and_wider_rows(gpu_lib, dtype):
+    B, d_c = 70, 256
+    r = np.random.default_rng(3)
+    firsts = r.integers(-1, 300, B)
+    dims, c, kr, ids, table, rows, cache = append_case([1] * B, list(firsts), d_c, dtype)
+    wide = normal((B, 40 + d_c + 64), dtype, 8)
+    c, kr = wide[:, 40:40 + d_c], wide[:, 40 + d_c:]
+    before, st = cache.clone(), status_word()
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, ints(table), ints(firsts), None, st)
+    kept = torch.as_tensor(firsts >= 0, device="cuda")
+    assert_cache(cache, before, rows, kept, c, kr, ids)
+    out = torch.full_like(wide, 9)
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), ints(table), out[:, 40:40 + d_c], out[:, 40 + d_c:], None, ints(firsts),
+                               None, st)
+    assert torch.equal(out[kept][:, 40 + d_c:], kr[kept]) and bool((out[:, :40] == 9).all()) and bool((out[~kept] == 9).all())
+    # a cache without ids, and ids left as they were
+    none = Cache(cache.c8.shape[0], d_c, dtype, ids=False)
+    _lib.eg_mla_append_latent_q8(dims, *none.all(), c, kr, ids, ints(table), ints(firsts), None, st)
+    kept_ids = cache.ids.clone()
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, None, ints(table), ints(firsts), None, st)
+    assert torch.equal(cache.ids, kept_ids) and torch.equal(none.scale[none.scale != 3], cache.scale[cache.scale != 3])
+    assert int(st) == 0
+
+
+def test_pages_out_of_range_are_reported_and_skipped(gpu_lib):
+    lens, firsts = [70, 5, 10, 80], [0, 0, 120, 10]
+    dims, c, kr, ids, table, rows, cache = append_case(lens, firsts, 192, "bf16")
+    table[0, 1], table[1, 0] = -3, cache.c8.shape[0]
+    narrow = table[:, :2].copy()
+    narrow[2, 0] = 99999999   # not met: the sequence's tokens are in its second page
+    ok = np.concatenate([np.arange(70) < 64, np.zeros(5, bool), (120 + np.arange(10)) // P < 2, np.ones(80, bool)])
+    rows = np.array([narrow[b, p // P] * P + p % P if p // P < 2 else -1
+                     for b, (f, n) in enumerate(zip(firsts, lens)) for p in range(f, f + n)])
+    kept = torch.as_tensor(ok, device="cuda")
+    before, st = cache.clone(), status_word()
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, ints(narrow), ints(firsts), ints(offsets(lens)), st)
+    assert int(st) == RANGE
+    assert_cache(cache, before, rows[ok], kept, c, kr, ids)
+    co, ko, io = torch.full_like(c, 9), torch.full_like(kr, 9), torch.full_like(ids, 9)
+    st.zero_()
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), ints(narrow), co, ko, io, ints(firsts), ints(offsets(lens)), st)
+    assert int(st) == RANGE and torch.equal(ko[kept], kr[kept])
+    assert bool((co[~kept] == 9).all()) and bool((ko[~kept] == 9).all()) and bool((io[~kept] == 9).all())
+    # the same without a status word
+    _lib.eg_mla_read_latent_q8(dims, *cache.all(), ints(narrow), co, ko, io, ints(firsts), ints(offsets(lens)))
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ decode
+def quantised(dc, pages=None):
+    """The cache of an uploaded case in 8 bits, and the values it holds as a pool of the case's type."""
+    n = dc.c_pool.shape[0]
+    d_c = dc.c_pool.shape[-1]
+    cache = Cache(n, d_c, dc.dtype, dc.kr_pool.shape[-1])
+    table, cu = ints([range(n)]), ints([0, n * P])
+    rows, kr, ids = dc.c_pool.view(-1, d_c), dc.kr_pool.view(n * P, -1), dc.id_pool.view(-1)
+    _lib.eg_mla_append_latent_q8(dc.dims, *cache.all(), rows, kr, ids, table, ints([0]), cu, dc.status)
+    back = torch.empty_like(rows)
+    _lib.eg_mla_read_latent_q8(dc.dims, *cache.all(), table, back, None, None, None, cu, dc.status)
+    return cache, back.view(dc.c_pool.shape)
+
+
+def decode_q8(dc, cache, out=None, stream=None, workspace=None):
+    out = torch.full_like(dc.out, 9) if out is None else out
+    _lib.eg_mla_decode_q8(dc.dims, dc.q, *cache.all(), dc.block_table, dc.seq_lens, dc.max_seq_len, dc.gate_table,
+                          dc.ln_gamma, dc.ln_beta, dc.w_uk, dc.w_uv, out, dc.workspace if workspace is None else workspace,
+                          dc.num_splits, dc.status, stream)
+    return out
+
+
+def make(lens, d_c=256, gate="mul_ln", seed=11, splits=0, d_nope=128, d_v=128, vocab=3000):
+    dims = synth.Dims(num_heads=16, d_nope=d_nope, d_rope=64, d_v=d_v, d_c=d_c, page_size=64, vocab=vocab, dtype="bf16",
+                      gate=gate != "none", gate_op="mul_ln" if gate == "none" else gate)
+    case = synth.make_case("q8", dims, list(lens), seed=seed, latent_scale=0.5, layout="permuted", affine_ln=True, extra_pages=5)
+    dc = device.upload(case, num_splits=splits)
+    dc.append()
+    return case, dc
+
+
+def same(a, b):
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num())
+
+
+FORMS = [(256, "mul_ln"), (192, "mul_ln"), (256, "mul"), (192, "mul"), (256, "add_ln"), (192, "add_ln"), (256, "none"),
+         (192, "none"), (512, "none")]
+
+
+@pytest.mark.parametrize("d_c,gate", FORMS)
+@pytest.mark.parametrize("lens", [(1,), (0, 1, 2, 63, 64, 65, 0), (31, 32, 33, 96, 97, 700), (2000, 1, 130, 5, 640, 64, 64, 1, 300, 77, 0, 11)])
+def test_decode_equals_the_decode_over_what_it_holds(gpu_lib, d_c, gate, lens):
+    for splits in (1, 3, 152):
+        case, dc = make(lens, d_c, gate, splits=splits)
+        cache, back = quantised(dc)
+        got = decode_q8(dc, cache)
+        dc.c_pool.copy_(back)
+        want = dc.decode(out=torch.full_like(dc.out, 9))
+        assert torch.equal(got, want), splits
+        assert dc.read_status() == 0
+    ref_case = dataclasses.replace(case, c_pool=device.bf16_tensor_to_bits(back))
+    u = device.output_f64(got)
+    ref = orc.decode_absorbed(_no_append(ref_case))
+    assert np.linalg.norm(u - ref) <= 5e-3 * np.linalg.norm(ref)
+    assert (np.abs(u - ref) <= 1e-2 * np.maximum(1.0, np.abs(ref))).all()
+
+
+def _no_append(case):
+    """The case with its new token already in the pool (the pool is the device's after the append): the oracle
+    writes the token again, so it is given what the cache holds there."""
+    c_new = case.c_new.copy()
+    for b in range(case.batch):
+        n = int(case.seq_lens[b])
+        if n > 0:
+            page = int(case.block_table[b, (n - 1) // P])
+            c_new[b] = case.c_pool.reshape(-1, P, case.c_pool.shape[-1])[page, (n - 1) % P]
+    return dataclasses.replace(case, c_new=c_new)
+
+
+@pytest.mark.parametrize("batch,d_nope,d_v", [(9, 40, 136), (10, 128, 256), (33, 256, 8), (140, 72, 128)])
+def test_decode_of_batches_and_widths(gpu_lib, batch, d_nope, d_v):
+    """Fused and separate combine, absorption tiles, long and short sequences at once."""
+    lens = [(97 * b) % 400 + (3000 if b == 2 else 0) for b in range(batch)]
+    for d_c, gate in ((256, "mul_ln"), (512, "none")):
+        _, dc = make(lens, d_c, gate, d_nope=d_nope, d_v=d_v)
+        cache, back = quantised(dc)
+        got = decode_q8(dc, cache)
+        dc.c_pool.copy_(back)
+        assert torch.equal(got, dc.decode(out=torch.full_like(dc.out, 9))) and dc.read_status() == 0
+
+
+@pytest.mark.parametrize("H,dn,dr,dc_,gate", [(16, 128, 64, 256, "mul_ln"), (4, 32, 16, 64, "mul_ln"), (12, 64, 64, 128, "none"),
+                                              (3, 24, 8, 16, "add_ln"), (16, 32, 64, 512, "mul"), (7, 32, 4, 272, "mul_ln")])
+def test_decode_fp32(gpu_lib, H, dn, dr, dc_, gate):
+    lens = [0, 1, 64, 65, 700, 130, 3]
+    dims = synth.Dims(num_heads=H, d_nope=dn, d_rope=dr, d_v=dn, d_c=dc_, page_size=64, vocab=500, dtype="fp32",
+                      gate=gate != "none", gate_op="mul_ln" if gate == "none" else gate)
+    case = synth.make_case("q8f", dims, lens, seed=3, layout="permuted", affine_ln=True, extra_pages=3)
+    for splits in (1, 5, 152):
+        dc = device.upload(case, num_splits=splits)
+        dc.append()
+        cache, back = quantised(dc)
+        got = decode_q8(dc, cache)
+        dc.c_pool.copy_(back)
+        assert torch.equal(got, dc.decode(out=torch.full_like(dc.out, 9))) and dc.read_status() == 0
+    ref = orc.decode_absorbed(_no_append(dataclasses.replace(case, c_pool=back.cpu().numpy())))
+    u = got.double().cpu().numpy()
+    assert np.linalg.norm(u - ref) <= 1e-5 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("d_c,gate", FORMS)
+@pytest.mark.parametrize("power", [-90, -20, 0, 20, 60])
+def test_decode_of_small_and_large_scales_and_every_code(gpu_lib, d_c, gate, power):
+    """Every code under scales that need the second factor and that do not; what the values are decides nothing
+    here: both decodes meet the same ones."""
+    _, dc = make([200, 64, 130], d_c, gate)
+    n = dc.c_pool.shape[0]
+    cache = Cache(n, d_c, "bf16")
+    codes = torch.arange(n * P * d_c, device="cuda").mul(37).remainder(256).to(torch.uint8)
+    cache.c8.copy_(torch.where(codes & 0x7f == 0x7f, codes - 1, codes).view(n, P, d_c))
+    cache.scale.copy_(2.0 ** torch.randint(power - 4, power + 5, (n, P), device="cuda",
+                                           generator=torch.Generator(device="cuda").manual_seed(1)).double())
+    cache.kr.copy_(dc.kr_pool)
+    cache.ids.copy_(dc.id_pool)
+    table, cu = ints([range(n)]), ints([0, n * P])
+    back = torch.empty((n * P, d_c), dtype=torch.bfloat16, device="cuda")
+    _lib.eg_mla_read_latent_q8(dc.dims, *cache.all(), table, back, None, None, None, cu, dc.status)
+    value = torch.tensor(np.concatenate([GRID, [0], -GRID, [0]]), device="cuda")[cache.c8.long()] * cache.scale.double()[..., None]
+    assert torch.equal(back.double().view(n, P, d_c), value)
+    got = decode_q8(dc, cache)
+    dc.c_pool.copy_(back.view(n, P, d_c))
+    assert same(got, dc.decode(out=torch.full_like(dc.out, 9))) and dc.read_status() == 0
+
+
+@pytest.mark.parametrize("d_c,gate", [(256, "mul_ln"), (192, "add_ln"), (256, "none"), (512, "none")])
+def test_decode_with_nan_inside_and_behind(gpu_lib, d_c, gate):
+    """Scales and codes behind the sequences' ends are of no account; a NaN row is its own sequence's alone."""
+    _, dc = make([130, 70, 5], d_c, gate)
+    cache, _ = quantised(dc)
+    want = decode_q8(dc, cache)
+    other = cache.clone()
+    lens, table = dc.seq_lens.cpu().numpy(), dc.block_table.cpu().numpy()
+    used = torch.zeros(cache.scale.numel(), dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        for p in range(n):
+            used[int(table[b, p // P]) * P + p % P] = True
+    for fill in (float("nan"), float("inf"), -1.0, 3e38):
+        other.scale.view(-1)[~used] = fill
+        other.c8.view(-1, d_c)[~used] = 0x7f
+        assert torch.equal(decode_q8(dc, other), want)
+    other.scale.view(-1)[int(table[1, 0]) * P + 3] = float("nan")
+    got = decode_q8(dc, other)
+    assert bool(got[1].isnan().all()) and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+def test_decode_reports_bad_pages_and_ids(gpu_lib):
+    for d_c, gate in ((256, "mul_ln"), (512, "none")):
+        _, dc = make([130, 70, 5], d_c, gate)
+        cache, _ = quantised(dc)
+        want = decode_q8(dc, cache)
+        good = int(dc.block_table[0, 1])
+        for bad in (-1, cache.c8.shape[0], 2 ** 31 - 1):
+            dc.block_table[0, 1] = bad
+            decode_q8(dc, cache)
+            assert dc.read_status() == RANGE
+            dc.status.zero_()
+        dc.block_table[0, 1] = good
+        assert torch.equal(decode_q8(dc, cache), want) and dc.read_status() == 0
+        if gate != "none":
+            cache.ids[good, 3] = 3000
+            decode_q8(dc, cache)
+            assert dc.read_status() == RANGE
+
+
+def test_decode_over_pages_past_32_bits_of_a_pool(gpu_lib):
+    """Codes more than 2^32 bytes into their pool; append and read there too."""
+    _, dc = make([500, 130], 512, "none")
+    small, _ = quantised(dc)
+    want = decode_q8(dc, small)
+    n, far = small.c8.shape[0], 140000
+    big = Cache(far, 512, "bf16")
+    table, cu = ints([range(far - n, far)]), ints([0, n * P])
+    rows = dc.c_pool.view(-1, 512)
+    _lib.eg_mla_append_latent_q8(dc.dims, *big.all(), rows, dc.kr_pool.view(n * P, -1), dc.id_pool.view(-1), table, ints([0]),
+                                 cu, dc.status)
+    assert torch.equal(big.c8[far - n:], small.c8) and same(big.scale[far - n:], small.scale)
+    assert bool((big.c8[:far - n] == 0x33).all())
+    back = [torch.empty_like(rows) for _ in range(2)]
+    _lib.eg_mla_read_latent_q8(dc.dims, *big.all(), table, back[0], None, None, None, cu, dc.status)
+    _lib.eg_mla_read_latent_q8(dc.dims, *small.all(), ints([range(n)]), back[1], None, None, None, cu, dc.status)
+    assert same(back[0], back[1])
+    dc.block_table.add_(far - n)
+    assert torch.equal(decode_q8(dc, big), want) and dc.read_status() == 0
+
+
+def test_withheld_page_copy_times_out_with_a_status(gpu_lib):
+    for d_c, gate in ((256, "mul_ln"), (512, "none")):
+        _, dc = make([3000, 200], d_c, gate, splits=4)
+        cache, _ = quantised(dc)
+        want = decode_q8(dc, cache)
+        torch.cuda.synchronize()
+        _lib.eg_mla_debug_set_fault(1, 3, 20_000_000)
+        try:
+            decode_q8(dc, cache)
+            torch.cuda.synchronize()
+        finally:
+            _lib.eg_mla_debug_set_fault(-1)
+        assert dc.read_status() == _lib.EG_MLA_ERR_TIMEOUT
+        dc.status.zero_()
+        assert torch.equal(decode_q8(dc, cache), want) and dc.read_status() == 0
+
+
+# ------------------------------------------------------------------ streams, graphs, threads
+def states(seed=0):
+    """(call, outputs) of every call on tensors of its own."""
+    _, dc = make([700, 64, 3, 300], seed=seed)
+    cache, _ = quantised(dc)
+    lens, firsts = [50, 0, 33], [10, 3, 0]
+    dims, c, kr, ids, table, rows, fresh = append_case(lens, firsts, 256, "bf16", seed=seed)
+    q, k = normal((83, 16, 192), "bf16", seed), normal((83, 64), "bf16", seed + 1)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    out, rows_out = torch.zeros_like(dc.out), torch.zeros_like(c)
+    cu, pos, tab = ints(offsets(lens)), ints(firsts), ints(table)
+    _lib.eg_mla_append_latent_q8(dims, *fresh.all(), c, kr, ids, tab, pos, cu, dc.status)
+    again = Cache(fresh.c8.shape[0], 256, "bf16")
+    rope = _lib.make_rope()
+    torch.cuda.synchronize()
+    return {"rope": (lambda s=None: _lib.eg_mla_rope(dims, rope, q, qo, k, ko, pos, cu, dc.status, s), qo),
+            "append": (lambda s=None: _lib.eg_mla_append_latent_q8(dims, *again.all(), c, kr, ids, tab, pos, cu, dc.status, s),
+                       again.c8),
+            "read": (lambda s=None: _lib.eg_mla_read_latent_q8(dims, *fresh.all(), tab, rows_out, None, None, pos, cu,
+                                                               dc.status, s), rows_out),
+            "decode": (lambda s=None: decode_q8(dc, cache, out, s), out)}, dc
+
+
+@pytest.mark.parametrize("name", ["rope", "append", "read", "decode"])
+def test_calls_allocate_nothing_and_can_be_captured(gpu_lib, name):
+    calls, dc = states()
+    call, out = calls[name]
+    call()
+    torch.cuda.synchronize()
+    want = out.clone()
+    before = torch.cuda.mem_get_info()[0]
+    for _ in range(3):
+        call()
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == before
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+        call()
+    out.fill_(0x33 if name == "append" else 0)   # (as Cache was filled)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and dc.read_status() == 0
+
+
+@pytest.mark.parametrize("name", ["rope", "append", "read", "decode"])
+def test_two_threads_leave_each_other_alone(gpu_lib, name):
+    results = {}
+
+    def work(k):
+        torch.cuda.set_device(0)
+        calls, dc = states()
+        call, out = calls[name]
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                call(stream)
+        stream.synchronize()
+        results[k] = (out.clone(), dc.read_status())
+        torch.cuda.synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    (a, sa), (b, sb) = results[0], results[1]
+    assert sa == 0 and sb == 0 and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_calls_in_turn(gpu_lib, graph):
+    """Two problems in turn, every call of a step after the other without the host's pace, on one workspace and one
+    cache: rope feeds the append and the decode, whose results are those of each problem alone."""
+    d_c, B, steps = 256, 6, 20
+    dims = _lib.make_dims(16, 128, 64, 128, d_c, 500)
+    probs = []
+    for s in range(2):
+        probs.append(dict(q=normal((B, 16, 192), "bf16", s), k=normal((B, 64), "bf16", 10 + s), c=normal((B, d_c), "bf16", 20 + s),
+                          ids=ints(np.arange(B) + s), pos=ints([5 + s, 64, 127 - s, 0, 300, 63 + s])))
+    w = [normal((16, 128, d_c), "bf16", 30 + i, d_c ** -0.5) for i in range(2)]
+    gate = (normal((500, d_c), "bf16", 40) * 0.1 + 1, torch.ones(d_c, device="cuda"), torch.zeros(d_c, device="cuda"))
+    table = ints(np.arange(B * 5).reshape(B, 5))
+    cache, fill = Cache(B * 5, d_c, "bf16"), normal((B * 320, d_c), "bf16", 50, 0.5)
+    cu = ints([0, B * 320])
+    _lib.eg_mla_append_latent_q8(dims, *cache.all(), fill, normal((B * 320, 64), "bf16", 51), ints(np.arange(B * 320) % 500),
+                                 table.view(1, -1), ints([0]), cu)
+    first = cache.clone()
+    ws = torch.empty(_lib.eg_mla_decode_workspace_size(dims, B), dtype=torch.uint8, device="cuda")
+    qr, kr, out, st = torch.empty_like(probs[0]["q"]), torch.empty_like(probs[0]["k"]), torch.empty((B, 16, 128), dtype=torch.bfloat16, device="cuda"), status_word()
+    lens = ints([0] * B)
+    got = [torch.empty_like(out) for _ in range(steps)]
+
+    def step(i):
+        p = probs[i % 2]
+        for a, b in zip(cache.all(), first.all()):
+            a.copy_(b)
+        lens.copy_(p["pos"] + 1)
+        _lib.eg_mla_rope(dims, _lib.make_rope(), p["q"], qr, p["k"], kr, p["pos"], None, st)
+        _lib.eg_mla_append_latent_q8(dims, *cache.all(), p["c"], kr, p["ids"], table, p["pos"], None, st)
+        _lib.eg_mla_decode_q8(dims, qr, *cache.all(), table, lens, 320, *gate, *w, out, ws, dev_status=st)
+
+    want = []
+    for i in range(2):
+        ws.fill_(255)
+        step(i)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+
+    def run():
+        for i in range(steps):
+            step(i)
+            got[i].copy_(out)
+
+    if graph:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        for _ in range(3):
+            g.replay()
+    else:
+        run()
+    torch.cuda.synchronize()
+    assert int(st) == 0 and not torch.equal(want[0], want[1])
+    for i, g in enumerate(got):
+        assert torch.equal(g, want[i % 2]), i
+
+
+# ------------------------------------------------------------------ together
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(prompts=(1,), steps=1), dict(prompts=(64, 63, 700, 5), steps=70)])
+def test_example_agrees_with_the_cache_in_bf16(gpu_lib, kw):
+    """The loop over the cache in 8 bits against the same tokens' values in a bf16 cache (bit for bit), and against
+    the unrounded bf16 cache.  A code is off by at most 2^-4 of its value, evenly spread, so a latent by 2^-4 / sqrt(3) =
+    3.6e-2 relative in each entry; LayerNorm, weights and values pass on an error of that size at most, and the
+    attention's mean over several tokens makes it smaller."""
+    spec = importlib.util.spec_from_file_location("serve_q8", os.path.join(ROOT, "examples", "serve_q8.py"))
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    exact, rounded, all_free, status = mod.main(**kw)
+    assert exact and rounded <= 0.1 and all_free and status == 0
