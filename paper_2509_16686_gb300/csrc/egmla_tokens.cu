@@ -94,6 +94,15 @@ __device__ __forceinline__ float2 turn_cos_sin(uint64_t fraction, float m) {
   return make_float2(m * cs, m * sn);
 }
 
+// 16 bytes that are read once
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
 template <typename T>
 __device__ __forceinline__ float to_f32(T x) { return static_cast<float>(x); }
 template <typename T>
@@ -114,41 +123,160 @@ __device__ __forceinline__ float2 turned(float x, float y, float2 cs) {
   return make_float2(fmaf(x, cs.x, -(y * cs.y)), fmaf(x, cs.y, y * cs.x));
 }
 
+// One part of a head in registers: what is loaded before it is turned.
+template <typename T, bool HALF>
+struct RopeItem {
+  static constexpr int N = 16 / sizeof(T);
+  Vec<T> a, b;   // HALF: a unit of the first half and its partner in the second; else a alone
+  __device__ __forceinline__ void load(const uint4* row, int r, int half_units) {
+    a.raw = ld_stream(row + r);
+    if (HALF) b.raw = ld_stream(row + r + half_units);
+  }
+  __device__ __forceinline__ void turn_and_store(uint4* row, int r, int half_units, const float2* cs) {
+    if constexpr (HALF) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float2 t = turned(to_f32(a.v[i]), to_f32(b.v[i]), cs[r * N + i]);
+        a.v[i] = from_f32<T>(t.x);
+        b.v[i] = from_f32<T>(t.y);
+      }
+      row[r + half_units] = b.raw;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const float2 t = turned(to_f32(a.v[2 * i]), to_f32(a.v[2 * i + 1]), cs[r * (N / 2) + i]);
+        a.v[2 * i] = from_f32<T>(t.x);
+        a.v[2 * i + 1] = from_f32<T>(t.y);
+      }
+    }
+    row[r] = a.raw;
+  }
+};
+
+// The token's units of heads h0 .. h1 - 1 dealt to the lanes: item u is unit u % n of head
+// h0 + u / n, kept up without divisions as u grows by 32.
+struct Deal {
+  int h, r, n, dh, dr;
+  __device__ __forceinline__ Deal(int h0, int n, int lane) : h(h0 + lane / n), r(lane % n), n(n), dh(32 / n), dr(32 % n) {}
+  __device__ __forceinline__ void next() {
+    h += dh;
+    r += dr;
+    if (r >= n) {
+      r -= n;
+      ++h;
+    }
+  }
+};
+
 // A warp per token and part of its H + 1 heads (the last one is the key); blockIdx.y: the
-// part.  VEC: rows and their parts in 16-byte units.
-template <typename T, bool VEC>
+// part.  Rows, heads and their rotated parts consist of 16-byte units, each read once,
+// kUnroll of them in flight per lane, the first before the token's angles are known.  The
+// angles are taken once per warp and token, a pair per lane, and shared by all heads.
+template <typename T, bool HALF>
 __global__ void __launch_bounds__(kTokThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int kUnroll = 4;
+  __shared__ __align__(16) float2 table[kTokWarps][kMaxPairs];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int k = blockIdx.x * kTokWarps + warp;
+  grid_dependency_wait();
+  if (k >= a.tok.tokens) return;
+  constexpr int kBytes = sizeof(T);
+  const int heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
+  const int h0 = heads * part / parts, h1 = heads * (part + 1) / parts;
+  const int units = a.dr * kBytes / 16, items = HALF ? units / 2 : units;   // of a head's rotated part
+  const int nope = a.dn * kBytes / 16, stride = nope + units;
+  const uint4* q = reinterpret_cast<const uint4*>(a.q + k * a.q_stride);
+  const uint4* key = reinterpret_cast<const uint4*>(a.k + k * a.k_stride);
+  uint4* q_out = reinterpret_cast<uint4*>(a.q_out + k * a.q_out_stride);
+  uint4* key_out = reinterpret_cast<uint4*>(a.k_out + k * a.k_out_stride);
+  const int hq = a.q == nullptr ? a.H : h0;                       // first head there is
+  const int hend = a.k == nullptr ? min(h1, a.H) : h1;
+
+  RopeItem<T, HALF> item[kUnroll];
+  Deal first(hq, items, lane);
+  {
+    Deal d = first;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j, d.next())
+      if (d.h < hend) item[j].load(d.h < a.H ? q + d.h * stride + nope : key, d.r, items);
+  }
+  int b;
+  int64_t pos;
+  if (!find_token(a.tok, k, lane, b, pos)) return;
+  if (nope > 0 && !a.q_in_place && a.q != nullptr) {
+    Deal d(h0, nope, lane);
+    const int end = min(h1, a.H);
+    while (d.h < end) {
+      uint4 v[kUnroll];
+      Deal e = d;
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j, e.next())
+        if (e.h < end) v[j] = ld_stream(q + e.h * stride + e.r);
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j, d.next())
+        if (d.h < end) q_out[d.h * stride + d.r] = v[j];
+    }
+  }
+  float2* cs = table[warp];
+  for (int i = lane; i < a.dr / 2; i += 32) cs[i] = turn_cos_sin(static_cast<uint64_t>(pos) * a.turn[i], a.magnitude);
+  __syncwarp();
+  while (first.h < hend) {
+    Deal d = first;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j, d.next())
+      if (d.h < hend) item[j].turn_and_store(d.h < a.H ? q_out + d.h * stride + nope : key_out, d.r, items, cs);
+    first = d;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j, d.next())
+      if (d.h < hend) item[j].load(d.h < a.H ? q + d.h * stride + nope : key, d.r, items);
+  }
+}
+
+// The same at any alignment and size, a pair per lane and turn.
+template <typename T>
+__global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ float2 table[kTokWarps][kMaxPairs];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = blockIdx.x * kTokWarps + warp;
-  const int pairs = a.dr / 2;
   grid_dependency_wait();
   int b;
   int64_t pos;
   if (k >= a.tok.tokens || !find_token(a.tok, k, lane, b, pos)) return;
-  for (int i = lane; i < pairs; i += 32)
-    table[warp][i] = turn_cos_sin(static_cast<uint64_t>(pos) * a.turn[i], a.magnitude);
+  const int pairs = a.dr / 2, heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
+  float2* cs = table[warp];
+  for (int i = lane; i < pairs; i += 32) cs[i] = turn_cos_sin(static_cast<uint64_t>(pos) * a.turn[i], a.magnitude);
   __syncwarp();
-  const float2* cs = table[warp];
-  const int heads = a.H + 1;
-  int h0 = heads * static_cast<int>(blockIdx.y) / static_cast<int>(gridDim.y);
-  const int h1 = heads * (static_cast<int>(blockIdx.y) + 1) / static_cast<int>(gridDim.y);
-  const int dq = a.dn + a.dr;
-  for (int h = h0; h < h1; ++h) {
-    const bool key = h == a.H;
-    if ((key ? a.k : a.q) == nullptr) continue;
-    const T* src = reinterpret_cast<const T*>(key ? a.k + k * a.k_stride : a.q + k * a.q_stride) + (key ? 0 : h * dq);
-    T* dst = reinterpret_cast<T*>(key ? a.k_out + k * a.k_out_stride : a.q_out + k * a.q_out_stride) + (key ? 0 : h * dq);
-    const int dn = key ? 0 : a.dn;
-    if (dn > 0 && !a.q_in_place)
-      for (int f = lane; f < dn; f += 32) dst[f] = src[f];
-    for (int i = lane; i < pairs; i += 32) {
-      const int x = dn + (a.half ? i : 2 * i), y = a.half ? x + pairs : x + 1;
-      const float2 r = turned(to_f32(src[x]), to_f32(src[y]), cs[i]);
-      dst[x] = from_f32<T>(r.x);
-      dst[y] = from_f32<T>(r.y);
-    }
+  const T* q = reinterpret_cast<const T*>(a.q + k * a.q_stride);
+  const T* key = reinterpret_cast<const T*>(a.k + k * a.k_stride);
+  T* q_out = reinterpret_cast<T*>(a.q_out + k * a.q_out_stride);
+  T* key_out = reinterpret_cast<T*>(a.k_out + k * a.k_out_stride);
+  const int h0 = heads * part / parts, h1 = heads * (part + 1) / parts;
+  const int dq = a.dn + a.dr, hend = a.k == nullptr ? min(h1, a.H) : h1;
+  if (a.dn > 0 && !a.q_in_place && a.q != nullptr)
+    for (Deal d(h0, a.dn, lane); d.h < min(h1, a.H); d.next()) q_out[d.h * dq + d.r] = q[d.h * dq + d.r];
+  for (Deal d(a.q == nullptr ? a.H : h0, pairs, lane); d.h < hend; d.next()) {
+    const int x = a.half ? d.r : 2 * d.r, y = a.half ? x + pairs : x + 1;
+    const T* src = d.h < a.H ? q + d.h * dq + a.dn : key;
+    T* dst = d.h < a.H ? q_out + d.h * dq + a.dn : key_out;
+    const float2 t = turned(to_f32(src[x]), to_f32(src[y]), cs[d.r]);
+    dst[x] = from_f32<T>(t.x);
+    dst[y] = from_f32<T>(t.y);
   }
+}
+
+// Parts that a token's heads are cut into: as many as leave every SM kRopeWarps warps.
+constexpr int kRopeWarps = 16;
+template <typename T>
+cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
+  auto on = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; };
+  const int e = sizeof(T);
+  const bool units = a.dn * e % 16 == 0 && a.dr * e % (a.half ? 32 : 16) == 0 && on(a.q, a.q_stride) &&
+                     on(a.q_out, a.q_out_stride) && on(a.k, a.k_stride) && on(a.k_out, a.k_out_stride);
+  const int want = (kSms * kRopeWarps - 1) / a.tok.tokens + 1;
+  const dim3 grid((a.tok.tokens + kTokWarps - 1) / kTokWarps, want < a.H + 1 ? want : a.H + 1), block(kTokThreads);
+  if (!units) return launch_chained(rope_any_kernel<T>, grid, block, 0, st, a);
+  return a.half ? launch_chained(rope_kernel<T, true>, grid, block, 0, st, a)
+                : launch_chained(rope_kernel<T, false>, grid, block, 0, st, a);
 }
 
 // ------------------------------------------------------------------ the cache in 8 bits
@@ -166,32 +294,67 @@ struct CacheArgs {
   int max_pages, num_pages, d_c, kr_bytes;
 };
 
-// Row of the pool of packed token k, the same in every lane; -1: none.
-__device__ __forceinline__ int64_t cache_row(const CacheArgs& a, int k, int lane) {
-  int b;
-  int64_t pos;
-  if (!find_token(a.tok, k, lane, b, pos)) return -1;
+// Rows of the pool of the packed tokens k0 .. k0 + T - 1: lane i < T gets token i's, -1 for none.
+template <int T>
+__device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) {
+  int b = 0;
+  int64_t pos = -1;
+  if (T > 1 && a.tok.cu != nullptr && a.tok.batch <= 32) {
+    // every offset in a lane: the tokens' sequences by a ballot each
+    const int end = lane < a.tok.batch ? __ldg(a.tok.cu + lane + 1) : INT32_MAX;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      const int n = __popc(__ballot_sync(0xffffffffu, end <= k0 + i && lane < a.tok.batch));
+      if (lane == i) b = n;
+    }
+    if (lane < T && k0 + lane < a.tok.tokens && b < a.tok.batch) {
+      const int first = __ldg(a.tok.cu + b), start = a.tok.positions != nullptr ? __ldg(a.tok.positions + b) : 0;
+      if (first > k0 + lane) report_status(a.tok.status, kStatusOutOfRange);
+      else if (start >= 0) pos = static_cast<int64_t>(start) + (k0 + lane) - first;
+    }
+  } else {
+    for (int i = 0; i < T && k0 + i < a.tok.tokens; ++i) {
+      int bi;
+      int64_t pi;
+      if (find_token(a.tok, k0 + i, lane, bi, pi) && lane == i) {
+        b = bi;
+        pos = pi;
+      }
+    }
+  }
+  if (pos < 0) return -1;
   const int64_t lp = pos / kPage;
   const int page = lp < a.max_pages ? __ldg(a.table + static_cast<size_t>(b) * a.max_pages + lp) : -1;
   if (page < 0 || page >= a.num_pages) {
-    if (lane == 0) report_status(a.tok.status, kStatusOutOfRange);
+    report_status(a.tok.status, kStatusOutOfRange);
     return -1;
   }
-  return static_cast<int64_t>(page) * kPage + pos % kPage;
+  return page * kPage + static_cast<int>(pos % kPage);   // (num_pages x 64 rows fit 32 bits)
 }
 
-// eight values of a packed row
+// eight values of a packed row as they are stored
 template <typename T>
-__device__ __forceinline__ void load8(const uint8_t* row, int unit, float (&x)[8]) {
-  constexpr int N = 16 / sizeof(T);
+struct Packed8 {
+  static constexpr int N = 16 / sizeof(T);
+  Vec<T> v[8 / N];
+  __device__ __forceinline__ void load(const uint8_t* row, int unit) {
 #pragma unroll
-  for (int j = 0; j < 8 / N; ++j) {
-    Vec<T> v;
-    v.raw = *reinterpret_cast<const uint4*>(row + (unit * (8 / N) + j) * 16);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[j * N + i] = to_f32(v.v[i]);
+    for (int j = 0; j < 8 / N; ++j) v[j].raw = ld_stream(reinterpret_cast<const uint4*>(row) + unit * (8 / N) + j);
   }
-}
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f32(v[i / N].v[i % N]);
+  }
+  // the fp32 bits of the largest magnitude (above those of infinity: a NaN)
+  __device__ __forceinline__ uint32_t most() const {
+    float x[8];
+    widen(x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    return m;
+  }
+};
 template <typename T>
 __device__ __forceinline__ void store8(uint8_t* row, int unit, const float (&x)[8]) {
   constexpr int N = 16 / sizeof(T);
@@ -204,68 +367,128 @@ __device__ __forceinline__ void store8(uint8_t* row, int unit, const float (&x)[
   }
 }
 
-// A warp per token, eight features of the latent a lane and turn.
-template <typename T>
+// A warp per T tokens, eight features of the latent a lane and turn (TURNS of them).  The
+// tokens' rows are requested before their places are looked up, a chain of three
+// dependent loads that T tokens share.
+template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_constant__ CacheArgs a) {
-  const int lane = threadIdx.x & 31, k = blockIdx.x * kTokWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
   grid_dependency_wait();
-  if (k >= a.tok.tokens) return;
-  const int units = a.d_c / 8;   // at most 64
-  const uint8_t* src = a.c_rows + k * a.c_stride;
-  float x[2][8] = {};
-  uint32_t most = 0;
+  if (k0 >= a.tok.tokens) return;
+  const int units = a.d_c / 8, kru = a.kr_bytes / 16;
+  Packed8<E> x[T][TURNS];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (lane + 32 * j < units) load8<T>(src, lane + 32 * j, x[j]);
+  for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[j][i]) & 0x7fffffffu);
-  }
-  const int64_t row = cache_row(a, k, lane);
-  if (row < 0) return;
-  most = __reduce_max_sync(0xffffffffu, most);
-  float scale, inverse;
-  q8_scale(most, scale, inverse);
-  uint2* dst = reinterpret_cast<uint2*>(a.c8 + row * a.d_c);
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (lane + 32 * j < units) {
-      uint32_t w[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        w[i] = q8_encode2(x[j][4 * i] * inverse, x[j][4 * i + 1] * inverse) |
-               q8_encode2(x[j][4 * i + 2] * inverse, x[j][4 * i + 3] * inverse) << 16;
-      dst[lane + 32 * j] = make_uint2(w[0], w[1]);
+    for (int j = 0; j < TURNS; ++j) {
+      x[t][j] = Packed8<E>{};
+      if (k0 + t < a.tok.tokens && lane + 32 * j < units) x[t][j].load(a.c_rows + (k0 + t) * a.c_stride, lane + 32 * j);
     }
-  for (int u = lane; u < a.kr_bytes / 16; u += 32)
-    reinterpret_cast<uint4*>(a.kr + row * a.kr_bytes)[u] = reinterpret_cast<const uint4*>(a.kr_rows + k * a.kr_stride)[u];
-  if (lane == 0) {
-    a.scale[row] = scale;
-    if (a.ids != nullptr && a.id_rows != nullptr) a.ids[row] = a.id_rows[k];
+  const int row = cache_rows<T>(a, k0, lane);
+  float own_scale = 0.f;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j) most = max(most, x[t][j].most());
+    most = __reduce_max_sync(0xffffffffu, most);
+    const int r = __shfl_sync(0xffffffffu, row, t);
+    if (r < 0) continue;
+    float scale, inverse;
+    q8_scale(most, scale, inverse);
+    if (lane == t) own_scale = scale;
+    uint2* dst = reinterpret_cast<uint2*>(a.c8 + static_cast<size_t>(r) * a.d_c);
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j)
+      if (lane + 32 * j < units) {
+        float v[8];
+        x[t][j].widen(v);
+        uint32_t w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          w[i] = q8_encode2(v[4 * i] * inverse, v[4 * i + 1] * inverse) |
+                 q8_encode2(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse) << 16;
+        dst[lane + 32 * j] = make_uint2(w[0], w[1]);
+      }
+  }
+  if (lane < T && row >= 0) {
+    a.scale[row] = own_scale;
+    if (a.ids != nullptr && a.id_rows != nullptr) a.ids[row] = a.id_rows[k0 + lane];
+  }
+  Deal d(0, kru, lane);
+  for (int u = 0; u < T * kru; u += 32, d.next()) {   // (every lane to the end, for the shuffle)
+    const int r = __shfl_sync(0xffffffffu, row, d.h < T ? d.h : 0);
+    if (d.h < T && r >= 0)
+      reinterpret_cast<uint4*>(a.kr + static_cast<size_t>(r) * a.kr_bytes)[d.r] =
+          ld_stream(reinterpret_cast<const uint4*>(a.kr_rows + (k0 + d.h) * a.kr_stride) + d.r);
   }
 }
 
-template <typename T>
+// A warp per T tokens, likewise.
+template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) read_q8_kernel(const __grid_constant__ CacheArgs a) {
-  const int lane = threadIdx.x & 31, k = blockIdx.x * kTokWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
   grid_dependency_wait();
-  if (k >= a.tok.tokens) return;
-  const int64_t row = cache_row(a, k, lane);
-  if (row < 0) return;
-  const float scale = __ldg(a.scale + row);
-  const uint2* src = reinterpret_cast<const uint2*>(a.c8 + row * a.d_c);
-  for (int u = lane; u < a.d_c / 8; u += 32) {
-    const uint2 w = src[u];
-    float x[8];
-    q8_decode4(w.x, x);
-    q8_decode4(w.y, x + 4);
+  if (k0 >= a.tok.tokens) return;
+  const int units = a.d_c / 8, kru = a.kr_bytes / 16;
+  const int row = cache_rows<T>(a, k0, lane);
+  const float own_scale = lane < T && row >= 0 ? __ldg(a.scale + row) : 0.f;
+  uint2 w[T][TURNS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= scale;
-    store8<T>(a.c_rows + k * a.c_stride, u, x);
+  for (int t = 0; t < T; ++t) {
+    const int r = __shfl_sync(0xffffffffu, row, t);
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j)
+      if (r >= 0 && lane + 32 * j < units)
+        w[t][j] = __ldg(reinterpret_cast<const uint2*>(a.c8 + static_cast<size_t>(r) * a.d_c) + lane + 32 * j);
   }
-  if (a.kr_rows != nullptr)
-    for (int u = lane; u < a.kr_bytes / 16; u += 32)
-      reinterpret_cast<uint4*>(a.kr_rows + k * a.kr_stride)[u] = reinterpret_cast<const uint4*>(a.kr + row * a.kr_bytes)[u];
-  if (lane == 0 && a.id_rows != nullptr) a.id_rows[k] = a.ids[row];
+  if (a.kr_rows != nullptr) {
+    Deal d(0, kru, lane);
+    for (int u = 0; u < T * kru; u += 32, d.next()) {   // (every lane to the end, for the shuffle)
+      const int r = __shfl_sync(0xffffffffu, row, d.h < T ? d.h : 0);
+      if (d.h < T && r >= 0)
+        reinterpret_cast<uint4*>(a.kr_rows + (k0 + d.h) * a.kr_stride)[d.r] =
+            ld_stream(reinterpret_cast<const uint4*>(a.kr + static_cast<size_t>(r) * a.kr_bytes) + d.r);
+    }
+  }
+  if (lane < T && row >= 0 && a.id_rows != nullptr) a.id_rows[k0 + lane] = a.ids[row];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int r = __shfl_sync(0xffffffffu, row, t);
+    const float scale = __shfl_sync(0xffffffffu, own_scale, t);
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j)
+      if (r >= 0 && lane + 32 * j < units) {
+        float x[8];
+        q8_decode4(w[t][j].x, x);
+        q8_decode4(w[t][j].y, x + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= scale;
+        store8<E>(a.c_rows + (k0 + t) * a.c_stride, lane + 32 * j, x);
+      }
+  }
+}
+
+// Tokens per warp: one while that leaves every SM no more than kTokFew warps, so that the
+// fewest tokens wait for one another; else T.
+constexpr int kTokFew = 16;
+template <int T, typename F>
+cudaError_t launch_tokens(const CacheArgs& a, cudaStream_t st, F&& kernel) {
+  const bool few = a.tok.tokens <= kSms * kTokFew;
+  const int per_block = kTokWarps * (few ? 1 : T);
+  return launch_chained(kernel(few), dim3((a.tok.tokens + per_block - 1) / per_block), dim3(kTokThreads), 0, st, a);
+}
+template <typename E>
+cudaError_t launch_append_q8(const CacheArgs& a, cudaStream_t st) {
+  if (a.d_c <= 256)
+    return launch_tokens<4>(a, st, [](bool few) { return few ? append_q8_kernel<E, 1, 1> : append_q8_kernel<E, 4, 1>; });
+  return launch_tokens<4>(a, st, [](bool few) { return few ? append_q8_kernel<E, 1, 2> : append_q8_kernel<E, 4, 2>; });
+}
+template <typename E>
+cudaError_t launch_read_q8(const CacheArgs& a, cudaStream_t st) {
+  if (a.d_c <= 256)
+    return launch_tokens<8>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 1> : read_q8_kernel<E, 8, 1>; });
+  return launch_tokens<8>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 2> : read_q8_kernel<E, 8, 2>; });
 }
 
 // ------------------------------------------------------------------ arguments
@@ -274,11 +497,10 @@ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 // the common part of the three calls; EG_MLA_OK or the error code
 int check_packed(const int32_t* cu, const int32_t* positions, int32_t batch, int32_t tokens) {
   if (batch < 0 || tokens < 0) return EG_MLA_ERR_INVALID_ARG;
+  if (tokens > INT32_MAX - 256) return EG_MLA_ERR_UNSUPPORTED;   // (a block's tokens are counted in 32 bits)
   if (cu == nullptr && (tokens != batch || (positions == nullptr && tokens > 0))) return EG_MLA_ERR_INVALID_ARG;
   return EG_MLA_OK;
 }
-
-unsigned token_blocks(int32_t tokens) { return static_cast<unsigned>((static_cast<int64_t>(tokens) + kTokWarps - 1) / kTokWarps); }
 
 int to_status(cudaError_t e) { return e == cudaSuccess ? EG_MLA_OK : EG_MLA_ERR_CUDA; }
 
@@ -410,11 +632,8 @@ int eg_mla_rope(const eg_mla_dims* dims, const eg_mla_rope_dims* rope, const voi
   a.half = rope->layout == EG_MLA_ROPE_HALF;
   a.q_in_place = q == q_out;
   a.k_in_place = k == k_out;
-  const dim3 grid(token_blocks(tokens), 1);
   auto* st = static_cast<cudaStream_t>(stream);
-  return to_status(dims->dtype == EG_MLA_BF16
-                       ? launch_chained(rope_kernel<__nv_bfloat16, false>, grid, dim3(kTokThreads), 0, st, a)
-                       : launch_chained(rope_kernel<float, false>, grid, dim3(kTokThreads), 0, st, a));
+  return to_status(dims->dtype == EG_MLA_BF16 ? launch_rope<__nv_bfloat16>(a, st) : launch_rope<float>(a, st));
 }
 
 int eg_mla_append_latent_q8(const eg_mla_dims* dims, void* c8_pool, float* scale_pool, void* krope_pool,
@@ -428,10 +647,8 @@ int eg_mla_append_latent_q8(const eg_mla_dims* dims, void* c8_pool, float* scale
                             dev_status);
   if (rc != EG_MLA_OK || tokens == 0 || batch == 0) return rc;
   if (krope_new == nullptr) return EG_MLA_ERR_INVALID_ARG;
-  const dim3 grid(token_blocks(tokens)), block(kTokThreads);
   auto* st = static_cast<cudaStream_t>(stream);
-  return to_status(dims->dtype == EG_MLA_BF16 ? launch_chained(append_q8_kernel<__nv_bfloat16>, grid, block, 0, st, a)
-                                              : launch_chained(append_q8_kernel<float>, grid, block, 0, st, a));
+  return to_status(dims->dtype == EG_MLA_BF16 ? launch_append_q8<__nv_bfloat16>(a, st) : launch_append_q8<float>(a, st));
 }
 
 int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const float* scale_pool,
@@ -445,10 +662,8 @@ int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const fl
                             dev_status);
   if (rc != EG_MLA_OK || tokens == 0 || batch == 0) return rc;
   if (ids_out != nullptr && id_pool == nullptr) return EG_MLA_ERR_INVALID_ARG;
-  const dim3 grid(token_blocks(tokens)), block(kTokThreads);
   auto* st = static_cast<cudaStream_t>(stream);
-  return to_status(dims->dtype == EG_MLA_BF16 ? launch_chained(read_q8_kernel<__nv_bfloat16>, grid, block, 0, st, a)
-                                              : launch_chained(read_q8_kernel<float>, grid, block, 0, st, a));
+  return to_status(dims->dtype == EG_MLA_BF16 ? launch_read_q8<__nv_bfloat16>(a, st) : launch_read_q8<float>(a, st));
 }
 
 }  // extern "C"
