@@ -254,56 +254,76 @@ def _shaped(t: Optional[torch.Tensor], shape: tuple, name: str) -> None:
 
 
 _MODEL_DTYPES = {EG_MLA_BF16: torch.bfloat16, EG_MLA_FP32: torch.float32}
+_CODES = (torch.float8_e4m3fn, torch.uint8)
 
 
-def _typed(t: Optional[torch.Tensor], dtypes, name: str) -> None:
-    if t is not None and t.dtype not in dtypes:
-        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
-
-
-def _token_rows(t: Optional[torch.Tensor], shape: tuple, dtype, name: str):
-    """Pointer and token stride of rows [tokens, ...] that are dense but for the first dimension."""
-    if t is None:
-        return None, 0
+def _refuse(t: torch.Tensor, shape: tuple, dtypes, dev: int, name: str) -> None:
+    """The error of a tensor that is not what a call takes."""
     _shaped(t, shape, name)
-    _typed(t, (dtype,), name)
-    if not t.is_cuda:
-        raise ValueError("device tensor expected")
-    width = 1
-    for n, step in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
-        if n > 1 and step != width:
-            raise ValueError(f"{name}: rows that are dense expected")
-        width *= n
-    stride = t.stride(0) if shape[0] > 1 else width
-    if stride < width:
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on another device than the others")
+    raise ValueError(f"{name}: contiguous tensor expected")
+
+
+def _arg(t: torch.Tensor, shape: tuple, dtype, dev: int, name: str) -> int:
+    """Pointer of a tensor of this shape, type and device (one expression: the checks of a call's nine tensors
+    take as long as its launch)."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, shape, (dtype,), dev, name)
+
+
+def _rows(t: torch.Tensor, shape: tuple, dtype, dev: int, name: str) -> tuple:
+    """Pointer and token stride of rows [tokens, ...] that are dense but for the first dimension."""
+    width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    step = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        _refuse(t, shape, (dtype,), dev, name)
+    if step[-1] != 1 or (len(shape) == 3 and step[1] != shape[2]):   # (of a dimension of one entry the step is of no account)
+        dense = 1
+        for n, k in zip(reversed(shape[1:]), reversed(step[1:])):
+            if n > 1 and k != dense:
+                raise ValueError(f"{name}: rows that are dense expected")
+            dense *= n
+    if shape[0] <= 1:
+        return t.data_ptr(), width
+    if step[0] < width:
         raise ValueError(f"{name}: rows that overlap")
-    return t.data_ptr(), stride
+    return t.data_ptr(), step[0]
 
 
-def _packed(tokens: int, positions, cu_seqlens) -> tuple:
-    """(cu_seqlens, positions, batch) of packed tokens as pointers, their shapes checked."""
-    if cu_seqlens is None and positions is None:
-        raise ValueError("positions or cu_seqlens expected")
-    batch = cu_seqlens.shape[0] - 1 if cu_seqlens is not None else tokens
-    _shaped(positions, (batch,), "positions")
-    for name, t in (("positions", positions), ("cu_seqlens", cu_seqlens)):
-        _typed(t, (torch.int32,), name)
-    return _ptr(cu_seqlens), _ptr(positions), batch
+def _packed(tokens: int, positions, cu_seqlens, dev: int) -> tuple:
+    """(cu_seqlens, positions, batch) of packed tokens as pointers."""
+    if cu_seqlens is None:
+        if positions is None:
+            raise ValueError("positions or cu_seqlens expected")
+        return None, _arg(positions, (tokens,), torch.int32, dev, "positions"), tokens
+    batch = cu_seqlens.shape[0] - 1
+    return (_arg(cu_seqlens, (batch + 1,), torch.int32, dev, "cu_seqlens"),
+            None if positions is None else _arg(positions, (batch,), torch.int32, dev, "positions"), batch)
 
 
-def _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table) -> tuple:
-    """Pointers of a cache in 8 bits, its shapes and types checked."""
-    pages = c8_pool.shape[0]
-    _shaped(c8_pool, (pages, dims.page_size, dims.d_c), "c8_pool")
-    _shaped(scale_pool, (pages, dims.page_size), "scale_pool")
-    _shaped(krope_pool, (pages, dims.page_size, dims.d_rope), "krope_pool")
-    _shaped(id_pool, (pages, dims.page_size), "id_pool")
-    _typed(c8_pool, (torch.float8_e4m3fn, torch.uint8), "c8_pool")
-    _typed(scale_pool, (torch.float32,), "scale_pool")
-    _typed(krope_pool, (_MODEL_DTYPES.get(dims.dtype),), "krope_pool")
-    for name, t in (("id_pool", id_pool), ("block_table", block_table)):
-        _typed(t, (torch.int32,), name)
-    return _ptr(c8_pool), _ptr(scale_pool), _ptr(krope_pool), _ptr(id_pool)
+def _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev: int) -> tuple:
+    """Pointers of a cache in 8 bits."""
+    pages, size = c8_pool.shape[0], dims.page_size
+    codes = c8_pool.dtype
+    if codes not in _CODES:
+        _refuse(c8_pool, (pages, size, dims.d_c), _CODES, dev, "c8_pool")
+    return (_arg(c8_pool, (pages, size, dims.d_c), codes, dev, "c8_pool"),
+            _arg(scale_pool, (pages, size), torch.float32, dev, "scale_pool"),
+            _arg(krope_pool, (pages, size, dims.d_rope), dtype, dev, "krope_pool"),
+            None if id_pool is None else _arg(id_pool, (pages, size), torch.int32, dev, "id_pool"))
+
+
+def _stream_on(dev: int, stream) -> int:
+    """Handle of the stream for tensors of this device, which has to be the current one."""
+    if dev < 0:
+        raise ValueError("device tensor expected")
+    if dev != torch.cuda.current_device():
+        raise ValueError("tensors on another device than the current one")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _stream(stream) -> int:
@@ -482,60 +502,64 @@ def eg_mla_rope(dims: EgMlaDims, rope: EgMlaRopeDims, q, q_out, k, k_out, positi
     tokens may be apart (a slice of wider rows); q_out may be q, k_out k, and either pair None: see include/egmla.h."""
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q with q_out or k with k_out expected")
-    tokens = (q if q is not None else k).shape[0]
-    rows = []
-    for name, t, shape in (("q", q, (dims.num_heads, dims.d_nope + dims.d_rope)),
-                           ("q_out", q_out, (dims.num_heads, dims.d_nope + dims.d_rope)),
-                           ("k", k, (dims.d_rope,)), ("k_out", k_out, (dims.d_rope,))):
-        rows += _token_rows(t, (tokens, *shape), _MODEL_DTYPES.get(dims.dtype), name)
-    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
+    some, dtype = q if q is not None else k, _MODEL_DTYPES.get(dims.dtype)
+    tokens, dev, none = some.shape[0], some.get_device(), (None, 0)
+    heads, keys = (tokens, dims.num_heads, dims.d_nope + dims.d_rope), (tokens, dims.d_rope)
+    rows = (*(none if q is None else _rows(q, heads, dtype, dev, "q")),
+            *(none if q is None else _rows(q_out, heads, dtype, dev, "q_out")),
+            *(none if k is None else _rows(k, keys, dtype, dev, "k")),
+            *(none if k is None else _rows(k_out, keys, dtype, dev, "k_out")))
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens, dev)
     _check(load().eg_mla_rope(ctypes.byref(dims), ctypes.byref(rope), *rows, cu, pos, batch, tokens, _ptr(dev_status),
-                              _stream(stream)), "eg_mla_rope")
+                              _stream_on(dev, stream)), "eg_mla_rope")
 
 
 def eg_mla_append_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_pool, c_new, krope_new, ids_new,
                             block_table, positions, cu_seqlens=None, dev_status=None, stream=None) -> None:
     """New tokens into a cache that holds the latent in 8 bits (c8_pool e4m3 or its bytes), a token per sequence
     or packed by cu_seqlens; the rows of c_new and krope_new may be apart: see include/egmla.h."""
-    tokens, dtype = c_new.shape[0], _MODEL_DTYPES.get(dims.dtype)
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
-    rows = (*_token_rows(c_new, (tokens, dims.d_c), dtype, "c_new"),
-            *_token_rows(krope_new, (tokens, dims.d_rope), dtype, "krope_new"))
-    _shaped(ids_new, (tokens,), "ids_new")
-    _typed(ids_new, (torch.int32,), "ids_new")
-    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
-    _shaped(block_table, (batch, block_table.shape[1]), "block_table")
-    _check(load().eg_mla_append_latent_q8(
-        ctypes.byref(dims), *cache, *rows, _ptr(ids_new), cu, pos, _ptr(block_table), block_table.shape[1], batch, tokens,
-        c8_pool.shape[0], _ptr(dev_status), _stream(stream)), "eg_mla_append_latent_q8")
+    tokens, dtype, dev = c_new.shape[0], _MODEL_DTYPES.get(dims.dtype), c8_pool.get_device()
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
+    rows = (*_rows(c_new, (tokens, dims.d_c), dtype, dev, "c_new"),
+            *_rows(krope_new, (tokens, dims.d_rope), dtype, dev, "krope_new"))
+    ids = None if ids_new is None else _arg(ids_new, (tokens,), torch.int32, dev, "ids_new")
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens, dev)
+    width = block_table.shape[1]
+    table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
+    _check(load().eg_mla_append_latent_q8(ctypes.byref(dims), *cache, *rows, ids, cu, pos, table, width, batch, tokens,
+                                          c8_pool.shape[0], _ptr(dev_status), _stream_on(dev, stream)),
+           "eg_mla_append_latent_q8")
 
 
 def eg_mla_read_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_pool, block_table, c_out, krope_out,
                           ids_out, positions=None, cu_seqlens=None, dev_status=None, stream=None) -> None:
     """Cached tokens of a cache in 8 bits as packed rows (krope_out and ids_out may be None): see include/egmla.h."""
-    tokens, dtype = c_out.shape[0], _MODEL_DTYPES.get(dims.dtype)
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
-    rows = (*_token_rows(c_out, (tokens, dims.d_c), dtype, "c_out"),
-            *_token_rows(krope_out, (tokens, dims.d_rope), dtype, "krope_out"))
-    _shaped(ids_out, (tokens,), "ids_out")
-    _typed(ids_out, (torch.int32,), "ids_out")
-    cu, pos, batch = _packed(tokens, positions, cu_seqlens)
-    _shaped(block_table, (batch, block_table.shape[1]), "block_table")
-    _check(load().eg_mla_read_latent_q8(
-        ctypes.byref(dims), *cache, cu, pos, _ptr(block_table), block_table.shape[1], *rows, _ptr(ids_out), batch, tokens,
-        c8_pool.shape[0], _ptr(dev_status), _stream(stream)), "eg_mla_read_latent_q8")
+    tokens, dtype, dev = c_out.shape[0], _MODEL_DTYPES.get(dims.dtype), c8_pool.get_device()
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
+    rows = (*_rows(c_out, (tokens, dims.d_c), dtype, dev, "c_out"),
+            *((None, 0) if krope_out is None else _rows(krope_out, (tokens, dims.d_rope), dtype, dev, "krope_out")))
+    ids = None if ids_out is None else _arg(ids_out, (tokens,), torch.int32, dev, "ids_out")
+    cu, pos, batch = _packed(tokens, positions, cu_seqlens, dev)
+    width = block_table.shape[1]
+    table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
+    _check(load().eg_mla_read_latent_q8(ctypes.byref(dims), *cache, cu, pos, table, width, *rows, ids, batch, tokens,
+                                        c8_pool.shape[0], _ptr(dev_status), _stream_on(dev, stream)),
+           "eg_mla_read_latent_q8")
 
 
 def eg_mla_decode_q8(dims: EgMlaDims, q, c8_pool, scale_pool, krope_pool, id_pool, block_table, seq_lens, max_seq_len,
                      gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, workspace, num_splits=0, dev_status=None,
                      stream=None) -> None:
     """eg_mla_decode over a cache in 8 bits: see include/egmla.h."""
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, block_table)
+    dev, batch, width = c8_pool.get_device(), seq_lens.shape[0], block_table.shape[1]
+    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, _MODEL_DTYPES.get(dims.dtype), dev)
+    table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
+    lens = _arg(seq_lens, (batch,), torch.int32, dev, "seq_lens")
+    handle = _stream_on(dev, stream)
     _check(load().eg_mla_decode_q8(
-        ctypes.byref(dims), _ptr(q), *cache, _ptr(block_table), block_table.shape[1], _ptr(seq_lens), int(max_seq_len),
-        seq_lens.shape[0], c8_pool.shape[0], _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk), _ptr(w_uv),
-        _ptr(out), num_splits, _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(dev_status),
-        _stream(stream)), "eg_mla_decode_q8")
+        ctypes.byref(dims), _ptr(q), *cache, table, width, lens, int(max_seq_len), batch, c8_pool.shape[0],
+        _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk), _ptr(w_uv), _ptr(out), num_splits, _ptr(workspace),
+        workspace.nbytes, _ptr(dev_status), handle), "eg_mla_decode_q8")
 
 
 def make_layer_dims(n_embd: int, rope_theta: float = 10000.0, rms_eps: float = 0.0,

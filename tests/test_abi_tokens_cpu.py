@@ -176,27 +176,29 @@ def test_binding_checks_shapes_and_types():
             _lib.eg_mla_read_latent_q8(d, *args, table, c, k, pos, pos)
         with pytest.raises(ValueError, match=name):
             _lib.eg_mla_decode_q8(d, q, *args, table, pos, 100, c, None, None, c, c, q, c)
+    for name, bad in (("c_new", (c[:, :128], k, pos, table, pos)), ("krope_new", (c, k[:2], pos, table, pos)),
+                      ("ids_new", (c, k, pos.long(), table, pos)), ("block_table", (c, k, pos, table[:2], pos)),
+                      ("positions", (c, k, pos, table, pos[:2])), ("cu_seqlens", (c, k, pos, table, pos, pos.long()))):
+        with pytest.raises(ValueError, match=name):
+            _lib.eg_mla_append_latent_q8(d, c8, scale, kr, ids, *bad)
     with pytest.raises(ValueError, match="device"):
         _lib.eg_mla_append_latent_q8(d, c8, scale, kr, ids, c, k, pos, table, pos)
+    with pytest.raises(ValueError, match="device"):
+        _lib.eg_mla_decode_q8(d, q, c8, scale, kr, ids, table, pos, 100, c, None, None, c, c, q, c)
+    with pytest.raises(ValueError, match="device"):
+        _lib.eg_mla_rope(d, rope, q, q, k, k, pos)
 
 
 def test_token_rows_are_dense_but_for_the_tokens():
-    class Fake:
-        is_cuda = True
-
-        def __init__(self, t):
-            self.t = t
-
-        def __getattr__(self, name):
-            return getattr(self.t, name)
-
     def rows(t, shape):
-        return _lib._token_rows(Fake(t), shape, torch.float32, "x")[1]
+        return _lib._rows(t, shape, torch.float32, -1, "x")[1]   # (-1: the CPU)
     wide = torch.zeros(5, 100)
     assert rows(wide[:, 4:64].unflatten(1, (3, 20)), (5, 3, 20)) == 100
     assert rows(wide[:1, :60], (1, 60)) == 60
     assert rows(wide[:, :1].unsqueeze(-1), (5, 1, 1)) == 100
+    assert rows(wide[:, :20].unsqueeze(1), (5, 1, 20)) == 100
     for bad, shape in ((wide.t()[:60], (60, 5)), (wide[:, ::2], (5, 50)), (wide[:1].expand(5, 100), (5, 100)),
-                       (wide[:, :60].unflatten(1, (3, 20))[:, :, :10], (5, 3, 10))):
+                       (wide[:, :60].unflatten(1, (3, 20))[:, :, :10], (5, 3, 10)), (wide[:, ::2].unsqueeze(1), (5, 1, 50)),
+                       (wide, (5, 99)), (wide.double(), (5, 100))):
         with pytest.raises(ValueError):
             rows(bad, shape)
