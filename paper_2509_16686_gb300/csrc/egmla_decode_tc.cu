@@ -411,6 +411,16 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<uint32_t*>(&z);
 }
 
+// s += z and q += z^2 of a pair, in fp32 straight from the bf16 values
+__device__ __forceinline__ void sum_bf16x2(uint32_t z, float2& s, float2& q) {
+  asm("{\n\t.reg .b16 lo, hi, one;\n\t"
+      "mov.b16 one, 0x3f80;\n\tmov.b32 {lo, hi}, %4;\n\t"
+      "fma.rn.f32.bf16 %0, lo, one, %0;\n\tfma.rn.f32.bf16 %1, hi, one, %1;\n\t"
+      "fma.rn.f32.bf16 %2, lo, lo, %2;\n\tfma.rn.f32.bf16 %3, hi, hi, %3;\n\t}"
+      : "+f"(s.x), "+f"(s.y), "+f"(q.x), "+f"(q.y)
+      : "r"(z));
+}
+
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   __nv_bfloat162 z = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&z);
@@ -1073,9 +1083,161 @@ __global__ void __launch_bounds__(kThreads, 1)
     Tile t, t1;
     bool have = w.next(t);
     bool have1 = have && w.next(t1);
+    if constexpr (Q8 && GATE) {
+      // A cache in 8 bits: the gate warps take the longest of all roles here (widening a
+      // code costs as much as gating and summing it), so nothing of theirs waits at a tile's
+      // start: the next tile's codes and gate rows take the place of this tile's, column by
+      // column, as soon as these are used (its copies have landed long before), its ids
+      // and scales before that.
+      uint4 g[C::NCH][2];
+      float scale = 0.f;
+      auto raw_of = [&](int jj) { return smem + C::OFF_RAW + (jj % C::RING) * C::RSLOT + C::PCHUNK + row * D_C + 16 * pp; };
+      auto scale_of = [&](int jj) {
+        return reinterpret_cast<const float*>(smem + C::OFF_META + (jj % C::RING) * C::RMETA)[row];
+      };
+      if (have) have = warp_wait(smem_u32(&bars.full[0]), 0, abort_flag, wait_ns);
+      bool loaded = false;
+      for (int j = 0; have; ++j) {
+        const int slot = j % C::NS;
+        tr.mark(0, j);
+        if (!loaded) {
+          if (!warp_wait(smem_u32(&bars.full[j % C::RING]), (j / C::RING) & 1, abort_flag, wait_ns)) break;
+          load_g(slot_id(j, t), g);
+          scale = scale_of(j);
+#pragma unroll
+          for (int fc = 0; fc < C::NCH; ++fc) codes[fc] = *reinterpret_cast<const uint4*>(raw_of(j) + fc * 64);
+        }
+        tr.mark(1, j);
+        widen.set(scale);
+        const bool more = widen.unfinished();
+        loaded = !GATE_ADD && have1 && warp_test(smem_u32(&bars.full[(j + 1) % C::RING]), ((j + 1) / C::RING) & 1);
+        const uint8_t* raw_next = raw_of(j + 1);
+        const __nv_bfloat16* g_next = p.gate_table;
+        if (loaded) {
+          g_next = g_row(slot_id(j + 1, t1));
+          scale = scale_of(j + 1);
+        }
+        auto load_next = [&](int fc) {
+          if (loaded) {
+            ldg_32_na_hint(g_next + fc * 64, pol_keep, g[fc][0], g[fc][1]);
+            codes[fc] = *reinterpret_cast<const uint4*>(raw_next + fc * 64);
+          }
+        };
+        auto latent = [&](int fc, int h) {
+          uint4 c = widen.unit(h ? codes[fc].z : codes[fc].x, h ? codes[fc].w : codes[fc].y);
+          if (more) widen.finish(c);
+          return c;
+        };
+        // the latent slot of the tile (output MMAs of the tile NS before it complete)
+        if (!warp_wait(smem_u32(&bars.zfree[slot]), ((j / C::NS) & 1) ^ 1, abort_flag, wait_ns)) break;
+        tr.mark(5, j);
+        uint8_t* zpage = smem + slot * C::SLOT;
+        float* st = reinterpret_cast<float*>(smem + C::OFF_STAT + slot * C::STAT_BYTES);
+        const bool full_page = t.ntok == C::TOK, valid = row < t.ntok;
+        float2 s1 = make_float2(0.f, 0.f), s2 = s1, a1 = s1, a2 = s1;
+        auto row_sums = [&](float& sum1, float& sum2) {
+          s1 = __fadd2_rn(s1, a1);
+          s2 = __fadd2_rn(s2, a2);
+          sum1 = s1.x + s1.y;
+          sum2 = s2.x + s2.y;
+#pragma unroll
+          for (int o = 1; o < kGateLanesPerRow; o <<= 1) {
+            sum1 += __shfl_xor_sync(0xffffffffu, sum1, o);
+            sum2 += __shfl_xor_sync(0xffffffffu, sum2, o);
+          }
+        };
+        constexpr float inv_dc = 1.f / D_C;
+        if constexpr (GATE_ADD) {
+          // (as below without the 8 bits: centred before the rounding; the same sums)
+#pragma unroll
+          for (int fc = 0; fc < C::NCH; ++fc)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 c4 = latent(fc, h);
+              const uint32_t* cw = reinterpret_cast<const uint32_t*>(&c4);
+              const uint32_t* gw2 = reinterpret_cast<const uint32_t*>(&g[fc][h]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 zf = __fadd2_rn(unpack_bf16x2(cw[k]), unpack_bf16x2(gw2[k]));
+                s1 = __fadd2_rn(s1, zf);
+                s2 = __ffma2_rn(zf, zf, s2);
+              }
+            }
+          float sum1, sum2;
+          row_sums(sum1, sum2);
+          const float mu = sum1 * inv_dc;
+          const float r = rsqrtf(fmaxf(sum2 * inv_dc - mu * mu, 0.f) + p.eps);
+#pragma unroll
+          for (int fc = 0; fc < C::NCH; ++fc) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 c4 = latent(fc, h);
+              const uint32_t* cw = reinterpret_cast<const uint32_t*>(&c4);
+              const uint32_t* gw2 = reinterpret_cast<const uint32_t*>(&g[fc][h]);
+              uint4 z;
+              uint32_t* zw = reinterpret_cast<uint32_t*>(&z);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 zf = __fadd2_rn(__fadd2_rn(unpack_bf16x2(cw[k]), unpack_bf16x2(gw2[k])), make_float2(-mu, -mu));
+                zw[k] = pack_bf16x2(zf.x, zf.y);
+              }
+              if (!full_page && !valid) z = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(zpage + unit_off(fc, h)) = z;
+            }
+            load_next(fc);
+          }
+          if (pp == 0) {
+            st[row] = 0.f;
+            st[kPage + row] = valid ? r : 1.f;
+          }
+        } else {
+#pragma unroll
+          for (int fc = 0; fc < C::NCH; ++fc) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint4 c4 = latent(fc, h);
+              uint4 z;
+              z.x = mul_bf16x2(c4.x, g[fc][h].x);
+              z.y = mul_bf16x2(c4.y, g[fc][h].y);
+              z.z = mul_bf16x2(c4.z, g[fc][h].z);
+              z.w = mul_bf16x2(c4.w, g[fc][h].w);
+              if (!full_page && !valid) z = make_uint4(0, 0, 0, 0);
+              if (GATE_LN) {
+                sum_bf16x2(z.x, s1, s2);
+                sum_bf16x2(z.y, a1, a2);
+                sum_bf16x2(z.z, s1, s2);
+                sum_bf16x2(z.w, a1, a2);
+              }
+              *reinterpret_cast<uint4*>(zpage + unit_off(fc, h)) = z;
+            }
+            load_next(fc);
+          }
+          tr.mark(6, j);
+          float mu = 0.f, r = 1.f;
+          if (GATE_LN) {
+            float sum1, sum2;
+            row_sums(sum1, sum2);
+            mu = sum1 * inv_dc;
+            r = rsqrtf(fmaxf(sum2 * inv_dc - mu * mu, 0.f) + p.eps);
+          }
+          if (pp == 0) {
+            st[row] = valid ? mu : 0.f;
+            st[kPage + row] = valid ? r : 1.f;
+          }
+        }
+        tr.mark(2, j);
+        fence_proxy_async_smem();
+        warp_arrive(smem_u32(&bars.zready[slot]));
+        tr.mark(3, j);
+        t = t1;
+        have = have1;
+        have1 = have1 && w.next(t1);
+      }
+      have = false;
+    }
     uint4 gcur[C::NCH][kGateUnits], gnext[C::NCH][kGateUnits];
     int id0 = 0;
-    if (GATE && have) {
+    if (!Q8 && GATE && have) {
       // the first tile's rows: its page must land first
       if (warp_wait(smem_u32(&bars.full[0]), 0, abort_flag, wait_ns)) {
         id0 = slot_id(0, t);
@@ -1142,9 +1304,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < kQCols; ++i) codes[i] = *reinterpret_cast<const uint4*>(raw + i * (C::NCH / kQCols) * 64);
           widen.set(scales[qrow]);
+          const bool more = widen.unfinished();
           if (!warp_wait(smem_u32(&bars.zfree[slot]), ((j / C::NS) & 1) ^ 1, abort_flag, wait_ns)) break;
-        }
-        if constexpr (Q8 && !GATE) {
 #pragma unroll
           for (int i = 0; i < kQCols; ++i) {
 #pragma unroll
@@ -1152,10 +1313,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               // (of a row shared by eight lanes, the second four write their units in
               // the other order, so that the eight meet different banks)
               const int hh = kQSubs > 1 ? h ^ qsub : h;
-              const uint32_t w0 = hh ? codes[i].z : codes[i].x, w1 = hh ? codes[i].w : codes[i].y;
-              uint4 z;
-              widen.four(w0, z.x, z.y);
-              widen.four(w1, z.z, z.w);
+              uint4 z = widen.unit(hh ? codes[i].z : codes[i].x, hh ? codes[i].w : codes[i].y);
+              if (more) widen.finish(z);
               if (qrow >= t.ntok) z = make_uint4(0, 0, 0, 0);
               *reinterpret_cast<uint4*>(cpage + (i * (C::NCH / kQCols) + qsub) * C::PCHUNK + qrow * 128 +
                                         (((2 * (lane % 4) + hh) ^ (qrow & 7)) << 4)) = z;
@@ -1169,15 +1328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int fc = 0; fc < C::NCH; ++fc)
 #pragma unroll
-            for (int h = 0; h < kGateUnits; ++h) {
-              if constexpr (Q8) {
-                uint4& c = cv[fc][h];
-                widen.four(h ? codes[fc].z : codes[fc].x, c.x, c.y);
-                widen.four(h ? codes[fc].w : codes[fc].y, c.z, c.w);
-              } else {
-                cv[fc][h] = *reinterpret_cast<const uint4*>(cpage + unit_off(fc, h));
-              }
-            }
+            for (int h = 0; h < kGateUnits; ++h) cv[fc][h] = *reinterpret_cast<const uint4*>(cpage + unit_off(fc, h));
           tr.mark(5, j);
           const bool valid = row < t.ntok;
           if constexpr (GATE_ADD) {

@@ -65,16 +65,24 @@ struct Q8Widen {
     const __nv_bfloat162 z = __hmul2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&z);
   }
-  __device__ __forceinline__ uint32_t two(uint32_t high_bytes) const {
-    const uint32_t x = (high_bytes & 0x80008000u) | ((high_bytes >> 4) & 0x07f007f0u);
-    uint32_t z = mul(x, mult);
-    if (more != 0x3f803f80u) z = mul(z, more);
+  // codes in the bytes of w, the first in the low one, as two pairs: the low nibble of a code
+  // is the second nibble of its bf16 value's low byte, the high nibble makes the high byte
+  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
+    const uint32_t a = (w << 4) & 0xf0f0f0f0u, b = ((w >> 4) & 0x07070707u) | (w & 0x80808080u);
+    lo = mul(__byte_perm(a, b, 0x5140), mult);
+    hi = mul(__byte_perm(a, b, 0x7362), mult);
+  }
+  // eight codes as a 16-byte unit
+  __device__ __forceinline__ uint4 unit(uint32_t w0, uint32_t w1) const {
+    uint4 z;
+    four(w0, z.x, z.y);
+    four(w1, z.z, z.w);
     return z;
   }
-  // codes in the bytes of w, the first in the low one, as two pairs
-  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
-    lo = two(__byte_perm(w, 0, 0x1404));
-    hi = two(__byte_perm(w, 0, 0x3424));
+  // whether values need the second factor (apart, so that rows that do not pay nothing for it)
+  __device__ __forceinline__ bool unfinished() const { return more != 0x3f803f80u; }
+  __device__ __forceinline__ void finish(uint4& z) const {
+    z = make_uint4(mul(z.x, more), mul(z.y, more), mul(z.z, more), mul(z.w, more));
   }
 };
 
