@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libegmla.so")
 
-SOURCES = ["egmla_api.cu", "egmla_aux.cu", "egmla_decode_tc.cu", "egmla_layer.cu",
+SOURCES = ["egmla_api.cu", "egmla_aux.cu", "egmla_decode_q8.cu", "egmla_decode_tc.cu", "egmla_layer.cu",
            "egmla_linear.cu", "egmla_pages.cu", "egmla_prefill.cu", "egmla_r0.cu", "egmla_shared.cu", "egmla_tokens.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

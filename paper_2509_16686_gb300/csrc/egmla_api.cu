@@ -86,6 +86,16 @@ bool encode_decode_maps(CUtensorMap (&maps)[2], const eg_mla_dims* d, const void
          encode_3d(&maps[1], krope_pool, dr, rows, 1, dr, rows * dr, tile, 1);
 }
 
+// maps = {codes, RoPE-key pool} of the ungated decode in 8 bits: a page's codes as
+// 128-byte-swizzled 128-feature columns (pairs of codes as 16-bit elements)
+bool encode_plain_q8_maps(CUtensorMap (&maps)[2], const eg_mla_dims* d, const void* c8_pool, const void* krope_pool,
+                          int32_t num_pages) {
+  std::memset(maps, 0, sizeof(maps));
+  const uint64_t rows = static_cast<uint64_t>(num_pages) * d->page_size, dc = d->d_c, dr = d->d_rope;
+  return encode_3d(&maps[0], c8_pool, 64, rows, dc / 128, dc / 2, 64, egmla::kPage, static_cast<uint32_t>(dc / 128)) &&
+         encode_3d(&maps[1], krope_pool, dr, rows, 1, dr, rows * dr, egmla::kPage, 1);
+}
+
 // maps of the tensor-core query absorption: {W_UK, q}
 bool encode_absorb_maps(CUtensorMap (&maps)[2], const DecodeArgs& a, int tile) {
   std::memset(maps, 0, sizeof(maps));
@@ -412,7 +422,9 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
   a.scale_pool = scale_pool;
   if (is_tc_path(dims)) {
     CUtensorMap maps[2];
-    if (!encode_decode_maps(maps, dims, scale_pool == nullptr ? c_pool : nullptr, krope_pool, num_pages))
+    const bool plain_q8 = scale_pool != nullptr && !a.gate && egmla::plain_q8_supported(a.d_c);
+    if (plain_q8 ? !encode_plain_q8_maps(maps, dims, c_pool, krope_pool, num_pages)
+                 : !encode_decode_maps(maps, dims, scale_pool == nullptr ? c_pool : nullptr, krope_pool, num_pages))
       return EG_MLA_ERR_CUDA;
     if (scale_pool == nullptr) apply_trace(a);   // (no traced build over a cache in 8 bits)
     apply_fault(a);
@@ -464,7 +476,8 @@ int decode_impl(const eg_mla_dims* dims, const void* q, const void* c_pool, cons
     bool fused = false;
     if (e == cudaSuccess) {
       prof_mark(st, true);
-      e = egmla::launch_decode_tc(a, maps, false, st, &fused);
+      e = plain_q8 ? egmla::launch_decode_plain_q8(a, maps, st, &fused)
+                   : egmla::launch_decode_tc(a, maps, false, st, &fused);
       prof_mark(st, false);
     }
     if (e == cudaSuccess && !fused) {

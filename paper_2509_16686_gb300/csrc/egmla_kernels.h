@@ -238,6 +238,10 @@ cudaError_t launch_combine(const DecodeArgs& a, bool tc_path, const CUtensorMap*
 // (cooperative launch); otherwise launch_combine must follow.
 cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool dump, cudaStream_t st,
                              bool* fused);
+// the same over the ungated latent in 8 bits (scale_pool); `maps` = {codes as 16-bit pairs
+// in boxes of a page's 128-feature columns, kr_pool map of whole pages}
+cudaError_t launch_decode_plain_q8(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_t st, bool* fused);
+bool plain_q8_supported(int d_c);
 // true if the bf16 tensor-core path has a kernel for these shapes
 bool tc_supported(int d_c, int gate);
 

@@ -9,7 +9,9 @@ eg_mla_append_latent_q8 is whole numbers: codes and scales equal a search over e
 grid in 64 bits, bit for bit.  eg_mla_read_latent_q8 gives scale x code exactly.
 
 eg_mla_decode_q8 equals eg_mla_decode over the values read back, bit for bit, and is within
-the hot path's bounds of the oracle on them."""
+the hot path's bounds (rel-L2 5e-3) of the oracle on them.  Ungated at d_c 256 and 512 it
+multiplies the codes themselves and is held to those bounds alone; two results that keep
+them are within 1e-2 of each other."""
 import dataclasses
 import importlib.util
 import math
@@ -515,6 +517,32 @@ def make(lens, d_c=256, gate="mul_ln", seed=11, splits=0, d_nope=128, d_v=128, v
     return case, dc
 
 
+def plain(d_c, gate):
+    """Whether the decode takes the codes as they are."""
+    return gate == "none" and d_c in (256, 512)
+
+
+def apart(got, want):
+    got, want = got.double(), want.double()
+    return float((got - want).norm() / want.norm())
+
+
+def reference64(dc, values):
+    """The ungated decode over a pool of values, in 64 bits."""
+    B, (H, dn) = dc.batch, dc.w_uk.shape[:2]
+    q, w_uk, w_uv = dc.q.double(), dc.w_uk.double(), dc.w_uv.double()
+    out = torch.zeros((B, H, dc.w_uv.shape[1]), dtype=torch.float64, device="cuda")
+    for b, n in enumerate(dc.seq_lens.tolist()):
+        if n == 0:
+            continue
+        page = dc.block_table[b, :-(-n // P)].long()
+        c = values[page].reshape(-1, values.shape[-1])[:n].double()
+        kr = dc.kr_pool[page].reshape(-1, dc.kr_pool.shape[-1])[:n].double()
+        s = torch.einsum("hd,hdc->hc", q[b, :, :dn], w_uk) @ c.T + q[b, :, dn:] @ kr.T
+        out[b] = torch.einsum("hc,hdc->hd", (s / math.sqrt(q.shape[-1])).softmax(-1) @ c, w_uv)
+    return out
+
+
 def same(a, b):
     return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num())
 
@@ -532,7 +560,10 @@ def test_decode_equals_the_decode_over_what_it_holds(gpu_lib, d_c, gate, lens):
         got = decode_q8(dc, cache)
         dc.c_pool.copy_(back)
         want = dc.decode(out=torch.full_like(dc.out, 9))
-        assert torch.equal(got, want), splits
+        if plain(d_c, gate):
+            assert apart(got, want) <= 1e-2, splits
+        else:
+            assert torch.equal(got, want), splits
         assert dc.read_status() == 0
     ref_case = dataclasses.replace(case, c_pool=device.bf16_tensor_to_bits(back))
     u = device.output_f64(got)
@@ -562,7 +593,11 @@ def test_decode_of_batches_and_widths(gpu_lib, batch, d_nope, d_v):
         cache, back = quantised(dc)
         got = decode_q8(dc, cache)
         dc.c_pool.copy_(back)
-        assert torch.equal(got, dc.decode(out=torch.full_like(dc.out, 9))) and dc.read_status() == 0
+        want = dc.decode(out=torch.full_like(dc.out, 9))
+        assert apart(got, want) <= 1e-2 if plain(d_c, gate) else torch.equal(got, want)
+        assert dc.read_status() == 0
+        if plain(d_c, gate):
+            assert apart(got, reference64(dc, back)) <= 5e-3
 
 
 @pytest.mark.parametrize("H,dn,dr,dc_,gate", [(16, 128, 64, 256, "mul_ln"), (4, 32, 16, 64, "mul_ln"), (12, 64, 64, 128, "none"),
@@ -592,6 +627,8 @@ def test_decode_of_small_and_large_scales_and_every_code(gpu_lib, d_c, gate, pow
     _, dc = make([200, 64, 130], d_c, gate)
     n = dc.c_pool.shape[0]
     cache = Cache(n, d_c, "bf16")
+    if plain(d_c, gate):   # scores of ordinary size: at others the largest decides alone, by its rounding
+        dc.q[..., :128] *= 2.0 ** (-power - 8)
     codes = torch.arange(n * P * d_c, device="cuda").mul(37).remainder(256).to(torch.uint8)
     cache.c8.copy_(torch.where(codes & 0x7f == 0x7f, codes - 1, codes).view(n, P, d_c))
     cache.scale.copy_(2.0 ** torch.randint(power - 4, power + 5, (n, P), device="cuda",
@@ -605,7 +642,36 @@ def test_decode_of_small_and_large_scales_and_every_code(gpu_lib, d_c, gate, pow
     assert torch.equal(back.double().view(n, P, d_c), value)
     got = decode_q8(dc, cache)
     dc.c_pool.copy_(back.view(n, P, d_c))
-    assert same(got, dc.decode(out=torch.full_like(dc.out, 9))) and dc.read_status() == 0
+    if plain(d_c, gate):
+        assert apart(got * 2.0 ** -power, reference64(dc, dc.c_pool) * 2.0 ** -power) <= 5e-3
+    else:
+        assert same(got, dc.decode(out=torch.full_like(dc.out, 9)))
+    assert dc.read_status() == 0
+
+
+@pytest.mark.parametrize("d_c", [256, 512])
+def test_plain_decode_of_many_small_weights(gpu_lib, d_c):
+    """One token whose weight is far above the others', of which there are enough to count together: their weights
+    lie below what two parts of eight bits hold beside it.  And the reverse: weights that grow from tile to tile."""
+    _, dc = make([20000, 20000, 6000], d_c, "none", vocab=100)
+    cache, back = quantised(dc)
+    # scores by the RoPE part alone: k^R_j = x_j e, q^R = 1 e, the latent's part 2^-20 of it
+    dc.q.zero_()
+    dc.q[..., 128] = 1.0
+    dc.kr_pool.zero_()
+    first = dc.block_table[:, 0].long()
+    scale = math.sqrt(192.0)
+    for b, drop in ((0, 9.0), (1, 12.0)):   # nats below the first token's: 20000 e^-9 = 2.5, 20000 e^-12 = 0.12
+        dc.kr_pool[dc.block_table[b].long(), :, 0] = -drop * scale
+        dc.kr_pool[first[b], 0, 0] = 0
+    pages = dc.block_table[2, :94].long()
+    dc.kr_pool[pages, :, 0] = (torch.arange(94, device="cuda").float() * 0.7 * scale).to(torch.bfloat16)[:, None]
+    cache.kr.copy_(dc.kr_pool)
+    got = decode_q8(dc, cache)
+    want = reference64(dc, back)
+    for b in range(3):
+        assert apart(got[b], want[b]) <= 5e-3, b
+    assert dc.read_status() == 0
 
 
 @pytest.mark.parametrize("d_c,gate", [(256, "mul_ln"), (192, "add_ln"), (256, "none"), (512, "none")])
