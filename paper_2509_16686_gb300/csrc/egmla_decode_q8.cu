@@ -19,9 +19,11 @@
 //   l = sum_j P'_j 2^-e_j with the rounded P', so that the rounding cancels in O / l.
 // The RoPE part stays bf16 (kind::f16) in columns of its own.
 //
-// Roles as in egmla_decode_tc.cu; in place of the gate warps eight query warps make each
-// segment's query block from the absorbed bf16 queries, and clear the rows behind a
-// sequence's end in its last page (whose codes may be anything, NaN too).
+// Roles as in egmla_decode_tc.cu, but for the gate warps: the softmax, here the longest of
+// all roles, has two groups of four warps, eight heads each, which need nothing of one
+// another; four query warps make each segment's query block from the absorbed bf16
+// queries, and clear the rows behind a sequence's end in its last page (whose codes may be
+// anything, NaN too).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -37,6 +39,10 @@ namespace egmla {
 
 namespace {
 
+constexpr int kPlainThreads = 512;
+constexpr int kGroupHeads = 8;                       // heads of a softmax group
+constexpr int kSoft2Warp0 = 8;                       // warps 8-11: the second group (a warp reads the TMEM lanes of warp % 4)
+constexpr int kQueryWarp0 = 12, kQueryWarps = 4;
 constexpr int kQParts = 2, kPParts = 3;
 constexpr float kPart2 = 1.f / 16, kPart3 = 1.f / 65536;
 // weights of at most 2^(4 + 4) = 256: below e4m3's 448, and as far above its smallest
@@ -100,15 +106,33 @@ __device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, ui
       : "memory");
 }
 
-// 16 lanes x 16 columns, as tmem_ld_16x256b_x4 for two groups of eight columns
-__device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, float (&v)[8]) {
+// 16 lanes x 8 columns, as tmem_ld_16x256b_x4 for one group of eight columns
+__device__ __forceinline__ void tmem_ld_16x256b_x1(uint32_t taddr, float (&v)[4]) {
+  uint32_t r[4];
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(taddr)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// 32 lanes x 8 columns: thread i of the warp gets (or writes) its lane's 8 values
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
   uint32_t r[8];
-  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr)
                : "memory");
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+               "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+               "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
 }
 
 // two codes as fp32 values
@@ -117,7 +141,7 @@ __device__ __forceinline__ float2 decode2(uint32_t c) {
 }
 
 template <int D_C>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kPlainThreads, 1)
     decode_plain_q8_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap krmap,
                            const TcParams p) {
   using C = PlainCfg<D_C>;
@@ -134,18 +158,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&bars.full[s]), 1);
       mbar_init(smem_u32(&bars.empty[s]), 1);
     }
-    mbar_init(smem_u32(&bars.qfull[0]), kGateWarps);
+    mbar_init(smem_u32(&bars.qfull[0]), kQueryWarps);
     // the last score MMA of the segment (commit) and the softmax warps' read of its scales
-    mbar_init(smem_u32(&bars.qempty[0]), 1 + kSoftWarps);
+    mbar_init(smem_u32(&bars.qempty[0]), 1 + 2 * kSoftWarps);
     for (int s = 0; s < kNB; ++s) {
       mbar_init(smem_u32(&bars.sready[s]), 1);
-      mbar_init(smem_u32(&bars.sfree[s]), kSoftWarps);
+      mbar_init(smem_u32(&bars.sfree[s]), 2 * kSoftWarps);
     }
     for (int s = 0; s < kNP; ++s) {
-      mbar_init(smem_u32(&bars.spdone[s]), kSoftWarps);
+      mbar_init(smem_u32(&bars.spdone[s]), 2 * kSoftWarps);
       mbar_init(smem_u32(&bars.pfree[s]), 1);
     }
-    mbar_init(smem_u32(&bars.zfix), kGateWarps);
+    mbar_init(smem_u32(&bars.zfix), kQueryWarps);
     mbar_init(smem_u32(&bars.drain_s), 1);
     mbar_init(smem_u32(&bars.drain_o), 1);
     bars.abort = 0;
@@ -294,13 +318,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     __syncwarp();
-  } else if (warp >= kGateWarp0) {
+  } else if (warp >= kQueryWarp0) {
     // ---------------------------------------------------------------- query blocks, rows behind the end
-    // Warp w has heads 2w and 2w + 1, half a warp each; a lane every sixteenth block of 16
+    // Warp w has heads 4w .. 4w + 3, eight lanes each; a lane every eighth block of 16
     // features of its head.
-    constexpr int BLOCKS = D_C / 16 / 16;
-    const int gw = warp - kGateWarp0, tid = gw * 32 + lane;
-    const int h = 2 * gw + lane / 16, l16 = lane % 16;
+    constexpr int LANES = 32 * kQueryWarps / kHeads, BLOCKS = D_C / 16 / LANES;
+    const int tid = (warp - kQueryWarp0) * 32 + lane;
+    const int h = tid / LANES, l16 = tid % LANES;
     uint8_t* qb = smem + C::OFF_QBUF;
     Walker<kPage> w;
     w.start(p);
@@ -310,14 +334,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (t.first) {
         ++seg;
         const uint8_t* src = p.qprep + static_cast<size_t>(t.b) * qprep_bytes_tc(D_C, kRope);
-        uint4 raw[BLOCKS][2], rope = make_uint4(0, 0, 0, 0);
+        uint4 raw[BLOCKS][2];
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            raw[i][e] = __ldcg(reinterpret_cast<const uint4*>(src + qlat_offset(h, 16 * (l16 + 16 * i) + 8 * e, D_C)));
-        const bool copies = tid < static_cast<int>(qprep_rope_bytes(kRope) / 16);
-        if (copies) rope = __ldcg(reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C)) + tid);
+            raw[i][e] = __ldcg(reinterpret_cast<const uint4*>(src + qlat_offset(h, 16 * (l16 + LANES * i) + 8 * e, D_C)));
+        static_assert(qprep_rope_bytes(kRope) == 16 * 32 * kQueryWarps, "a unit of q^R per thread");
+        const uint4 rope = __ldcg(reinterpret_cast<const uint4*>(src + qprep_lat_bytes(D_C)) + tid);
         // the head's largest magnitude (two bf16 values at once: their bits order them)
         uint32_t most = 0;
 #pragma unroll
@@ -329,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < 4; ++k) most = max(most, max(v[k] << 16 & 0x7fff0000u, v[k] & 0x7fff0000u));
           }
 #pragma unroll
-        for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+        for (int o = 1; o < LANES; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
         float scale, inverse;
         q8_scale(most, scale, inverse);
         // the block is free once the segment before has read it
@@ -356,10 +380,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
 #pragma unroll
           for (int n = 0; n < kQParts; ++n)
-            *reinterpret_cast<uint4*>(qb + (l16 + 16 * i) * C::QCORE + (2 * n + h / 8) * 128 + (h % 8) * 16) =
+            *reinterpret_cast<uint4*>(qb + (l16 + LANES * i) * C::QCORE + (2 * n + h / 8) * 128 + (h % 8) * 16) =
                 make_uint4(part[n][0], part[n][1], part[n][2], part[n][3]);
         }
-        if (copies) reinterpret_cast<uint4*>(qb + C::Q_ROPE)[tid] = rope;
+        reinterpret_cast<uint4*>(qb + C::Q_ROPE)[tid] = rope;
         if (l16 == 0) reinterpret_cast<float*>(qb + C::Q_SCALE)[h] = p.scale_log2 * scale;
         fence_proxy_async_smem();
         warp_arrive(smem_u32(&bars.qfull[0]));
@@ -368,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int slot = j % C::NS;
       if (!warp_wait(smem_u32(&bars.full[slot]), (j / C::NS) & 1, abort_flag, wait_ns)) break;
       if (t.ntok < kPage) {
-        for (int i = tid; i < (kPage - t.ntok) * 8; i += 32 * kGateWarps)
+        for (int i = tid; i < (kPage - t.ntok) * 8; i += 32 * kQueryWarps)
 #pragma unroll
           for (int fc = 0; fc < C::NCH; ++fc)
             *reinterpret_cast<uint4*>(smem + slot * C::SLOT + fc * C::PCHUNK + (t.ntok + i / 8) * 128 + i % 8 * 16) =
@@ -377,20 +401,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         warp_arrive(smem_u32(&bars.zfix));
       }
     }
-  } else {
+  } else if (warp < kSoftWarps || warp >= kSoft2Warp0) {
     // ---------------------------------------------------------------- softmax, output read-out
-    // (threads, tokens and heads as in egmla_decode_tc.cu)
-    const int q = lane & 3;
-    const int r0 = 16 * warp + (lane >> 2), r1 = r0 + 8;
-    const uint32_t tq = tmem + (static_cast<uint32_t>(32 * warp) << 16);
+    // Group g has heads 8g .. 8g + 7; its warp w reads TMEM lane quadrant w: tokens 16w ..
+    // 16w + 15 of a tile's scores, latent features 32w .. 32w + 31 of each 128-feature
+    // chunk of O^T.  Thread t owns tokens r0 = 16w + t / 4 and r1 = r0 + 8 and heads 8g + 2q,
+    // 8g + 2q + 1 (q = t % 4).  Lane i < 8 of every warp also keeps the reference of head 8g + i.
+    const int g = warp >= kSoft2Warp0, quad = warp & 3, q = lane & 3;
+    const int r0 = 16 * quad + (lane >> 2), r1 = r0 + 8;
+    const int bar_tile = 1 + 2 * g, bar_xch = 2 + 2 * g;
+    const uint32_t tq = tmem + (static_cast<uint32_t>(32 * quad) << 16);
     const float scale = p.scale_log2;
-    float* xmax = reinterpret_cast<float*>(smem + C::OFF_XCH);   // [4 warps][16 heads]
-    float* xsum = xmax + kSoftWarps * kHeads;                    // [4 warps][16 heads]
-    auto head_of = [&](int k) { return (k & 1) + 2 * q + 8 * (k >> 1); };
-    float m_ref[4], l_acc[4], qs[4];
-    float m16 = -INFINITY;   // head `lane` (lanes 0-15)
+    float* xmax = reinterpret_cast<float*>(smem + C::OFF_XCH) + g * 64;   // [4 warps][8 heads]
+    float* xsum = xmax + kSoftWarps * kGroupHeads;                        // [4 warps][8 heads]
+    float m_ref[2], l_acc[2], qs[2];
+    float m8 = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
       m_ref[k] = -INFINITY;
       l_acc[k] = 0.f;
       qs[k] = 0.f;
@@ -406,9 +433,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++seg;
         ok = warp_wait(smem_u32(&bars.qfull[0]), seg & 1, abort_flag, wait_ns);
         if (ok) {
-          const float* hs = reinterpret_cast<const float*>(smem + C::OFF_QBUF + C::Q_SCALE);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) qs[k] = hs[head_of(k)];
+          const float* hs = reinterpret_cast<const float*>(smem + C::OFF_QBUF + C::Q_SCALE) + kGroupHeads * g + 2 * q;
+          qs[0] = hs[0];
+          qs[1] = hs[1];
           warp_arrive(smem_u32(&bars.qempty[0]));
         }
       }
@@ -421,13 +448,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (r1 < t.ntok) ts[1] = sc[r1];
       }
       ok = ok && warp_wait(smem_u32(&bars.sready[sb]), (it / kNB) & 1, abort_flag, wait_ns);
-      float s[2][4];
+      float s[2][2];
       bool exceed = false;
       if (ok) {
-        float v[16], vr[8];
+        float v1[4], v2[4], vr[4];
         tc_fence_after();
-        tmem_ld_16x256b_x4(tq + C::COL_S + sb * C::S_COLS, v);
-        tmem_ld_16x256b_x2(tq + C::COL_S + sb * C::S_COLS + C::S_ROPE, vr);
+        const uint32_t ds = tq + C::COL_S + sb * C::S_COLS + kGroupHeads * g;
+        tmem_ld_16x256b_x1(ds, v1);
+        tmem_ld_16x256b_x1(ds + kHeads, v2);
+        tmem_ld_16x256b_x1(ds + C::S_ROPE, vr);
         tmem_wait_ld();
         tc_fence_before();
         warp_arrive(smem_u32(&bars.sfree[sb]));
@@ -436,63 +465,62 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool valid = (e ? r1 : r0) < t.ntok;
           const float lift = static_cast<float>(static_cast<int>(__float_as_uint(ts[e]) >> 23) - 127);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int i = (k >> 1) * 4 + 2 * e + (k & 1);
-            const float lat = fmaf(v[8 + i], kPart2, v[i]) * ts[e];
+          for (int k = 0; k < 2; ++k) {
+            const int i = 2 * e + k;
+            const float lat = fmaf(v2[i], kPart2, v1[i]) * ts[e];
             const float x = fmaf(lat, qs[k], fmaf(vr[i], scale, lift));
             s[e][k] = valid ? x : -INFINITY;
             exceed = exceed || (x > m_ref[k] + kPlainLazy && valid);
           }
         }
       }
-      if (soft_vote(kBarTile, exceed || !ok)) {
-        if (soft_vote(kBarTile, !ok)) break;   // uniform: every warp leaves
+      if (soft_vote(bar_tile, exceed || !ok)) {
+        if (soft_vote(bar_tile, !ok)) break;   // uniform: every warp of the group leaves
         // ---- slow path: tile maxima of the heads over the 64 tokens
-        float tm[4];
+        float tm[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tm[k] = fmaxf(s[0][k], s[1][k]);
+        for (int k = 0; k < 2; ++k) tm[k] = fmaxf(s[0][k], s[1][k]);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) tm[k] = fmaxf(tm[k], __shfl_xor_sync(0xffffffffu, tm[k], o));
+          for (int k = 0; k < 2; ++k) tm[k] = fmaxf(tm[k], __shfl_xor_sync(0xffffffffu, tm[k], o));
         if (lane < 4) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) xmax[warp * kHeads + head_of(k)] = tm[k];
+          for (int k = 0; k < 2; ++k) xmax[quad * kGroupHeads + 2 * q + k] = tm[k];
         }
-        soft_sync(kBarXch);
+        soft_sync(bar_xch);
         float alpha = 1.f;
-        if (lane < kHeads) {
-          const float tmax = fmaxf(fmaxf(xmax[lane], xmax[kHeads + lane]),
-                                   fmaxf(xmax[2 * kHeads + lane], xmax[3 * kHeads + lane]));
-          if (m16 == -INFINITY) {
-            m16 = tmax;
+        if (lane < kGroupHeads) {
+          const float tmax = fmaxf(fmaxf(xmax[lane], xmax[kGroupHeads + lane]),
+                                   fmaxf(xmax[2 * kGroupHeads + lane], xmax[3 * kGroupHeads + lane]));
+          if (m8 == -INFINITY) {
+            m8 = tmax;
             alpha = 0.f;
-          } else if (tmax > m16 + kPlainLazy) {
-            alpha = ex2_approx(m16 - tmax);
-            m16 = tmax;
+          } else if (tmax > m8 + kPlainLazy) {
+            alpha = ex2_approx(m8 - tmax);
+            m8 = tmax;
           }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) m_ref[k] = __shfl_sync(0xffffffffu, m16, head_of(k));
-        if (!t.first && __any_sync(0xffffffffu, lane < kHeads && alpha != 1.f)) {
+        for (int k = 0; k < 2; ++k) m_ref[k] = __shfl_sync(0xffffffffu, m8, 2 * q + k);
+        if (!t.first && __any_sync(0xffffffffu, lane < kGroupHeads && alpha != 1.f)) {
           // what was accumulated against the old reference, after the tile before
           const int pv = (it - 1) % kNP;
           ok = warp_wait(smem_u32(&bars.pfree[pv]), ((it - 1) / kNP) & 1, abort_flag, wait_ns);
           if (ok) {
             tc_fence_after();
 #pragma unroll
-            for (int c16 = 0; c16 < kPParts * C::NMC; ++c16) {
-              float o[16];
-              tmem_ld16(tq + C::COL_O + 16 * c16, o);
+            for (int c = 0; c < kPParts * C::NMC; ++c) {
+              float o[8];
+              tmem_ld8(tq + C::COL_O + kHeads * c + kGroupHeads * g, o);
               tmem_wait_ld();
-              uint32_t r[16];
 #pragma unroll
-              for (int c = 0; c < 16; ++c) r[c] = __float_as_uint(o[c] * __shfl_sync(0xffffffffu, alpha, c));
-              tmem_st16(tq + C::COL_O + 16 * c16, r);
+              for (int i = 0; i < kGroupHeads; ++i) o[i] *= __shfl_sync(0xffffffffu, alpha, i);
+              tmem_st8(tq + C::COL_O + kHeads * c + kGroupHeads * g, o);
             }
             tmem_wait_st();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) l_acc[k] *= __shfl_sync(0xffffffffu, alpha, head_of(k));
+            for (int k = 0; k < 2; ++k) l_acc[k] *= __shfl_sync(0xffffffffu, alpha, 2 * q + k);
           }
         }
       }
@@ -503,27 +531,24 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = e ? r1 : r0;
-          uint8_t* prow = pbuf + (r >> 3) * C::PGROUP + (r & 7) * 16 + 2 * q;
+          uint8_t* prow = pbuf + (r >> 3) * C::PGROUP + (r & 7) * 16 + kGroupHeads * g + 2 * q;
           // 2^-e of the token's scale (NaN: NaN)
           const float lower = ts[e] != ts[e] ? ts[e] : __uint_as_float((254u << 23) - __float_as_uint(ts[e]));
-#pragma unroll
-          for (int hp = 0; hp < 2; ++hp) {
-            const float p0 = ex2_approx(s[e][2 * hp] - (m_ref[2 * hp] - kWeightLog2));
-            const float p1 = ex2_approx(s[e][2 * hp + 1] - (m_ref[2 * hp + 1] - kWeightLog2));
-            const uint32_t c1 = q8_encode2(p0, p1);
-            const float2 d1 = decode2(c1);
-            const uint32_t c2 = q8_encode2((p0 - d1.x) * 16.f, (p1 - d1.y) * 16.f);
-            const float2 d2 = decode2(c2);
-            const float t0 = fmaf(d2.x, kPart2, d1.x), t1 = fmaf(d2.y, kPart2, d1.y);
-            const float g0 = p0 - t0, g1 = p1 - t1;   // what p3 takes, as far as it reaches
-            const uint32_t c3 = q8_encode2(g0 * 65536.f, g1 * 65536.f);
-            constexpr float kReach = 448.f * kPart3;
-            l_acc[2 * hp] = fmaf(t0 + fminf(fmaxf(g0, -kReach), kReach), lower, l_acc[2 * hp]);
-            l_acc[2 * hp + 1] = fmaf(t1 + fminf(fmaxf(g1, -kReach), kReach), lower, l_acc[2 * hp + 1]);
-            *reinterpret_cast<uint16_t*>(prow + 8 * hp) = static_cast<uint16_t>(c1);
-            *reinterpret_cast<uint16_t*>(prow + 128 + 8 * hp) = static_cast<uint16_t>(c2);
-            *reinterpret_cast<uint16_t*>(prow + 256 + 8 * hp) = static_cast<uint16_t>(c3);
-          }
+          const float p0 = ex2_approx(s[e][0] - (m_ref[0] - kWeightLog2));
+          const float p1 = ex2_approx(s[e][1] - (m_ref[1] - kWeightLog2));
+          const uint32_t c1 = q8_encode2(p0, p1);
+          const float2 d1 = decode2(c1);
+          const uint32_t c2 = q8_encode2((p0 - d1.x) * 16.f, (p1 - d1.y) * 16.f);
+          const float2 d2 = decode2(c2);
+          const float t0 = fmaf(d2.x, kPart2, d1.x), t1 = fmaf(d2.y, kPart2, d1.y);
+          const float g0 = p0 - t0, g1 = p1 - t1;   // what p3 takes, as far as it reaches
+          const uint32_t c3 = q8_encode2(g0 * 65536.f, g1 * 65536.f);
+          constexpr float kReach = 448.f * kPart3;
+          l_acc[0] = fmaf(t0 + fminf(fmaxf(g0, -kReach), kReach), lower, l_acc[0]);
+          l_acc[1] = fmaf(t1 + fminf(fmaxf(g1, -kReach), kReach), lower, l_acc[1]);
+          *reinterpret_cast<uint16_t*>(prow) = static_cast<uint16_t>(c1);
+          *reinterpret_cast<uint16_t*>(prow + 128) = static_cast<uint16_t>(c2);
+          *reinterpret_cast<uint16_t*>(prow + 256) = static_cast<uint16_t>(c3);
         }
         fence_proxy_async_smem();
         tc_fence_before();
@@ -535,35 +560,34 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) l_acc[k] += __shfl_xor_sync(0xffffffffu, l_acc[k], o);
+          for (int k = 0; k < 2; ++k) l_acc[k] += __shfl_xor_sync(0xffffffffu, l_acc[k], o);
         if (lane < 4) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) xsum[warp * kHeads + head_of(k)] = l_acc[k];
+          for (int k = 0; k < 2; ++k) xsum[quad * kGroupHeads + 2 * q + k] = l_acc[k];
         }
-        if (soft_vote(kBarXch, !ok)) break;   // uniform
+        if (soft_vote(bar_xch, !ok)) break;   // uniform
         ok = warp_wait(smem_u32(&bars.pfree[pb]), (it / kNP) & 1, abort_flag, wait_ns);
         if (ok) {
           tc_fence_after();
           const int slot_out = blockIdx.x + t.b;
-          float* po = p.part_o + static_cast<size_t>(slot_out) * kHeads * D_C;
+          float* po = p.part_o + (static_cast<size_t>(slot_out) * kHeads + kGroupHeads * g) * D_C;
 #pragma unroll
           for (int mc = 0; mc < C::NMC; ++mc) {
-            float o12[32], o3[16];
-            tmem_ld32(tq + C::COL_O + C::O_COLS * mc, o12);
-            tmem_ld16(tq + C::COL_O + C::O_COLS * mc + 32, o3);
-            tmem_wait_ld();
-            const int f = 128 * mc + 32 * warp + lane;
+            float o[kPParts][8];
 #pragma unroll
-            for (int hh = 0; hh < kHeads; ++hh)
-              po[hh * D_C + f] = fmaf(o3[hh], kPart3, fmaf(o12[kHeads + hh], kPart2, o12[hh]));
+            for (int n = 0; n < kPParts; ++n) tmem_ld8(tq + C::COL_O + C::O_COLS * mc + kHeads * n + kGroupHeads * g, o[n]);
+            tmem_wait_ld();
+            const int f = 128 * mc + 32 * quad + lane;
+#pragma unroll
+            for (int i = 0; i < kGroupHeads; ++i) po[i * D_C + f] = fmaf(o[2][i], kPart3, fmaf(o[1][i], kPart2, o[0][i]));
           }
           tc_fence_before();
-          if (warp == 0 && lane < kHeads) {
+          if (quad == 0 && lane < kGroupHeads) {
             float lh = 0.f;
 #pragma unroll
-            for (int ww = 0; ww < kSoftWarps; ++ww) lh += xsum[ww * kHeads + lane];
-            float* ml = p.part_ml + (static_cast<size_t>(slot_out) * kHeads + lane) * 2;
-            ml[0] = m16 - kWeightLog2;
+            for (int ww = 0; ww < kSoftWarps; ++ww) lh += xsum[ww * kGroupHeads + lane];
+            float* ml = p.part_ml + (static_cast<size_t>(slot_out) * kHeads + kGroupHeads * g + lane) * 2;
+            ml[0] = m8 - kWeightLog2;
             ml[1] = lh;
           }
           if (p.fuse) {
@@ -574,9 +598,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        m16 = -INFINITY;
+        m8 = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
           m_ref[k] = -INFINITY;
           l_acc[k] = 0.f;
         }
@@ -590,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kMmaWarp) tmem_dealloc(tmem, C::TMEM_COLS);
   if (threadIdx.x == 0 && bars.abort) report_status(p.status, kStatusTimeout);
   if constexpr (D_C <= 256) {
-    if (p.fuse) fused_combine<D_C, false>(p, smem, bars);
+    if (p.fuse) fused_combine<D_C, false, 2 * kSoftWarps>(p, smem, bars);
   }
 }
 
@@ -604,9 +628,9 @@ cudaError_t launch_plain(const DecodeArgs& a, const CUtensorMap* maps, cudaStrea
   // (the line between the two forms of the combine: see egmla_decode_tc.cu)
   p.fuse = !a.apart && D_C <= 256 && a.batch > 0 && kHeads * a.batch <= a.num_splits &&
            a.d_v <= kCombineRowsPerWarp * (kThreads / 32) &&
-           a.num_splits <= resident_ctas<decode_plain_q8_kernel<D_C>>(C::SMEM);
+           a.num_splits <= resident_ctas<decode_plain_q8_kernel<D_C>, kPlainThreads>(C::SMEM);
   if (fused) *fused = p.fuse != 0;
-  return launch_split_kernel(kern, C::SMEM, a, maps, p, st);
+  return launch_split_kernel<kPlainThreads>(kern, C::SMEM, a, maps, p, st);
 }
 
 }  // namespace

@@ -412,7 +412,8 @@ __device__ __forceinline__ float reduce8_rows(const float (&v)[8], int lane) {
 // into shared memory.  u: the warp's first eight row sums
 // reduced across the lanes by a transposing butterfly (9 shuffles, after
 // which lane 4r holds row r) and the ninth by a plain warp sum.
-template <int D_C, bool TRACE>
+// ARRIVALS: softmax warps that leave a part of each partial
+template <int D_C, bool TRACE, int ARRIVALS = kSoftWarps>
 __device__ void fused_combine(const TcParams& p, uint8_t* smem, Bars& bars) {
   constexpr int kWarps = kThreads / 32;
   constexpr int NFB = D_C / 32;      // 32-feature blocks of a row
@@ -443,7 +444,7 @@ __device__ void fused_combine(const TcParams& p, uint8_t* smem, Bars& bars) {
     const int n = q1 > q0 ? (q1 - 1) / chunk - c0 + 1 : 0;   // splits that covered it
     if (tid == 0 && !*abort_flag) {
       // every softmax warp's part of every split partial of the sequence stored
-      const uint32_t want = static_cast<uint32_t>(kSoftWarps) * static_cast<uint32_t>(n);
+      const uint32_t want = static_cast<uint32_t>(ARRIVALS) * static_cast<uint32_t>(n);
       const uint64_t t0 = globaltimer();
       while (ld_acquire_gpu(p.seq_done + b) < want) {
         if (*abort_flag) break;
@@ -527,7 +528,7 @@ __device__ void fused_combine(const TcParams& p, uint8_t* smem, Bars& bars) {
 
 // CTAs of Kern (with its one shared-memory size) that the current device holds at
 // once (1 per SM here), looked up once per kernel and device
-template <auto Kern>
+template <auto Kern, int THREADS = kThreads>
 int resident_ctas(uint32_t smem) {
   static std::atomic<int> cached[64];   // 0: not looked up yet
   int dev = 0;
@@ -535,7 +536,7 @@ int resident_ctas(uint32_t smem) {
   int n = cached[dev].load(std::memory_order_relaxed);
   if (n == 0) {
     int per_sm = 0, sms = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, Kern, kThreads, smem) != cudaSuccess ||
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, Kern, THREADS, smem) != cudaSuccess ||
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
       return 0;
     n = std::max(0, per_sm) * sms;
@@ -589,7 +590,7 @@ inline TcParams decode_params(const DecodeArgs& a) {
   return p;
 }
 
-template <typename Kern>
+template <int THREADS = kThreads, typename Kern>
 cudaError_t launch_split_kernel(Kern* kern, uint32_t smem, const DecodeArgs& a, const CUtensorMap* maps, const TcParams& p,
                                 cudaStream_t st) {
   // The kernel may start while the query-absorption kernel before it on the
@@ -597,7 +598,7 @@ cudaError_t launch_split_kernel(Kern* kern, uint32_t smem, const DecodeArgs& a, 
   // overlaps that kernel's tail, and grid_dependency_wait orders the rest.
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.num_splits);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
