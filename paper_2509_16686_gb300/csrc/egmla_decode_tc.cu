@@ -110,7 +110,7 @@ struct Cfg {
   static constexpr int NS1 = (int)((kSmemLimit - FIXED - QBUF) / (SLOT + STAT_BYTES));
   static constexpr int NQ = Q8 ? (D_C == 192 ? 2 : 1) : (NS2 < 5 && NS1 > NS2) ? 1 : 2;
   static constexpr int NS_FIT = NQ == 2 ? NS2 : NS1;
-  static constexpr int NS = Q8 ? 4 : NS_FIT > 6 ? 6 : NS_FIT;
+  static constexpr int NS = Q8 ? (D_C == 192 ? 4 : 3) : NS_FIT > 6 ? 6 : NS_FIT;
   // raw slots: what is left beside the latent slots
   static constexpr int NR_FIT =
       Q8 ? (int)((kSmemLimit - FIXED - NQ * QBUF - NS * (SLOT + STAT_BYTES)) / (RSLOT + RMETA + (Q8 ? 0 : 1))) : 0;
@@ -703,7 +703,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               *reinterpret_cast<uint4*>(zpage + unit_off(fc, h)) = z;
             }
-            load_next(fc);
+            // (the first column's with the second's: one task fewer among the first stores)
+            if (fc == 1) load_next(0);
+            if (fc > 0) load_next(fc);
           }
           tr.mark(6, j);
           float mu = 0.f, r = 1.f;
