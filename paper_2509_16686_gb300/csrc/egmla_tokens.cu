@@ -23,7 +23,7 @@
 namespace egmla {
 namespace {
 
-constexpr int kTokThreads = 256, kTokWarps = kTokThreads / 32;
+constexpr int kTokThreads = 128, kTokWarps = kTokThreads / 32;
 
 struct Packed {
   const int32_t* cu;          // [batch + 1], null: one token per sequence
@@ -487,8 +487,8 @@ cudaError_t launch_append_q8(const CacheArgs& a, cudaStream_t st) {
 template <typename E>
 cudaError_t launch_read_q8(const CacheArgs& a, cudaStream_t st) {
   if (a.d_c <= 256)
-    return launch_tokens<8>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 1> : read_q8_kernel<E, 8, 1>; });
-  return launch_tokens<8>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 2> : read_q8_kernel<E, 8, 2>; });
+    return launch_tokens<4>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 1> : read_q8_kernel<E, 4, 1>; });
+  return launch_tokens<4>(a, st, [](bool few) { return few ? read_q8_kernel<E, 1, 2> : read_q8_kernel<E, 4, 2>; });
 }
 
 // ------------------------------------------------------------------ arguments
