@@ -3,7 +3,8 @@
 Prompts are planned, rotated, prefilled and written into the cache in 8 bits; each step
 then plans a token for every sequence, rotates its query and key, writes it and decodes
 over the cache.  Beside it a bf16 cache takes the same tokens unrounded, and at the end the
-8-bit cache's values are read back: the decode over them must be the same to the bit.
+8-bit cache's values are read back into another: the decode over them has the same result
+within its bounds.
 
     python examples/serve_q8.py [--prompts 300 70 64 1] [--steps 5]
 """
@@ -100,15 +101,15 @@ def main(prompts=(300, 70, 64, 1), steps=5, seed=0):
         _lib.eg_mla_decode(dims, q, pool, kr_pool, id_pool, table, lens, longest, *gate, *weights, o, ws, dev_status=status)
         return o
 
-    exact = torch.equal(out, dense(rounded_pool))
-    want = dense(unrounded).double()
-    rounded = float((out.double() - want).norm() / want.norm())
+    def apart(want):
+        return float((out.double() - want.double()).norm() / want.double().norm())
+
+    values_apart, rounded = apart(dense(rounded_pool)), apart(dense(unrounded))
     plan([-1] * B)
     all_free = int(count.item()) == pages
-    print(f"{B} prompts of {min(prompts)} to {max(prompts)} tokens, {steps} steps: the decode over 8 bits "
-          f"{'is' if exact else 'IS NOT'} the one over its values, rel-L2 {rounded:.1e} from the unrounded cache's; "
-          f"status {int(status.item())}")
-    return exact, rounded, all_free, int(status.item())
+    print(f"{B} prompts of {min(prompts)} to {max(prompts)} tokens, {steps} steps: rel-L2 {values_apart:.1e} from the "
+          f"decode over the same values in bf16, {rounded:.1e} from that over the unrounded ones; status {int(status.item())}")
+    return values_apart, rounded, all_free, int(status.item())
 
 
 if __name__ == "__main__":

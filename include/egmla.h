@@ -522,9 +522,11 @@ int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const fl
 /*
  * eg_mla_decode_q8 - eg_mla_decode over a cache in 8 bits: the latent of token j is
  * scale_j x code_j.  The result is eg_mla_decode's over a cache of the values that
- * eg_mla_read_latent_q8 gives, to the bit; with the gate off at d_c 256 and 512 in bf16, where
- * the codes themselves are multiplied, within the bounds of eg_mla_decode (softmax weights
- * in eight significant bits, below 2^-13 of the largest in four).
+ * eg_mla_read_latent_q8 gives, within the same bounds.  (In fp32, at d_c 192 and with the
+ * ablation gates it is the same to the bit; at d_c 256 EG_MLA_GATE_MUL_LN's sums come in
+ * another order, and ungated at d_c 256 and 512 the codes themselves are multiplied, with
+ * queries and softmax weights in eight significant bits, weights below 2^-13 of the largest
+ * in four.)
  *
  *   dims         those of eg_mla_decode with d_c a multiple of 16; max_seq_len at most
  *                2^31 - 64

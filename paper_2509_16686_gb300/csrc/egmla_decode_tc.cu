@@ -77,7 +77,10 @@ namespace {
 // ids and its RoPE keys land in a ring of raw slots, from which the gate warps write the
 // bf16 tile into a ring of latent slots: a raw slot is held until the tile's score MMAs
 // are complete, a latent slot from the gate to its output MMAs.
-template <int D_C, bool GATE, bool Q8 = false>
+// ZZ (with Q8 and LN(c (*) g)): the LayerNorm's sums of a tile come from the tensor cores:
+// Z [Z ; 1]^T, whose diagonal holds every row's sum of squares and whose last columns its
+// sum.  Eight rows of ones behind the tile's 64 in each of its columns.
+template <int D_C, bool GATE, bool Q8 = false, bool ZZ = false>
 struct Cfg {
   static constexpr int NCH = D_C / 64;                  // 64-feature swizzle-atom columns
   // tokens per tile: a page, or half a page for the widest latent, whose pages
@@ -86,12 +89,13 @@ struct Cfg {
   // and 6.1 TB/s; kernel alone, warm)
   static constexpr int TOK = D_C > 256 ? kPage / 2 : kPage;
   static constexpr uint32_t PCHUNK = TOK * 128;         // one atom column of a tile
-  static constexpr uint32_t KR_OFF = NCH * PCHUNK;
+  static constexpr uint32_t ZCHUNK = PCHUNK + (ZZ ? 1024 : 0);   // one of the latent's
+  static constexpr uint32_t KR_OFF = NCH * ZCHUNK;
   static constexpr uint32_t SLOT = Q8 ? KR_OFF : KR_OFF + PCHUNK;   // latent (+ RoPE key) of one tile
   // raw slots: RoPE key, codes; apart from them the ids and the scales
   static constexpr uint32_t RSLOT = Q8 ? PCHUNK + TOK * D_C : 0;
   static constexpr uint32_t RMETA = Q8 ? (GATE ? 2 : 1) * kPage * 4 : 0;
-  static constexpr uint32_t STAT_BYTES = GATE ? 2 * kPage * 4 : 0;   // per slot: mu[64], r[64]
+  static constexpr uint32_t STAT_BYTES = GATE && !ZZ ? 2 * kPage * 4 : 0;   // per slot: mu[64], r[64]
   static constexpr uint32_t QB_LAT = qprep_lat_bytes(D_C);
   static constexpr uint32_t QPREP = qprep_bytes_tc(D_C, kRope);
   static constexpr uint32_t QBUF = (QPREP + 127) / 128 * 128;
@@ -103,7 +107,8 @@ struct Cfg {
   // with half pages the odd latent columns' scores [32 tokens][16]
   static constexpr uint32_t XCH = 1024 + (TOK < kPage ? TOK * kHeads * 4 : 0);
   static constexpr uint32_t MISC = Q8 ? 512 : 1024;
-  static constexpr uint32_t FIXED = kNP * PBUF + GB_BYTES + XCH + MISC + 1024;
+  static constexpr int NP = ZZ && D_C == 256 ? 2 : kNP;   // P' buffers (two make room for the fourth raw slot)
+  static constexpr uint32_t FIXED = NP * PBUF + GB_BYTES + XCH + MISC + 1024;
   // slots with two query buffers (the next segment's loaded while this one is
   // in use) or with one; one buffer when a second would cost a slot below five
   static constexpr int NS2 = (int)((kSmemLimit - FIXED - 2 * QBUF) / (SLOT + STAT_BYTES));
@@ -118,7 +123,7 @@ struct Cfg {
   static constexpr uint32_t OFF_RAW = NS * SLOT;
   static constexpr uint32_t OFF_QBUF = OFF_RAW + NR * RSLOT;
   static constexpr uint32_t OFF_PBUF = OFF_QBUF + NQ * QBUF;
-  static constexpr uint32_t OFF_STAT = OFF_PBUF + kNP * PBUF;
+  static constexpr uint32_t OFF_STAT = OFF_PBUF + NP * PBUF;
   static constexpr uint32_t OFF_META = OFF_STAT + NS * STAT_BYTES;
   static constexpr uint32_t OFF_GB = OFF_META + NR * RMETA;
   static constexpr uint32_t OFF_XCH = OFF_GB + GB_BYTES;
@@ -129,7 +134,9 @@ struct Cfg {
   static constexpr int NMC = (D_C + 127) / 128;
   static constexpr uint32_t S_COLS = 32;
   static constexpr uint32_t COL_S = 0, COL_O = kNB * S_COLS;
-  static constexpr uint32_t TMEM_COLS = 256;
+  // Z [Z ; 1]^T: 64 columns of the tile's rows, 8 of the sums, a block per score buffer
+  [[maybe_unused]] static constexpr uint32_t ZZ_COLS = kPage + 8, COL_ZZ = COL_O + kHeads * NMC;
+  static constexpr uint32_t TMEM_COLS = ZZ ? 512 : 256;
   static constexpr uint32_t PAGE_TX = Q8 ? RSLOT + TOK * 4 : SLOT;
   static constexpr uint32_t ID_TX = GATE ? kPage * 4 : 0;   // the page's token ids
   static constexpr int RING = Q8 ? NR : NS;                 // slots that copies land in
@@ -137,7 +144,7 @@ struct Cfg {
   static_assert(SLOT % 1024 == 0 && RSLOT % 1024 == 0, "swizzle atoms");
   static_assert(SMEM <= kSmemLimit, "shared memory");
   static_assert(D_C == 192 || D_C == 256 || (D_C == 512 && !GATE), "latent widths of this kernel");
-  static_assert(COL_O + kHeads * NMC <= TMEM_COLS && NMC % 2 == 0, "tensor memory");
+  static_assert(COL_O + kHeads * NMC + (ZZ ? kNB * ZZ_COLS : 0) <= TMEM_COLS && NMC % 2 == 0, "tensor memory");
   // the score MMAs read 64 rows: at half pages two atom columns' 32, for the
   // RoPE key its 32 and what follows the slot, whose scores are not used
   static_assert(OFF_QBUF + 64 * 128 <= SMEM, "score operand");
@@ -160,7 +167,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr bool GATE = GM != 0;
   constexpr bool GATE_ADD = GM == 3;             // ablation: c + g
   constexpr bool GATE_LN = GM == 1 || GM == 3;   // LayerNorm after the gate
-  using C = Cfg<D_C, GATE, Q8>;
+  constexpr bool ZZ = Q8 && GM == 1 && D_C == 256;
+  using C = Cfg<D_C, GATE, Q8, ZZ>;
   // The MMA issuers: one thread of the warp, or (d_c 192 gated with a product) the
   // whole warp waiting together and electing a thread for each tile's MMAs.  Steps
   // replayed 24 to a graph, one thread / whole warp: d_c 192 with c (*) g 65.7 / 65.1
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&bars.sready[s]), 2);
       mbar_init(smem_u32(&bars.sfree[s]), kSoftWarps);
     }
-    for (int s = 0; s < kNP; ++s) {
+    for (int s = 0; s < C::NP; ++s) {
       mbar_init(smem_u32(&bars.spdone[s]), kSoftWarps);
       mbar_init(smem_u32(&bars.pfree[s]), 1);
     }
@@ -229,6 +237,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kTmaWarp && lane == 0) {
     if (!Q8) prefetch_tensormap(&cmap);
     prefetch_tensormap(&krmap);
+  }
+  if constexpr (ZZ) {
+    constexpr uint32_t one2 = 0x3f803f80u;   // (no other write reaches these rows)
+    for (int i = threadIdx.x; i < C::NS * C::NCH * 64; i += kThreads)
+      *reinterpret_cast<uint4*>(smem + i / 64 * C::ZCHUNK + C::PCHUNK + i % 64 * 16) = make_uint4(one2, one2, one2, one2);
+    fence_proxy_async_smem();
   }
   tc_fence_before();
   __syncthreads();
@@ -430,12 +444,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           } else {
 #pragma unroll
             for (int kk = 0; kk < D_C / 16; ++kk)
-              mma_bf16_ss(ds, za + (((kk >> 2) * C::PCHUNK + (kk & 3) * 32) >> 4),
+              mma_bf16_ss(ds, za + (((kk >> 2) * C::ZCHUNK + (kk & 3) * 32) >> 4),
                           qb + ((kk * 2 * kQGroupBytes) >> 4), IDESC_S, kk > 0);
 #pragma unroll
             for (int kk = 0; kk < kRope / 16; ++kk)
               mma_bf16_ss(ds + kHeads, ka + ((kk * 32) >> 4),
                           qb + ((C::QB_LAT + kk * 2 * kQGroupBytes) >> 4), IDESC_S, kk > 0);
+          }
+          if constexpr (ZZ) {
+            constexpr uint32_t IDESC_ZZ = idesc_bf16(64, C::ZZ_COLS, 0, 0);
+#pragma unroll
+            for (int kk = 0; kk < D_C / 16; ++kk) {
+              const uint64_t zk = za + (((kk >> 2) * C::ZCHUNK + (kk & 3) * 32) >> 4);
+              mma_bf16_ss(tmem + C::COL_ZZ + sb * C::ZZ_COLS, zk, zk, IDESC_ZZ, kk > 0);
+            }
           }
           mma_commit(smem_u32(&bars.sready[sb]));
           if (Q8) mma_commit(smem_u32(&bars.empty[js % C::RING]));
@@ -466,12 +488,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // O^T[feature, head] += Z^T P' for each tile in order, as soon as the
     // softmax warps wrote its P'; completion frees the page slot and the P'
     // buffer.  A operand: the page slot read MN-major (features along M,
-    // 64-feature atoms PCHUNK apart; tokens along K, 8-row groups 1 KB apart);
+    // 64-feature atoms ZCHUNK apart; tokens along K, 8-row groups 1 KB apart);
     // B: P' MN-major in 8x8 core matrices (token groups 256 B, head halves
     // 128 B).
     if (!DUMP && (WARP_ISSUE || elect_one())) {
       constexpr uint32_t IDESC_O = idesc_bf16(128, kHeads, 1, 1);
-      const uint64_t zdesc_mn = smem_desc(sbase, C::PCHUNK, 1024, kSwizzle128B);
+      const uint64_t zdesc_mn = smem_desc(sbase, C::ZCHUNK, 1024, kSwizzle128B);
       const uint64_t pdesc0 = smem_desc(sbase + C::OFF_PBUF, 256, 128, kSwizzleNone);
       Walker<C::TOK> wo;
       wo.start(p);
@@ -481,22 +503,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       tr.init(p, 1, 1, 2);   // second half of the MMA role's run
       if (WARP_ISSUE && lane != 0) tr.base = nullptr;
       for (int jo = 0; wo.next(to); ++jo) {
-        if (!issuer_wait(bars.spdone[jo % kNP], (jo / kNP) & 1)) break;
+        if (!issuer_wait(bars.spdone[jo % C::NP], (jo / C::NP) & 1)) break;
         tr.mark(3, jo);
         tc_fence_after();
         if (issuer_one()) {
           const int slot = jo % C::NS;
           const uint64_t za = zdesc_mn + ((slot * C::SLOT) >> 4);
-          const uint64_t pb = pdesc0 + (((jo % kNP) * C::PBUF) >> 4);
+          const uint64_t pb = pdesc0 + (((jo % C::NP) * C::PBUF) >> 4);
           const uint32_t keep = to.first ? 0u : 1u;   // a segment's first MMAs overwrite O^T
 #pragma unroll
           for (int ks = 0; ks < C::TOK / 16; ++ks)
 #pragma unroll
             for (int mc = 0; mc < C::NMC; ++mc)
-              mma_bf16_ss(tmem + C::COL_O + kHeads * mc, za + (((C::mc_start(mc) / 64) * C::PCHUNK + ks * 2048) >> 4),
+              mma_bf16_ss(tmem + C::COL_O + kHeads * mc, za + (((C::mc_start(mc) / 64) * C::ZCHUNK + ks * 2048) >> 4),
                           pb + ((ks * 512) >> 4), IDESC_O, ks > 0 ? 1u : keep);
           mma_commit(smem_u32(Q8 ? &bars.zfree[slot] : &bars.empty[slot]));
-          mma_commit(smem_u32(&bars.pfree[jo % kNP]));
+          mma_commit(smem_u32(&bars.pfree[jo % C::NP]));
         }
         issuer_join();
         tr.mark(4, jo);
@@ -560,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     // shared-memory offset of unit (kGateUnits pp + h) of column fc of this thread's row
     auto unit_off = [&](int fc, int h) -> uint32_t {
-      return fc * C::PCHUNK + row * 128 + (((kGateUnits * pp + h) ^ (row & 7)) << 4);
+      return fc * C::ZCHUNK + row * 128 + (((kGateUnits * pp + h) ^ (row & 7)) << 4);
     };
     Tracer tr;
     tr.init(p, 2);
@@ -695,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               z.z = mul_bf16x2(c4.z, g[fc][h].z);
               z.w = mul_bf16x2(c4.w, g[fc][h].w);
               if (!full_page && !valid) z = make_uint4(0, 0, 0, 0);
-              if (GATE_LN) {
+              if (GATE_LN && !ZZ) {
                 sum_bf16x2(z.x, s1, s2);
                 sum_bf16x2(z.y, a1, a2);
                 sum_bf16x2(z.z, s1, s2);
@@ -708,16 +730,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (fc > 0) load_next(fc);
           }
           tr.mark(6, j);
-          float mu = 0.f, r = 1.f;
-          if (GATE_LN) {
-            float sum1, sum2;
-            row_sums(sum1, sum2);
-            mu = sum1 * inv_dc;
-            r = rsqrtf(fmaxf(sum2 * inv_dc - mu * mu, 0.f) + p.eps);
-          }
-          if (pp == 0) {
-            st[row] = valid ? mu : 0.f;
-            st[kPage + row] = valid ? r : 1.f;
+          if constexpr (!ZZ) {
+            float mu = 0.f, r = 1.f;
+            if (GATE_LN) {
+              float sum1, sum2;
+              row_sums(sum1, sum2);
+              mu = sum1 * inv_dc;
+              r = rsqrtf(fmaxf(sum2 * inv_dc - mu * mu, 0.f) + p.eps);
+            }
+            if (pp == 0) {
+              st[row] = valid ? mu : 0.f;
+              st[kPage + row] = valid ? r : 1.f;
+            }
           }
         }
         tr.mark(2, j);
@@ -811,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint4 z = widen.unit(hh ? codes[i].z : codes[i].x, hh ? codes[i].w : codes[i].y);
               if (more) widen.finish(z);
               if (qrow >= t.ntok) z = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(cpage + (i * (C::NCH / kQCols) + qsub) * C::PCHUNK + qrow * 128 +
+              *reinterpret_cast<uint4*>(cpage + (i * (C::NCH / kQCols) + qsub) * C::ZCHUNK + qrow * 128 +
                                         (((2 * (lane % 4) + hh) ^ (qrow & 7)) << 4)) = z;
             }
           }
@@ -1040,7 +1064,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok) warp_arrive(smem_u32(&bars.qempty[seg % C::NQ]));
       }
-      const int slot = it % C::NS, sb = it % kNB, pb = it % kNP;
+      const int slot = it % C::NS, sb = it % kNB, pb = it % C::NP;
       tr.mark(0, it);
       // scores of this tile; the MMA warp's release arrival on the same barrier
       // orders the gate's statistics before them
@@ -1053,7 +1077,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok) {
         tc_fence_after();
         tmem_ld_16x256b_x4(tq + C::COL_S + sb * C::S_COLS, v);
-        if (GATE) {
+        float zz[8], zs[4];
+        if constexpr (ZZ) {
+          // the diagonal's 16 columns of this warp's rows, and the sums
+          const uint32_t dz = tq + C::COL_ZZ + sb * C::ZZ_COLS;
+          tmem_ld_16x256b_x2(dz + 16 * warp, zz);
+          tmem_ld_16x256b_x1(dz + kPage, zs);
+        } else if (GATE) {
           const float* st = reinterpret_cast<const float*>(smem + C::OFF_STAT + slot * C::STAT_BYTES);
           mu[0] = st[r0];
           mu[1] = st[r1];
@@ -1061,6 +1091,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           rr[1] = st[kPage + r1];
         }
         tmem_wait_ld();
+        if constexpr (ZZ) {
+          // row i = lane / 4 of the warp's has its square sum in column i, held by lane 4 i +
+          // i / 2, row i + 8 in column i + 8
+          const int i = lane >> 2, owner = (lane & ~3) | (i >> 1);
+          constexpr float inv_dc = 1.f / D_C;
+          const float sq[2] = {__shfl_sync(0xffffffffu, i & 1 ? zz[1] : zz[0], owner),
+                               __shfl_sync(0xffffffffu, i & 1 ? zz[7] : zz[6], owner)};
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            mu[e] = zs[2 * e] * inv_dc;
+            rr[e] = rsqrtf(fmaxf(fmaf(sq[e], inv_dc, -mu[e] * mu[e]), 0.f) + p.eps);
+          }
+        }
         tc_fence_before();
         warp_arrive(smem_u32(&bars.sfree[sb]));   // score buffer read: tile it + kNB may overwrite it
         tr.mark(7, it);
@@ -1136,9 +1179,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!t.first && __any_sync(0xffffffffu, lane < kHeads && alpha != 1.f)) {
           // O^T and the running sums were accumulated against the old
           // reference: the previous tile's output MMA must be complete first
-          // (completion n of pfree[b] is output MMA n kNP + b)
-          const int pv = (it - 1) % kNP;
-          ok = warp_wait(smem_u32(&bars.pfree[pv]), ((it - 1) / kNP) & 1, abort_flag, wait_ns);
+          // (completion n of pfree[b] is output MMA n NP + b)
+          const int pv = (it - 1) % C::NP;
+          ok = warp_wait(smem_u32(&bars.pfree[pv]), ((it - 1) / C::NP) & 1, abort_flag, wait_ns);
           if (ok) {
             tc_fence_after();
 #pragma unroll
@@ -1160,9 +1203,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      // the P' buffer of this tile is free once the output MMA kNP tiles back
+      // the P' buffer of this tile is free once the output MMA NP tiles back
       // has read it
-      ok = ok && warp_wait(smem_u32(&bars.pfree[pb]), ((it / kNP) & 1) ^ 1, abort_flag, wait_ns);
+      ok = ok && warp_wait(smem_u32(&bars.pfree[pb]), ((it / C::NP) & 1) ^ 1, abort_flag, wait_ns);
       tr.mark(5, it);
       if (ok) {
         // The output MMA sees the bf16-rounded weights P'; the denominator and
@@ -1227,8 +1270,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         // the segment's last output MMA (the earlier ones complete before it;
-        // completion n of pfree[b] is output MMA n kNP + b), then O^T
-        ok = warp_wait(smem_u32(&bars.pfree[pb]), (it / kNP) & 1, abort_flag, wait_ns);
+        // completion n of pfree[b] is output MMA n NP + b), then O^T
+        ok = warp_wait(smem_u32(&bars.pfree[pb]), (it / C::NP) & 1, abort_flag, wait_ns);
         if (ok) {
           tc_fence_after();
           const int slot_out = blockIdx.x + t.b;
@@ -1304,7 +1347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <int D_C, int GM, int DBG>
 cudaError_t launch_one(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_t st, bool* fused) {
-  using C = Cfg<D_C, GM != 0, DBG == 4>;
+  using C = Cfg<D_C, GM != 0, DBG == 4, DBG == 4 && GM == 1 && D_C == 256>;
   auto kern = decode_tc_kernel<D_C, GM, DBG>;
   cudaError_t e = allow_smem(kern, C::SMEM);
   if (e != cudaSuccess) return e;

@@ -8,10 +8,11 @@ values of at most m (|x| + |y|); then the rounding of the output, half a step of
 eg_mla_append_latent_q8 is whole numbers: codes and scales equal a search over e4m3's
 grid in 64 bits, bit for bit.  eg_mla_read_latent_q8 gives scale x code exactly.
 
-eg_mla_decode_q8 equals eg_mla_decode over the values read back, bit for bit, and is within
-the hot path's bounds (rel-L2 5e-3) of the oracle on them.  Ungated at d_c 256 and 512 it
-multiplies the codes themselves and is held to those bounds alone; two results that keep
-them are within 1e-2 of each other."""
+eg_mla_decode_q8 is within the hot path's bounds (rel-L2 5e-3) of the oracle on the values
+read back, and so within 1e-2 of eg_mla_decode over them.  Where it differs from that only
+in how it comes by these values (fp32, d_c 192, the ablation gates) the two are equal, bit
+for bit; with LN(c (*) g) at d_c 256 its sums come in another order, and ungated at d_c 256 and
+512 it multiplies the codes themselves."""
 import dataclasses
 import importlib.util
 import math
@@ -522,6 +523,10 @@ def plain(d_c, gate):
     return gate == "none" and d_c in (256, 512)
 
 
+def bitwise(d_c, gate):
+    return (d_c, gate) != (256, "mul_ln") and not plain(d_c, gate)
+
+
 def apart(got, want):
     got, want = got.double(), want.double()
     return float((got - want).norm() / want.norm())
@@ -560,10 +565,10 @@ def test_decode_equals_the_decode_over_what_it_holds(gpu_lib, d_c, gate, lens):
         got = decode_q8(dc, cache)
         dc.c_pool.copy_(back)
         want = dc.decode(out=torch.full_like(dc.out, 9))
-        if plain(d_c, gate):
-            assert apart(got, want) <= 1e-2, splits
-        else:
+        if bitwise(d_c, gate):
             assert torch.equal(got, want), splits
+        else:
+            assert apart(got, want) <= 1e-2, splits
         assert dc.read_status() == 0
     ref_case = dataclasses.replace(case, c_pool=device.bf16_tensor_to_bits(back))
     u = device.output_f64(got)
@@ -594,7 +599,7 @@ def test_decode_of_batches_and_widths(gpu_lib, batch, d_nope, d_v):
         got = decode_q8(dc, cache)
         dc.c_pool.copy_(back)
         want = dc.decode(out=torch.full_like(dc.out, 9))
-        assert apart(got, want) <= 1e-2 if plain(d_c, gate) else torch.equal(got, want)
+        assert torch.equal(got, want) if bitwise(d_c, gate) else apart(got, want) <= 1e-2
         assert dc.read_status() == 0
         if plain(d_c, gate):
             assert apart(got, reference64(dc, back)) <= 5e-3
@@ -642,10 +647,15 @@ def test_decode_of_small_and_large_scales_and_every_code(gpu_lib, d_c, gate, pow
     assert torch.equal(back.double().view(n, P, d_c), value)
     got = decode_q8(dc, cache)
     dc.c_pool.copy_(back.view(n, P, d_c))
+    want = dc.decode(out=torch.full_like(dc.out, 9))
     if plain(d_c, gate):
         assert apart(got * 2.0 ** -power, reference64(dc, dc.c_pool) * 2.0 ** -power) <= 5e-3
-    else:
-        assert same(got, dc.decode(out=torch.full_like(dc.out, 9)))
+    elif bitwise(d_c, gate):
+        assert same(got, want)
+    elif power < 60:
+        assert apart(got, want) <= 1e-2
+    else:   # (squares of these latents are above fp32's range in both)
+        assert bool(got.isnan().all()) and bool(want.isnan().all())
     assert dc.read_status() == 0
 
 
@@ -886,12 +896,12 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 @pytest.mark.parametrize("kw", [dict(), dict(prompts=(1,), steps=1), dict(prompts=(64, 63, 700, 5), steps=70)])
 def test_example_agrees_with_the_cache_in_bf16(gpu_lib, kw):
-    """The loop over the cache in 8 bits against the same tokens' values in a bf16 cache (bit for bit), and against
-    the unrounded bf16 cache.  A code is off by at most 2^-4 of its value, evenly spread, so a latent by 2^-4 / sqrt(3) =
+    """The loop over the cache in 8 bits against the same tokens' values in a bf16 cache (both within rel-L2 5e-3 of
+    the exact result), and against the unrounded bf16 cache.  A code is off by at most 2^-4 of its value, evenly spread, so a latent by 2^-4 / sqrt(3) =
     3.6e-2 relative in each entry; LayerNorm, weights and values pass on an error of that size at most, and the
     attention's mean over several tokens makes it smaller."""
     spec = importlib.util.spec_from_file_location("serve_q8", os.path.join(ROOT, "examples", "serve_q8.py"))
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
-    exact, rounded, all_free, status = mod.main(**kw)
-    assert exact and rounded <= 0.1 and all_free and status == 0
+    values_apart, rounded, all_free, status = mod.main(**kw)
+    assert values_apart <= 1e-2 and rounded <= 0.1 and all_free and status == 0
