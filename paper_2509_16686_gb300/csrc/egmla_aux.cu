@@ -1133,7 +1133,7 @@ decode_f32_kernel(const void* __restrict__ c_pool, const float* __restrict__ sca
                 q8_decode4(__ldg(static_cast<const uint32_t*>(c_pool) + (row0 + t) * ncol + u), x);
                 z[k][i] = make_float4(s * x[0], s * x[1], s * x[2], s * x[3]);
               } else {
-                z[k][i] = __ldg(static_cast<const float4*>(c_pool) + (row0 + t) * ncol + u);
+                z[k][i] = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(c_pool) + (row0 + t) * d_c) + u);
               }
               if (gate) gv[k][i] = __ldg(reinterpret_cast<const float4*>(gate_table + static_cast<size_t>(id[k]) * d_c) + u);
             }

@@ -135,7 +135,7 @@ struct Cfg {
   static constexpr uint32_t S_COLS = 32;
   static constexpr uint32_t COL_S = 0, COL_O = kNB * S_COLS;
   // Z [Z ; 1]^T: 64 columns of the tile's rows, 8 of the sums, a block per score buffer
-  [[maybe_unused]] static constexpr uint32_t ZZ_COLS = kPage + 8, COL_ZZ = COL_O + kHeads * NMC;
+  static constexpr uint32_t ZZ_COLS = kPage + 8, COL_ZZ = COL_O + kHeads * NMC;
   static constexpr uint32_t TMEM_COLS = ZZ ? 512 : 256;
   static constexpr uint32_t PAGE_TX = Q8 ? RSLOT + TOK * 4 : SLOT;
   static constexpr uint32_t ID_TX = GATE ? kPage * 4 : 0;   // the page's token ids
@@ -144,7 +144,7 @@ struct Cfg {
   static_assert(SLOT % 1024 == 0 && RSLOT % 1024 == 0, "swizzle atoms");
   static_assert(SMEM <= kSmemLimit, "shared memory");
   static_assert(D_C == 192 || D_C == 256 || (D_C == 512 && !GATE), "latent widths of this kernel");
-  static_assert(COL_O + kHeads * NMC + (ZZ ? kNB * ZZ_COLS : 0) <= TMEM_COLS && NMC % 2 == 0, "tensor memory");
+  static_assert(COL_O + kHeads * NMC + (ZZ ? COL_ZZ - COL_O - kHeads * NMC + kNB * ZZ_COLS : 0) <= TMEM_COLS && NMC % 2 == 0, "tensor memory");
   // the score MMAs read 64 rows: at half pages two atom columns' 32, for the
   // RoPE key its 32 and what follows the slot, whose scores are not used
   static_assert(OFF_QBUF + 64 * 128 <= SMEM, "score operand");
@@ -587,14 +587,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     Tracer tr;
     tr.init(p, 2);
     if (threadIdx.x != kGateWarp0 * 32) tr.base = nullptr;
-    // Q8: this thread's row of the codes, its part of the row's 64-feature columns
-    // (qsub, qsub + kQSubs, ..: four lanes a row, eight with half pages), and 16 codes of
-    // each, which are the units 2 (lane % 4) and the next of the column's bf16 values
-    constexpr int kQSubs = kPage / C::TOK, kQCols = C::NCH / kQSubs;
-    const int qrow = gw * (C::TOK / kGateWarps) + lane / (4 * kQSubs), qsub = lane / 4 % kQSubs;
-    uint4 codes[Q8 ? kQCols : 1];
+    // Q8: 16 codes of every 64-feature column of this thread's row, which are the units 2 pp
+    // and the next of the column's bf16 values
+    uint4 codes[Q8 ? C::NCH : 1];
     Q8Widen widen;
-    static_assert(!Q8 || (kGateWarps == 8 && (!GATE || kQSubs == 1)), "rows of the codes");
+    static_assert(!Q8 || (kGateWarps == 8 && C::TOK == kPage), "rows of the codes");
     Tile t, t1;
     bool have = w.next(t);
     bool have1 = have && w.next(t1);
@@ -815,28 +812,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         const bool full_page = t.ntok == C::TOK;   // uniform: no token masking needed
         if constexpr (Q8) {
-          // the tile's codes into registers, and the latent slot of the tile (output
-          // MMAs of the tile NS before it complete)
-          const uint8_t* raw = smem + C::OFF_RAW + (j % C::RING) * C::RSLOT + C::PCHUNK;
-          const float* scales = reinterpret_cast<const float*>(smem + C::OFF_META + (j % C::RING) * C::RMETA);
-          raw += qrow * D_C + qsub * 64 + 16 * (lane % 4);
+          // (ungated: the values alone)
+          const uint8_t* raw = smem + C::OFF_RAW + (j % C::RING) * C::RSLOT + C::PCHUNK + row * D_C + 16 * pp;
 #pragma unroll
-          for (int i = 0; i < kQCols; ++i) codes[i] = *reinterpret_cast<const uint4*>(raw + i * (C::NCH / kQCols) * 64);
-          widen.set(scales[qrow]);
+          for (int fc = 0; fc < C::NCH; ++fc) codes[fc] = *reinterpret_cast<const uint4*>(raw + fc * 64);
+          widen.set(reinterpret_cast<const float*>(smem + C::OFF_META + (j % C::RING) * C::RMETA)[row]);
           const bool more = widen.unfinished();
+          // the latent slot of the tile (output MMAs of the tile NS before it complete)
           if (!warp_wait(smem_u32(&bars.zfree[slot]), ((j / C::NS) & 1) ^ 1, abort_flag, wait_ns)) break;
 #pragma unroll
-          for (int i = 0; i < kQCols; ++i) {
+          for (int fc = 0; fc < C::NCH; ++fc) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              // (of a row shared by eight lanes, the second four write their units in
-              // the other order, so that the eight meet different banks)
-              const int hh = kQSubs > 1 ? h ^ qsub : h;
-              uint4 z = widen.unit(hh ? codes[i].z : codes[i].x, hh ? codes[i].w : codes[i].y);
+              uint4 z = widen.unit(h ? codes[fc].z : codes[fc].x, h ? codes[fc].w : codes[fc].y);
               if (more) widen.finish(z);
-              if (qrow >= t.ntok) z = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(cpage + (i * (C::NCH / kQCols) + qsub) * C::ZCHUNK + qrow * 128 +
-                                        (((2 * (lane % 4) + hh) ^ (qrow & 7)) << 4)) = z;
+              if (row >= t.ntok) z = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(cpage + unit_off(fc, h)) = z;
             }
           }
         } else if (GATE) {
@@ -1035,7 +1026,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // d_c 512, ten seeds: 2.311e-3 without, 2.261e-3 with; whole-page tiles 2.284e-3).
     float lazy = kLazyLog2;
     bool was_first = false;
-    while (w.next(t)) {
+    // ZZ: the softmax is the longest role beside the gate; the next tile is found, and the P'
+    // buffer waited for, while the scores come out of TMEM (45.0 -> 44.6 us for 8 x 32K; at
+    // d_c 192 without ZZ the same took 76.7 us instead of 73.4 for 128 ragged)
+    Tile tn;
+    bool next_tile = ZZ && w.next(t);
+    while (ZZ ? next_tile : w.next(t)) {
       bool ok = true;
       if constexpr (C::TOK < kPage) {
         lazy = was_first && t.tok0 % kPage != 0 ? 0.f : kLazyLog2;
@@ -1071,7 +1067,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = ok && warp_wait(smem_u32(&bars.sready[sb]), (it / kNB) & 1, abort_flag, wait_ns);
       tr.mark(1, it);
       float s[2][4];
-      float mu[2] = {0.f, 0.f}, rr[2] = {1.f, 1.f};
+      float mu[2] = {0.f, 0.f}, rr[2] = {1.f, 1.f}, sd[2] = {1.f, 1.f};   // (ZZ: sd = 1 / rr)
       bool exceed = false;
       float v[16];
       if (ok) {
@@ -1090,6 +1086,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           rr[0] = st[kPage + r0];
           rr[1] = st[kPage + r1];
         }
+        if constexpr (ZZ) {
+          tn = t;
+          next_tile = w.next(tn);
+          ok = warp_wait(smem_u32(&bars.pfree[pb]), ((it / C::NP) & 1) ^ 1, abort_flag, wait_ns);
+        }
         tmem_wait_ld();
         if constexpr (ZZ) {
           // row i = lane / 4 of the warp's has its square sum in column i, held by lane 4 i +
@@ -1101,7 +1102,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             mu[e] = zs[2 * e] * inv_dc;
-            rr[e] = rsqrtf(fmaxf(fmaf(sq[e], inv_dc, -mu[e] * mu[e]), 0.f) + p.eps);
+            const float var = fmaxf(fmaf(sq[e], inv_dc, -mu[e] * mu[e]), 0.f) + p.eps;
+            rr[e] = rsqrtf(var);
+            sd[e] = var * rr[e];
           }
         }
         tc_fence_before();
@@ -1205,7 +1208,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // the P' buffer of this tile is free once the output MMA NP tiles back
       // has read it
-      ok = ok && warp_wait(smem_u32(&bars.pfree[pb]), ((it / C::NP) & 1) ^ 1, abort_flag, wait_ns);
+      if (!ZZ) ok = ok && warp_wait(smem_u32(&bars.pfree[pb]), ((it / C::NP) & 1) ^ 1, abort_flag, wait_ns);
       tr.mark(5, it);
       if (ok) {
         // The output MMA sees the bf16-rounded weights P'; the denominator and
@@ -1217,7 +1220,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = e ? r1 : r0;
-          const float ri = GATE ? 1.f / rr[e] : 1.f;
+          const float ri = ZZ ? sd[e] : GATE ? 1.f / rr[e] : 1.f;
           float pq[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) pq[k] = ex2_approx(s[e][k] - m_ref[k]) * rr[e];
@@ -1329,6 +1332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           bmu_acc[k] = 0.f;
         }
       }
+      if constexpr (ZZ) t = tn;
       ++it;
     }
   }
@@ -1381,9 +1385,11 @@ bool tc_supported(int d_c, int gate) {
 // none and mul_ln (the others run untraced)
 template <int GM>
 cudaError_t launch_mode(const DecodeArgs& a, const CUtensorMap* maps, cudaStream_t st, bool* fused) {
-  if (a.scale_pool != nullptr) {
+  if (a.scale_pool != nullptr) {   // (ungated, the other widths: egmla_decode_q8.cu)
     if (a.d_c == 192) return launch_one<192, GM, 4>(a, maps, st, fused);
-    if (a.d_c == 256) return launch_one<256, GM, 4>(a, maps, st, fused);
+    if constexpr (GM != 0) {
+      if (a.d_c == 256) return launch_one<256, GM, 4>(a, maps, st, fused);
+    }
     return cudaErrorInvalidValue;
   }
   if constexpr (GM <= 1) {
@@ -1412,8 +1418,7 @@ cudaError_t launch_decode_tc(const DecodeArgs& a, const CUtensorMap* maps, bool 
     return cudaErrorInvalidValue;
   }
   if (!a.gate) {
-    if (a.d_c == 512)
-      return a.scale_pool != nullptr ? launch_one<512, 0, 4>(a, maps, st, fused) : launch_one<512, 0, 0>(a, maps, st, fused);
+    if (a.d_c == 512 && a.scale_pool == nullptr) return launch_one<512, 0, 0>(a, maps, st, fused);
     return launch_mode<0>(a, maps, st, fused);
   }
   if (a.gate_add) return launch_mode<3>(a, maps, st, fused);
