@@ -879,7 +879,7 @@ int eg_mla_debug_linear_plan(int32_t n_out, int32_t k, int32_t batch, int32_t* c
 /*
  * eg_mla_debug_set_trace - pipeline event trace of the split-KV decode kernel
  * (a debugging aid, off by default).  With a device buffer set, later calls of
- * eg_mla_decode at d_c 192 or 256 in the gate modes none and mul_ln run a
+ * eg_mla_decode (not eg_mla_decode_q8) at d_c 192 or 256 in the gate modes none and mul_ln run a
  * separately compiled traced build of the kernel (same results; the untraced
  * build carries no trace code), whose first `ctas` CTAs record, per role (0 TMA producer,
  * 1 MMA issuers: the score issuer in the first half of the run, the output
@@ -895,7 +895,7 @@ int eg_mla_debug_set_trace(void* dev_buf, int64_t bytes, int32_t ctas);
 
 /*
  * eg_mla_debug_set_fault - test entry for the failure path of the split-KV
- * decode kernel (bf16).  With cta >= 0, later eg_mla_decode calls withhold one
+ * decode kernel (bf16).  With cta >= 0, later eg_mla_decode (and _q8) calls withhold one
  * page copy: CTA `cta` skips the copy of its tile `tile` (0-based in its walk; a
  * page, half a page at d_c 512) and its arrival, and every pipeline wait of
  * those launches gives up after wait_limit_ns (1 us .. 2 s) instead of the default

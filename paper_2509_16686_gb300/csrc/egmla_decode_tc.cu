@@ -76,10 +76,23 @@ namespace {
 // Q8: the cache holds the latent in 8 bits (egmla_q8.cuh).  The page's codes, scales and
 // ids and its RoPE keys land in a ring of raw slots, from which the gate warps write the
 // bf16 tile into a ring of latent slots: a raw slot is held until the tile's score MMAs
-// are complete, a latent slot from the gate to its output MMAs.
-// ZZ (with Q8 and LN(c (*) g)): the LayerNorm's sums of a tile come from the tensor cores:
-// Z [Z ; 1]^T, whose diagonal holds every row's sum of squares and whose last columns its
-// sum.  Eight rows of ones behind the tile's 64 in each of its columns.
+// are complete, a latent slot from the gate to its output MMAs.  (us for 8 x 32K at d_c 256
+// and 128 ragged sequences at d_c 192, before ZZ: three latent slots and four raw ones 47.2
+// and 75.7; four, and three and four raw ones, 48.5 and 73.9.)
+//
+// With 8 bits the copies bring 57 instead of 73 KB per page with its gate rows, and memory
+// no longer counts: the gate warps do, which have to widen the codes (4.5 operations a
+// pair of values beside the six of gate, sums and store), then the softmax.  44.5 us for 8
+// x 32K tokens where a bf16 cache takes 45.7 and the bytes 17.9; without the gate's work,
+// timed with its instructions left out, 40.  More warps for either role (twelve for the
+// gate, eight for the softmax), at 96 registers each instead of 128, were slower: 57 and 54.
+// ZZ (with Q8 and LN(c (*) g) at d_c 256): the LayerNorm's sums of a tile come from the tensor
+// cores: Z [Z ; 1]^T, whose diagonal holds every row's sum of squares and whose last
+// columns its sum.  Eight rows of ones behind the tile's 64 in each of its columns.  The
+// tensor pipe is idle for nine tenths of the time, and the gate saves a third of its
+// arithmetic and the row sums' shuffles: 8 x 32K 46.9 -> 45.0 us, 4 of 60 to 700 tokens 12.3
+// -> 12.9.  At d_c 192, where the softmax takes longer than the gate, 128 ragged sequences
+// went from 73.4 to 74.9.
 template <int D_C, bool GATE, bool Q8 = false, bool ZZ = false>
 struct Cfg {
   static constexpr int NCH = D_C / 64;                  // 64-feature swizzle-atom columns

@@ -5,6 +5,11 @@
 // Packed token k belongs to the sequence b with cu[b] <= k < cu[b + 1], as its token
 // k - cu[b], at position positions[b] + k - cu[b] (cu null: to sequence k, at
 // positions[k]).  A warp finds b for its token by ballots over 32 offsets at a time.
+//
+// All three calls are bound by memory: every row is read once and written once, in 16-byte
+// units with several in flight per lane, by warps that need nothing of one another.
+// Blocks of four warps: with eight, whose slots free up together, 32K tokens' rope took
+// 69.2 us instead of 63.9.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -32,22 +37,26 @@ struct Packed {
   int32_t* status;
 };
 
-// Sequence and position of packed token k, the same in every lane; false for a token of
-// no sequence or of one with a negative position.
-__device__ __forceinline__ bool find_token(const Packed& p, int k, int lane, int& b, int64_t& pos) {
-  int first = k;   // the sequence's first packed token
-  b = k;
+// Sequence of packed token k, the same in every lane: how many of cu[1 .. batch] are <= k;
+// `batch` behind the last one.
+__device__ __forceinline__ int sequence_of(const Packed& p, int k, int lane) {
+  int b = 0, n = p.batch;
+  while (n > 0) {
+    const int step = (n + 31) / 32, i = (lane + 1) * step;
+    const bool below = i <= n && __ldg(p.cu + b + i) <= k;
+    const int c = __popc(__ballot_sync(0xffffffffu, below));
+    b += c * step;
+    n = min(n - c * step, step - 1);
+  }
+  return b;
+}
+
+// Position of packed token k, the same in every lane; false for a token of no sequence or of
+// one with a negative position.
+__device__ __forceinline__ bool find_position(const Packed& p, int k, int lane, int64_t& pos) {
+  int first = k, b = k;   // the sequence's first packed token
   if (p.cu != nullptr) {
-    // how many of cu[1 .. batch] are <= k
-    int n = p.batch;
-    b = 0;
-    while (n > 0) {
-      const int step = (n + 31) / 32, i = (lane + 1) * step;
-      const bool below = i <= n && __ldg(p.cu + b + i) <= k;
-      const int c = __popc(__ballot_sync(0xffffffffu, below));
-      b += c * step;
-      n = min(n - c * step, step - 1);
-    }
+    b = sequence_of(p, k, lane);
     if (b >= p.batch) return false;   // a row behind the last sequence
     first = __ldg(p.cu + b);
     if (first > k) {   // (no token of offsets that begin above 0 or decrease)
@@ -172,6 +181,9 @@ struct Deal {
 // part.  Rows, heads and their rotated parts consist of 16-byte units, each read once,
 // kUnroll of them in flight per lane, the first before the token's angles are known.  The
 // angles are taken once per warp and token, a pair per lane, and shared by all heads.
+// 32,768 tokens of 16 heads of 128 + 64 and a key, from projection rows to dense ones (411
+// MB): 63.8 us, 6.4 TB/s, 95 % of the copy rate (with two units in flight 73.9, three 70.0;
+// a pair of bf16 values at a time, as below, 229).
 template <typename T, bool HALF>
 __global__ void __launch_bounds__(kTokThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int kUnroll = 4;
@@ -200,9 +212,8 @@ __global__ void __launch_bounds__(kTokThreads) rope_kernel(const __grid_constant
     for (int j = 0; j < kUnroll; ++j, d.next())
       if (d.h < hend) item[j].load(d.h < a.H ? q + d.h * stride + nope : key, d.r, items);
   }
-  int b;
   int64_t pos;
-  if (!find_token(a.tok, k, lane, b, pos)) return;
+  if (!find_position(a.tok, k, lane, pos)) return;
   if (nope > 0 && !a.q_in_place && a.q != nullptr) {
     Deal d(h0, nope, lane);
     const int end = min(h1, a.H);
@@ -239,9 +250,8 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = blockIdx.x * kTokWarps + warp;
   grid_dependency_wait();
-  int b;
   int64_t pos;
-  if (k >= a.tok.tokens || !find_token(a.tok, k, lane, b, pos)) return;
+  if (k >= a.tok.tokens || !find_position(a.tok, k, lane, pos)) return;
   const int pairs = a.dr / 2, heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
   float2* cs = table[warp];
   for (int i = lane; i < pairs; i += 32) cs[i] = turn_cos_sin(static_cast<uint64_t>(pos) * a.turn[i], a.magnitude);
@@ -264,15 +274,19 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
   }
 }
 
-// Parts that a token's heads are cut into: as many as leave every SM kRopeWarps warps.
-constexpr int kRopeWarps = 16;
+// Parts that a token's heads are cut into: as many as give every SM eight warps, and two up
+// to sixteen.  us with one part / with the rule: 1 token 3.1 / 2.5, 64 tokens 3.4 / 2.8,
+// 256 3.4 / 2.9, 1024 4.0 / 3.6, 2048 5.6 / 4.8, 4096 (one part) 10.0; as many as give
+// sixteen: 256 tokens 3.4, 512 3.4 (rule 3.2).
+constexpr int kRopeWarps = 8;
 template <typename T>
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
   auto on = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; };
   const int e = sizeof(T);
   const bool units = a.dn * e % 16 == 0 && a.dr * e % (a.half ? 32 : 16) == 0 && on(a.q, a.q_stride) &&
                      on(a.q_out, a.q_out_stride) && on(a.k, a.k_stride) && on(a.k_out, a.k_out_stride);
-  const int want = (kSms * kRopeWarps - 1) / a.tok.tokens + 1;
+  int want = (kSms * kRopeWarps - 1) / a.tok.tokens + 1;
+  if (want < 2 && a.tok.tokens <= 2 * kSms * kRopeWarps) want = 2;
   const dim3 grid((a.tok.tokens + kTokWarps - 1) / kTokWarps, want < a.H + 1 ? want : a.H + 1), block(kTokThreads);
   if (!units) return launch_chained(rope_any_kernel<T>, grid, block, 0, st, a);
   return a.half ? launch_chained(rope_kernel<T, true>, grid, block, 0, st, a)
@@ -297,9 +311,8 @@ struct CacheArgs {
 // Rows of the pool of the packed tokens k0 .. k0 + T - 1: lane i < T gets token i's, -1 for none.
 template <int T>
 __device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) {
-  int b = 0;
-  int64_t pos = -1;
-  if (T > 1 && a.tok.cu != nullptr && a.tok.batch <= 32) {
+  int b = k0 + lane;
+  if (a.tok.cu != nullptr && a.tok.batch <= 32) {
     // every offset in a lane: the tokens' sequences by a ballot each
     const int end = lane < a.tok.batch ? __ldg(a.tok.cu + lane + 1) : INT32_MAX;
 #pragma unroll
@@ -307,20 +320,26 @@ __device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) 
       const int n = __popc(__ballot_sync(0xffffffffu, end <= k0 + i && lane < a.tok.batch));
       if (lane == i) b = n;
     }
-    if (lane < T && k0 + lane < a.tok.tokens && b < a.tok.batch) {
-      const int first = __ldg(a.tok.cu + b), start = a.tok.positions != nullptr ? __ldg(a.tok.positions + b) : 0;
-      if (first > k0 + lane) report_status(a.tok.status, kStatusOutOfRange);
-      else if (start >= 0) pos = static_cast<int64_t>(start) + (k0 + lane) - first;
-    }
-  } else {
-    for (int i = 0; i < T && k0 + i < a.tok.tokens; ++i) {
-      int bi;
-      int64_t pi;
-      if (find_token(a.tok, k0 + i, lane, bi, pi) && lane == i) {
-        b = bi;
-        pos = pi;
+  } else if (a.tok.cu != nullptr) {
+    // a search for the first token, and for another only where its sequence ends before it
+    int found = 0, end = INT32_MIN;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      if (k0 + i >= end) {
+        found = sequence_of(a.tok, k0 + i, lane);
+        end = found < a.tok.batch ? __ldg(a.tok.cu + found + 1) : INT32_MAX;
       }
+      if (lane == i) b = found;
     }
+  }
+  int64_t pos = -1;
+  if (lane < T && k0 + lane < a.tok.tokens && b < a.tok.batch) {
+    const int first = a.tok.cu != nullptr ? __ldg(a.tok.cu + b) : b;
+    const int start = a.tok.positions != nullptr ? __ldg(a.tok.positions + b) : 0;
+    if (first > k0 + lane)
+      report_status(a.tok.status, kStatusOutOfRange);
+    else if (start >= 0)
+      pos = static_cast<int64_t>(start) + k0 + lane - first;
   }
   if (pos < 0) return -1;
   const int64_t lp = pos / kPage;
@@ -369,7 +388,8 @@ __device__ __forceinline__ void store8(uint8_t* row, int unit, const float (&x)[
 
 // A warp per T tokens, eight features of the latent a lane and turn (TURNS of them).  The
 // tokens' rows are requested before their places are looked up, a chain of three
-// dependent loads that T tokens share.
+// dependent loads that T tokens share.  32,768 tokens at d_c 256 (34 MB): 8.6 us, 3.9 TB/s;
+// with one token a warp 13.1, two 9.9, eight 10.8.
 template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_constant__ CacheArgs a) {
   const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
@@ -424,7 +444,8 @@ __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_con
   }
 }
 
-// A warp per T tokens, likewise.
+// A warp per T tokens, likewise.  85K tokens at d_c 256 (66 MB): 13.9 us, 4.8 TB/s, with one
+// token a warp 21.1, two 16.1, eight 16.3 (their last wave is nearly empty).
 template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) read_q8_kernel(const __grid_constant__ CacheArgs a) {
   const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
@@ -470,8 +491,10 @@ __global__ void __launch_bounds__(kTokThreads) read_q8_kernel(const __grid_const
 }
 
 // Tokens per warp: one while that leaves every SM no more than kTokFew warps, so that the
-// fewest tokens wait for one another; else T.
-constexpr int kTokFew = 16;
+// fewest tokens wait for one another; else T.  us to read, one / four a warp: 64 tokens 2.1
+// / 2.6, 1024 2.3 / 2.7, 3000 2.5 / 2.9, 5000 3.0 / 3.0, 8000 3.5 / 3.2; to write 64 2.3 / 2.4,
+// 3000 2.8 / 2.8, 8000 4.0 / 3.3.
+constexpr int kTokFew = 32;
 template <int T, typename F>
 cudaError_t launch_tokens(const CacheArgs& a, cudaStream_t st, F&& kernel) {
   const bool few = a.tok.tokens <= kSms * kTokFew;

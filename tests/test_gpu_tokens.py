@@ -557,7 +557,7 @@ FORMS = [(256, "mul_ln"), (192, "mul_ln"), (256, "mul"), (192, "mul"), (256, "ad
 
 
 @pytest.mark.parametrize("d_c,gate", FORMS)
-@pytest.mark.parametrize("lens", [(1,), (0, 1, 2, 63, 64, 65, 0), (31, 32, 33, 96, 97, 700), (2000, 1, 130, 5, 640, 64, 64, 1, 300, 77, 0, 11)])
+@pytest.mark.parametrize("lens", [(1,), (0, 0), (0, 1, 2, 63, 64, 65, 0), (31, 32, 33, 96, 97, 700), (2000, 1, 130, 5, 640, 64, 64, 1, 300, 77, 0, 11)])
 def test_decode_equals_the_decode_over_what_it_holds(gpu_lib, d_c, gate, lens):
     for splits in (1, 3, 152):
         case, dc = make(lens, d_c, gate, splits=splits)
@@ -568,7 +568,7 @@ def test_decode_equals_the_decode_over_what_it_holds(gpu_lib, d_c, gate, lens):
         if bitwise(d_c, gate):
             assert torch.equal(got, want), splits
         else:
-            assert apart(got, want) <= 1e-2, splits
+            assert torch.equal(got, want) or apart(got, want) <= 1e-2, splits   # (no token: zeros)
         assert dc.read_status() == 0
     ref_case = dataclasses.replace(case, c_pool=device.bf16_tensor_to_bits(back))
     u = device.output_f64(got)
