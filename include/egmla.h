@@ -526,7 +526,8 @@ int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const fl
  * ablation gates it is the same to the bit; at d_c 256 EG_MLA_GATE_MUL_LN's sums come in
  * another order, and ungated at d_c 256 and 512 the codes themselves are multiplied, with
  * queries and softmax weights in eight significant bits, weights below 2^-13 of the largest
- * in four.)
+ * in four; there tokens of one sequence whose scales are more than 2^100 apart lose weights
+ * of the smaller ones.)
  *
  *   dims         those of eg_mla_decode with d_c a multiple of 16; max_seq_len at most
  *                2^31 - 64

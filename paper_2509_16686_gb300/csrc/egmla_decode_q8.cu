@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::NS; ++s) {
       mbar_init(smem_u32(&bars.full[s]), 1);
-      mbar_init(smem_u32(&bars.empty[s]), 1);
+      // the page's output MMAs (commit) and the query warps, which look at every page
+      mbar_init(smem_u32(&bars.empty[s]), 1 + kQueryWarps);
     }
     mbar_init(smem_u32(&bars.qfull[0]), kQueryWarps);
     // the last score MMA of the segment (commit) and the softmax warps' read of its scales
@@ -382,7 +383,8 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         fence_proxy_async_smem();
         warp_arrive(smem_u32(&bars.qfull[0]));
       }
-      // (every page is waited for, so that no phase of a slot's barrier is taken for another)
+      // (every page is waited for and its slot given back, so that no phase of a slot's
+      // barrier is taken for another)
       const int slot = j % C::NS;
       if (!warp_wait(smem_u32(&bars.full[slot]), (j / C::NS) & 1, abort_flag, wait_ns)) break;
       if (t.ntok < kPage) {
@@ -394,6 +396,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         fence_proxy_async_smem();
         warp_arrive(smem_u32(&bars.zfix));
       }
+      warp_arrive(smem_u32(&bars.empty[slot]));
     }
   } else if (warp < kSoftWarps || warp >= kSoft2Warp0) {
     // ---------------------------------------------------------------- softmax, output read-out

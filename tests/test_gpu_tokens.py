@@ -659,6 +659,29 @@ def test_decode_of_small_and_large_scales_and_every_code(gpu_lib, d_c, gate, pow
     assert dc.read_status() == 0
 
 
+@pytest.mark.parametrize("d_c,gate", FORMS)
+@pytest.mark.parametrize("power", [0, 6])
+def test_decode_with_rows_of_zeros(gpu_lib, d_c, gate, power):
+    """Latents of zero have the least scale, 2^-100, and the weight of any other token.  (Ungated at d_c 256 and 512
+    it passes through 2^(s - 100 - e), e at most 0 for these latents: a normal number of fp32.)"""
+    _, dc = make([200, 64, 130], d_c, gate)
+    if power:   # (scores of ordinary size all the same)
+        dc.q[..., :128] *= 2.0 ** -power
+        dc.c_pool.mul_(2.0 ** power)
+    dc.c_pool.view(-1, d_c)[torch.arange(dc.c_pool.shape[0] * P, device="cuda") % 3 != 1] = 0
+    dc.c_pool[dc.block_table[1, 0].long()] = 0   # a sequence of nothing else
+    cache, back = quantised(dc)
+    assert float(cache.scale.nan_to_num(1.0).min()) == 2.0 ** -100   # (rows of no sequence hold NaN)
+    got = decode_q8(dc, cache)
+    assert bool(got.isfinite().all()) and dc.read_status() == 0
+    if plain(d_c, gate):
+        assert apart(got, reference64(dc, back)) <= 5e-3
+        return
+    dc.c_pool.copy_(back)
+    want = dc.decode(out=torch.full_like(dc.out, 9))
+    assert same(got, want) if bitwise(d_c, gate) else apart(got, want) <= 1e-2
+
+
 @pytest.mark.parametrize("d_c", [256, 512])
 def test_plain_decode_of_many_small_weights(gpu_lib, d_c):
     """One token whose weight is far above the others', of which there are enough to count together: their weights
