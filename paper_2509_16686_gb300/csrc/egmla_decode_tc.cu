@@ -613,7 +613,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // code costs as much as gating and summing it), so nothing of theirs waits at a tile's
       // start: the next tile's codes and gate rows take the place of this tile's, column by
       // column, as soon as these are used (its copies have landed long before), its ids
-      // and scales before that.
+      // and scales before that.  (Not with the additive gate, whose first pass over the tile
+      // leaves its codes in their registers for the second: 8 x 32K 68.6 us, so loaded 132.)
       uint4 g[C::NCH][2];
       float scale = 0.f;
       auto raw_of = [&](int jj) { return smem + C::OFF_RAW + (jj % C::RING) * C::RSLOT + C::PCHUNK + row * D_C + 16 * pp; };
@@ -709,7 +710,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!full_page && !valid) z = make_uint4(0, 0, 0, 0);
               *reinterpret_cast<uint4*>(zpage + unit_off(fc, h)) = z;
             }
-            load_next(fc);
           }
           if (pp == 0) {
             st[row] = 0.f;

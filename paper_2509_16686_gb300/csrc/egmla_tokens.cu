@@ -84,7 +84,7 @@ struct RopeArgs {
   uint8_t *q_out, *k_out;
   int64_t q_stride, q_out_stride, k_stride, k_out_stride;   // bytes between tokens
   int H, dn, dr;
-  int half, q_in_place, k_in_place;
+  int half, q_in_place;
   float magnitude;
   uint64_t turn[kMaxPairs];   // f_i / (2 pi) in 2^-64
 };
@@ -654,7 +654,6 @@ int eg_mla_rope(const eg_mla_dims* dims, const eg_mla_rope_dims* rope, const voi
   a.dr = dims->d_rope;
   a.half = rope->layout == EG_MLA_ROPE_HALF;
   a.q_in_place = q == q_out;
-  a.k_in_place = k == k_out;
   auto* st = static_cast<cudaStream_t>(stream);
   return to_status(dims->dtype == EG_MLA_BF16 ? launch_rope<__nv_bfloat16>(a, st) : launch_rope<float>(a, st));
 }
