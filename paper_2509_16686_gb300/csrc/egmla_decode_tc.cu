@@ -613,8 +613,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       // code costs as much as gating and summing it), so nothing of theirs waits at a tile's
       // start: the next tile's codes and gate rows take the place of this tile's, column by
       // column, as soon as these are used (its copies have landed long before), its ids
-      // and scales before that.  (Not with the additive gate, whose first pass over the tile
-      // leaves its codes in their registers for the second: 8 x 32K 68.6 us, so loaded 132.)
+      // and scales before that.  (Not with the additive gate at d_c 256, which keeps a tile's
+      // values for a second pass and has no registers left: 8 x 32K 53.6 us, so loaded 77.  At
+      // 192 128 ragged sequences took 88.0 us without it and take 84.5.)
+      constexpr bool AHEAD = !GATE_ADD || D_C == 192;
       uint4 g[C::NCH][2];
       float scale = 0.f;
       auto raw_of = [&](int jj) { return smem + C::OFF_RAW + (jj % C::RING) * C::RSLOT + C::PCHUNK + row * D_C + 16 * pp; };
@@ -636,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tr.mark(1, j);
         widen.set(scale);
         const bool more = widen.unfinished();
-        loaded = !GATE_ADD && have1 && warp_test(smem_u32(&bars.full[(j + 1) % C::RING]), ((j + 1) / C::RING) & 1);
+        loaded = AHEAD && have1 && warp_test(smem_u32(&bars.full[(j + 1) % C::RING]), ((j + 1) / C::RING) & 1);
         const uint8_t* raw_next = raw_of(j + 1);
         const __nv_bfloat16* g_next = p.gate_table;
         if (loaded) {
@@ -644,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           scale = scale_of(j + 1);
         }
         auto load_next = [&](int fc) {
-          if (loaded) {
+          if (AHEAD && loaded) {
             ldg_32_na_hint(g_next + fc * 64, pol_keep, g[fc][0], g[fc][1]);
             codes[fc] = *reinterpret_cast<const uint4*>(raw_next + fc * 64);
           }
@@ -674,17 +676,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         constexpr float inv_dc = 1.f / D_C;
         if constexpr (GATE_ADD) {
-          // (as below without the 8 bits: centred before the rounding; the same sums)
+          // (as below without the 8 bits: centred before the rounding; the same sums.  The codes are
+          // widened once and kept for the second pass: 8 x 32K tokens 69.3 us, so 55.8, with the
+          // sums from the bf16 values 53.6)
+          uint4 wide[C::NCH][2];
 #pragma unroll
           for (int fc = 0; fc < C::NCH; ++fc)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint4 c4 = latent(fc, h);
+              wide[fc][h] = c4;
               const uint32_t* cw = reinterpret_cast<const uint32_t*>(&c4);
               const uint32_t* gw2 = reinterpret_cast<const uint32_t*>(&g[fc][h]);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                const float2 zf = __fadd2_rn(unpack_bf16x2(cw[k]), unpack_bf16x2(gw2[k]));
+                const float2 zf = add_bf16x2(cw[k], gw2[k]);
                 s1 = __fadd2_rn(s1, zf);
                 s2 = __ffma2_rn(zf, zf, s2);
               }
@@ -697,19 +703,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int fc = 0; fc < C::NCH; ++fc) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint4 c4 = latent(fc, h);
+              const uint4 c4 = wide[fc][h];
               const uint32_t* cw = reinterpret_cast<const uint32_t*>(&c4);
               const uint32_t* gw2 = reinterpret_cast<const uint32_t*>(&g[fc][h]);
               uint4 z;
               uint32_t* zw = reinterpret_cast<uint32_t*>(&z);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                const float2 zf = __fadd2_rn(__fadd2_rn(unpack_bf16x2(cw[k]), unpack_bf16x2(gw2[k])), make_float2(-mu, -mu));
+                const float2 zf = __fadd2_rn(add_bf16x2(cw[k], gw2[k]), make_float2(-mu, -mu));
                 zw[k] = pack_bf16x2(zf.x, zf.y);
               }
               if (!full_page && !valid) z = make_uint4(0, 0, 0, 0);
               *reinterpret_cast<uint4*>(zpage + unit_off(fc, h)) = z;
             }
+            load_next(fc);
           }
           if (pp == 0) {
             st[row] = 0.f;

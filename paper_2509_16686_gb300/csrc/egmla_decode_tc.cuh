@@ -282,6 +282,18 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<uint32_t*>(&z);
 }
 
+// a + b of a pair in fp32, with a straight from its bf16 values
+__device__ __forceinline__ float2 add_bf16x2(uint32_t a, uint32_t b) {
+  const float2 y = unpack_bf16x2(b);
+  float2 z;
+  asm("{\n\t.reg .b16 lo, hi, one;\n\t"
+      "mov.b16 one, 0x3f80;\n\tmov.b32 {lo, hi}, %2;\n\t"
+      "fma.rn.f32.bf16 %0, lo, one, %3;\n\tfma.rn.f32.bf16 %1, hi, one, %4;\n\t}"
+      : "=f"(z.x), "=f"(z.y)
+      : "r"(a), "f"(y.x), "f"(y.y));
+  return z;
+}
+
 // s += z and q += z^2 of a pair, in fp32 straight from the bf16 values
 __device__ __forceinline__ void sum_bf16x2(uint32_t z, float2& s, float2& q) {
   asm("{\n\t.reg .b16 lo, hi, one;\n\t"
