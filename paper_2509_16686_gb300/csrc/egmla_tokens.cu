@@ -8,8 +8,8 @@
 //
 // All three calls are bound by memory: every row is read once and written once, in 16-byte
 // units with several in flight per lane, by warps that need nothing of one another.
-// Blocks of four warps: with eight, whose slots free up together, 32K tokens' rope took
-// 69.2 us instead of 63.9.
+// Blocks of four warps, or of one where rope has many tokens: a block's slots free up
+// together (32K tokens' rope with eight warps a block 69.2 us, four 63.9, one 63.1).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -182,14 +182,18 @@ struct Deal {
 // kUnroll of them in flight per lane, the first before the token's angles are known.  The
 // angles are taken once per warp and token, a pair per lane, and shared by all heads.
 // 32,768 tokens of 16 heads of 128 + 64 and a key, from projection rows to dense ones (411
-// MB): 63.8 us, 6.4 TB/s, 95 % of the copy rate (with two units in flight 73.9, three 70.0;
-// a pair of bf16 values at a time, as below, 229).
-template <typename T, bool HALF>
-__global__ void __launch_bounds__(kTokThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+// MB): 63.1 us, 6.5 TB/s, 96 % of the copy rate (in blocks of four warps with two units in
+// flight 73.9, three 70.0, four 63.9; a pair of bf16 values at a time, as below, 229).  13 ragged
+// prompts (13,271 tokens) in halves: 28.0 us, with the compiler's choice of 91 registers and
+// blocks of four warps 29.9, blocks of one with 72 registers 28.4 (spills), with 106 29.1.
+template <bool HALF, int WARPS>
+constexpr int kRopeResident = WARPS == 1 ? 24 : HALF ? 5 : 7;   // blocks per SM
+template <typename T, bool HALF, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, kRopeResident<HALF, WARPS>) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int kUnroll = 4;
-  __shared__ __align__(16) float2 table[kTokWarps][kMaxPairs];
+  __shared__ __align__(16) float2 table[WARPS][kMaxPairs];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int k = blockIdx.x * kTokWarps + warp;
+  const int k = blockIdx.x * WARPS + warp;
   grid_dependency_wait();
   if (k >= a.tok.tokens) return;
   constexpr int kBytes = sizeof(T);
@@ -274,11 +278,19 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
   }
 }
 
-// Parts that a token's heads are cut into: as many as give every SM eight warps, and two up
-// to sixteen.  us with one part / with the rule: 1 token 3.1 / 2.5, 64 tokens 3.4 / 2.8,
-// 256 3.4 / 2.9, 1024 4.0 / 3.6, 2048 5.6 / 4.8, 4096 (one part) 10.0; as many as give
-// sixteen: 256 tokens 3.4, 512 3.4 (rule 3.2).
+// Parts that a token's heads are cut into: as many as give every SM eight warps, and two while
+// all of their warps are resident at once.  us with one part / with the rule (blocks of
+// four warps): 1 token 3.1 / 2.5, 64 tokens 3.4 / 2.8, 256 3.4 / 2.9, 1024 4.0 / 3.6, 2048 5.6 /
+// 4.8; as many as give sixteen: 256 tokens 3.4, 512 3.4 (rule 3.1).  One part comes in blocks of one
+// warp: halves of 2048 tokens 5.3 us (two parts, whose last wave is nearly empty, 6.4), 4096
+// 10.7 (11.3); 64 tokens in such blocks 2.9 (2.8), 1024 3.7 (3.6).
 constexpr int kRopeWarps = 8;
+template <typename T, int WARPS>
+cudaError_t launch_rope_units(const RopeArgs& a, int parts, cudaStream_t st) {
+  const dim3 grid((a.tok.tokens + WARPS - 1) / WARPS, parts), block(32 * WARPS);
+  return a.half ? launch_chained(rope_kernel<T, true, WARPS>, grid, block, 0, st, a)
+                : launch_chained(rope_kernel<T, false, WARPS>, grid, block, 0, st, a);
+}
 template <typename T>
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
   auto on = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; };
@@ -286,11 +298,13 @@ cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
   const bool units = a.dn * e % 16 == 0 && a.dr * e % (a.half ? 32 : 16) == 0 && on(a.q, a.q_stride) &&
                      on(a.q_out, a.q_out_stride) && on(a.k, a.k_stride) && on(a.k_out, a.k_out_stride);
   int want = (kSms * kRopeWarps - 1) / a.tok.tokens + 1;
-  if (want < 2 && a.tok.tokens <= 2 * kSms * kRopeWarps) want = 2;
-  const dim3 grid((a.tok.tokens + kTokWarps - 1) / kTokWarps, want < a.H + 1 ? want : a.H + 1), block(kTokThreads);
-  if (!units) return launch_chained(rope_any_kernel<T>, grid, block, 0, st, a);
-  return a.half ? launch_chained(rope_kernel<T, true>, grid, block, 0, st, a)
-                : launch_chained(rope_kernel<T, false>, grid, block, 0, st, a);
+  const int resident = kSms * kTokWarps * (a.half ? kRopeResident<true, kTokWarps> : kRopeResident<false, kTokWarps>);
+  if (want < 2 && a.tok.tokens <= resident / 2) want = 2;
+  const int parts = want < a.H + 1 ? want : a.H + 1;
+  if (!units)
+    return launch_chained(rope_any_kernel<T>, dim3((a.tok.tokens + kTokWarps - 1) / kTokWarps, parts), dim3(kTokThreads), 0,
+                          st, a);
+  return parts == 1 ? launch_rope_units<T, 1>(a, parts, st) : launch_rope_units<T, kTokWarps>(a, parts, st);
 }
 
 // ------------------------------------------------------------------ the cache in 8 bits

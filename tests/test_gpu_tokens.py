@@ -152,6 +152,31 @@ def test_rope_of_one_token_per_sequence(gpu_lib, dtype, T):
     check_rope(ko[:, None], k[:, None], pos, 64, dtype, {})
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kw", [dict(), dict(layout="half"), dict(layout="half", scaling="linear", factor=2.0, inverse=True)])
+@pytest.mark.parametrize("shape", [(2, 16, 64), (3, 0, 256), (1, 128, 32), (2, 8, 16)])
+@pytest.mark.parametrize("T", [1216, 1217, 1520, 1521, 2128, 2129, 2433, 6001])
+def test_rope_of_many_tokens(gpu_lib, dtype, kw, shape, T):
+    """Where a token's heads come in one part and in several; ragged, with rows behind the last sequence."""
+    H, dn, dr = shape
+    lens = [T // 2, 0, 1, T - T // 2 - 1 - 5]
+    firsts = [5, 0, 1 << 20, 77]
+    dims = _lib.make_dims(H, dn, dr, 128, 256, 100, dtype=dtype)
+    q, k, st = normal((T, H, dn + dr), dtype, T), normal((T, dr), dtype, T + 1), status_word()
+    qo, ko = torch.full_like(q, 77), torch.full_like(k, 77)
+    args = ints(firsts), ints(offsets(lens)), st
+    _lib.eg_mla_rope(dims, _lib.make_rope(**kw), q, qo, k, ko, *args)
+    n, pos = T - 5, positions_of(lens, firsts)
+    check_rope(qo[:n], q[:n], pos, dr, dtype, kw)
+    check_rope(ko[:n, None], k[:n, None], pos, dr, dtype, kw)
+    assert bool((qo[n:] == 77).all()) and bool((ko[n:] == 77).all())
+    q2, k2 = q.clone(), k.clone()
+    _lib.eg_mla_rope(dims, _lib.make_rope(**kw), q2, q2, None, None, *args)
+    _lib.eg_mla_rope(dims, _lib.make_rope(**kw), None, None, k2, k2, *args)
+    assert torch.equal(q2[:n], qo[:n]) and torch.equal(k2[:n], ko[:n])
+    assert torch.equal(q2[n:], q[n:]) and torch.equal(k2[n:], k[n:]) and int(st) == 0
+
+
 def test_rope_at_the_farthest_positions(gpu_lib):
     """Positions up to 2^31 - 1, and past it with a sequence's own offset."""
     dims = _lib.make_dims(2, 0, 64, 128, 256, 100, dtype="fp32")
