@@ -458,7 +458,10 @@ typedef struct {
  * Angles are reduced as 64-bit fractions of a turn, which keeps them to 2^-32 of a turn
  * at any position; sums are fp32, rounded once.  16-byte alignment of rows, heads and
  * pointers is not needed but faster.  Device errors: EG_MLA_ERR_OUT_OF_RANGE for
- * cu_seqlens that begin above 0 or decrease (rows that belong to no sequence are left).
+ * cu_seqlens that do not begin at 0 or that decrease.  Rows that belong to no sequence by them
+ * are left as they were, and so are those of a sequence whose two offsets are not in order
+ * with each other and with the ones before and behind (one wrong offset that makes the list
+ * decrease takes no row to a wrong place; which others are left is not specified).
  */
 int eg_mla_rope(const eg_mla_dims* dims, const eg_mla_rope_dims* rope, const void* q, int64_t q_stride, void* q_out,
                 int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride,

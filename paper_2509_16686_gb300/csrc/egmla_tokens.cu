@@ -4,7 +4,9 @@
 //
 // Packed token k belongs to the sequence b with cu[b] <= k < cu[b + 1], as its token
 // k - cu[b], at position positions[b] + k - cu[b] (cu null: to sequence k, at
-// positions[k]).  A warp finds b for its token by ballots over 32 offsets at a time.
+// positions[k]).  A warp finds b for its token by ballots over 32 offsets at a time, which
+// see some of the offsets only: those around b are looked at again, and all offsets once
+// per call, so that a list that is not in order is reported and misplaces no token.
 //
 // All three calls are bound by memory: every row is read once and written once, in 16-byte
 // units with several in flight per lane, by warps that need nothing of one another.
@@ -51,6 +53,27 @@ __device__ __forceinline__ int sequence_of(const Packed& p, int k, int lane) {
   return b;
 }
 
+// First token of sequence b if token k is surely its: cu[b] <= k < cu[b + 1], and both in order
+// with the offsets before and behind them (before the first 0).  A single offset that makes
+// the list decrease is then none of b's two, and b is the sequence that the others say.
+// -1: of no sequence, or in doubt.
+__device__ __forceinline__ int first_of(const Packed& p, int b, int k) {
+  const int before = b > 0 ? __ldg(p.cu + b - 1) : 0, first = __ldg(p.cu + b), end = __ldg(p.cu + b + 1);
+  const int behind = b + 2 <= p.batch ? __ldg(p.cu + b + 2) : INT32_MAX;
+  return before <= first && first <= k && k < end && end <= behind ? first : -1;
+}
+
+// Reports offsets that do not begin at 0 or that decrease; warp `w` of `warps` looks at its
+// part of them.  (Where the warp goes on to look for its tokens' sequences, it has brought
+// the lines that this needs.)
+__device__ __forceinline__ void check_offsets(const Packed& p, int w, int warps, int lane) {
+  if (p.cu == nullptr) return;
+  bool wrong = w == 0 && __ldg(p.cu) != 0;
+  for (int64_t i = static_cast<int64_t>(w) * 32 + lane; i < p.batch; i += static_cast<int64_t>(warps) * 32)
+    wrong = wrong || __ldg(p.cu + i) > __ldg(p.cu + i + 1);
+  if (wrong) report_status(p.status, kStatusOutOfRange);
+}
+
 // Position of packed token k, the same in every lane; false for a token of no sequence or of
 // one with a negative position.
 __device__ __forceinline__ bool find_position(const Packed& p, int k, int lane, int64_t& pos) {
@@ -58,11 +81,8 @@ __device__ __forceinline__ bool find_position(const Packed& p, int k, int lane, 
   if (p.cu != nullptr) {
     b = sequence_of(p, k, lane);
     if (b >= p.batch) return false;   // a row behind the last sequence
-    first = __ldg(p.cu + b);
-    if (first > k) {   // (no token of offsets that begin above 0 or decrease)
-      if (lane == 0) report_status(p.status, kStatusOutOfRange);
-      return false;
-    }
+    first = first_of(p, b, k);
+    if (first < 0) return false;
   }
   const int start = p.positions != nullptr ? __ldg(p.positions + b) : 0;
   if (start < 0) return false;
@@ -216,6 +236,7 @@ __global__ void __launch_bounds__(32 * WARPS, kRopeResident<HALF, WARPS>) rope_k
     for (int j = 0; j < kUnroll; ++j, d.next())
       if (d.h < hend) item[j].load(d.h < a.H ? q + d.h * stride + nope : key, d.r, items);
   }
+  if (part == 0) check_offsets(a.tok, k, a.tok.tokens, lane);
   int64_t pos;
   if (!find_position(a.tok, k, lane, pos)) return;
   if (nope > 0 && !a.q_in_place && a.q != nullptr) {
@@ -254,8 +275,10 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = blockIdx.x * kTokWarps + warp;
   grid_dependency_wait();
+  if (k >= a.tok.tokens) return;
+  if (blockIdx.y == 0) check_offsets(a.tok, k, a.tok.tokens, lane);
   int64_t pos;
-  if (k >= a.tok.tokens || !find_position(a.tok, k, lane, pos)) return;
+  if (!find_position(a.tok, k, lane, pos)) return;
   const int pairs = a.dr / 2, heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
   float2* cs = table[warp];
   for (int i = lane; i < pairs; i += 32) cs[i] = turn_cos_sin(static_cast<uint64_t>(pos) * a.turn[i], a.magnitude);
@@ -325,17 +348,25 @@ struct CacheArgs {
 // Rows of the pool of the packed tokens k0 .. k0 + T - 1: lane i < T gets token i's, -1 for none.
 template <int T>
 __device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) {
-  int b = k0 + lane;
+  int b = k0 + lane, first = b;
   if (a.tok.cu != nullptr && a.tok.batch <= 32) {
     // every offset in a lane: the tokens' sequences by a ballot each
-    const int end = lane < a.tok.batch ? __ldg(a.tok.cu + lane + 1) : INT32_MAX;
+    const bool held = lane < a.tok.batch;
+    const int own = held ? __ldg(a.tok.cu + lane) : 0, end = held ? __ldg(a.tok.cu + lane + 1) : INT32_MAX;
 #pragma unroll
     for (int i = 0; i < T; ++i) {
-      const int n = __popc(__ballot_sync(0xffffffffu, end <= k0 + i && lane < a.tok.batch));
+      const int n = __popc(__ballot_sync(0xffffffffu, end <= k0 + i && held));
       if (lane == i) b = n;
     }
+    // (as first_of and check_offsets)
+    const int at = min(b, 31), begin = __shfl_sync(0xffffffffu, own, at), last = __shfl_sync(0xffffffffu, end, at);
+    const uint32_t falls = __ballot_sync(0xffffffffu, held && own > end);   // bit i: from offset i to i + 1
+    if (falls != 0 || (lane == 0 && own != 0)) report_status(a.tok.status, kStatusOutOfRange);
+    const bool doubt = (falls | falls << 1 | falls >> 1) >> at & 1;
+    first = !doubt && begin <= k0 + lane && k0 + lane < last ? begin : -1;   // (below 0 too: of no sequence)
   } else if (a.tok.cu != nullptr) {
     // a search for the first token, and for another only where its sequence ends before it
+    check_offsets(a.tok, k0 / T, (a.tok.tokens + T - 1) / T, lane);
     int found = 0, end = INT32_MIN;
 #pragma unroll
     for (int i = 0; i < T; ++i) {
@@ -348,12 +379,9 @@ __device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) 
   }
   int64_t pos = -1;
   if (lane < T && k0 + lane < a.tok.tokens && b < a.tok.batch) {
-    const int first = a.tok.cu != nullptr ? __ldg(a.tok.cu + b) : b;
     const int start = a.tok.positions != nullptr ? __ldg(a.tok.positions + b) : 0;
-    if (first > k0 + lane)
-      report_status(a.tok.status, kStatusOutOfRange);
-    else if (start >= 0)
-      pos = static_cast<int64_t>(start) + k0 + lane - first;
+    if (a.tok.cu != nullptr && a.tok.batch > 32) first = first_of(a.tok, b, k0 + lane);
+    if (first >= 0 && start >= 0) pos = static_cast<int64_t>(start) + k0 + lane - first;
   }
   if (pos < 0) return -1;
   const int64_t lp = pos / kPage;
