@@ -9,7 +9,9 @@
 //             q^ is bf16, whose eight significant bits two codes of four hold exactly as
 //             far as 2^-18 of the head's largest entry).  One product of N = 32 columns
 //             (16 heads x 2 parts), summed by the softmax warps:
-//               s_j = scale (2^e_j 2^k (S1 + S2 / 16) + q^R . k^R_j),  2^e_j token j's scale
+//               s_j = scale (2^e_j 2^k (S1 + S2 / 16) + q^R . k^R_j),  2^e_j token j's scale,
+//             with a 2^k below 1 before 2^e_j (up to 2^119, the sums up to 2^27) and one above
+//             behind it, so that no product is infinite where the score is not
 //   weights   P'_j = 2^(s'_j - m + 4), s'_j = s_j log2(e) + e_j: the token's scale goes into
 //             its weight, whose reference m is the largest s'.  P' = p1 + p2 / 16 +
 //             p3 / 2^16: eight significant bits of large weights, four of small ones down
@@ -62,7 +64,8 @@ struct PlainCfg {
   static constexpr uint32_t SLOT = KR_OFF + PCHUNK;
   static constexpr uint32_t META = kPage * 4;           // the page's scales
   // query block: codes [n = 16 part + head][feature] in 8 x 16-byte core matrices, 16
-  // features a K core of 512 bytes; q^R as the absorption wrote it; scale_log2 2^k per head
+  // features a K core of 512 bytes; q^R as the absorption wrote it; per head 2^min(k, 0) and
+  // scale_log2 2^max(k, 0)
   static constexpr uint32_t QCORE = kQParts * kHeads * 16;
   static constexpr uint32_t Q_ROPE = D_C / 16 * QCORE;
   static constexpr uint32_t Q_SCALE = Q_ROPE + qprep_rope_bytes(kRope);
@@ -379,7 +382,11 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
                 make_uint4(part[n][0], part[n][1], part[n][2], part[n][3]);
         }
         reinterpret_cast<uint4*>(qb + C::Q_ROPE)[tid] = rope;
-        if (l16 == 0) reinterpret_cast<float*>(qb + C::Q_SCALE)[h] = p.scale_log2 * scale;
+        if (l16 == 0) {
+          float* hs = reinterpret_cast<float*>(qb + C::Q_SCALE);
+          hs[h] = fminf(scale, 1.f);   // (a NaN is in the codes)
+          hs[kHeads + h] = p.scale_log2 * fmaxf(scale, 1.f);
+        }
         fence_proxy_async_smem();
         warp_arrive(smem_u32(&bars.qfull[0]));
       }
@@ -411,12 +418,13 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
     const float scale = p.scale_log2;
     float* xmax = reinterpret_cast<float*>(smem + C::OFF_XCH) + g * 64;   // [4 warps][8 heads]
     float* xsum = xmax + kSoftWarps * kGroupHeads;                        // [4 warps][8 heads]
-    float m_ref[2], l_acc[2], qs[2];
+    float m_ref[2], l_acc[2], qlow[2], qs[2];
     float m8 = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       m_ref[k] = -INFINITY;
       l_acc[k] = 0.f;
+      qlow[k] = 0.f;
       qs[k] = 0.f;
     }
     Walker<kPage> w;
@@ -431,8 +439,11 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         ok = warp_wait(smem_u32(&bars.qfull[0]), seg & 1, abort_flag, wait_ns);
         if (ok) {
           const float* hs = reinterpret_cast<const float*>(smem + C::OFF_QBUF + C::Q_SCALE) + kGroupHeads * g + 2 * q;
-          qs[0] = hs[0];
-          qs[1] = hs[1];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            qlow[k] = hs[k];
+            qs[k] = hs[kHeads + k];
+          }
           warp_arrive(smem_u32(&bars.qempty[0]));
         }
       }
@@ -464,7 +475,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int i = 2 * e + k;
-            const float lat = fmaf(v2[i], kPart2, v1[i]) * ts[e];
+            const float lat = fmaf(v2[i], kPart2, v1[i]) * qlow[k] * ts[e];
             const float x = fmaf(lat, qs[k], fmaf(vr[i], scale, lift));
             s[e][k] = valid ? x : -INFINITY;
             exceed = exceed || (x > m_ref[k] + kPlainLazy && valid);
