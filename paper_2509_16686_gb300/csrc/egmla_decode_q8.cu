@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 #pragma unroll
         for (int o = 1; o < LANES; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
         float scale, inverse;
-        q8_scale(most, scale, inverse);
+        q8_scale(most, scale, inverse, -126);   // (queries of 2^-118 and less lose bits; their scores need latents of 2^110)
         // the block is free once the segment before has read it
         if (!warp_wait(smem_u32(&bars.qempty[0]), (seg & 1) ^ 1, abort_flag, wait_ns)) break;
 #pragma unroll

@@ -20,11 +20,12 @@ namespace egmla {
 // shapes of the calls on the cache in 8 bits; EG_MLA_OK or the error code
 int q8_check_dims(const eg_mla_dims* d);
 
-// scale and 1 / scale for a row whose largest magnitude has the fp32 bits `most`
-__device__ __forceinline__ void q8_scale(uint32_t most, float& scale, float& inverse) {
+// scale and 1 / scale for a row whose largest magnitude has the fp32 bits `most`; least: of
+// the scale's exponent, at least -126 (both are normal numbers)
+__device__ __forceinline__ void q8_scale(uint32_t most, float& scale, float& inverse, int least = -100) {
   // 448 = 1.75 2^8; (a subnormal `most` counts as 2^-127 and is far below the least scale)
   int e = static_cast<int>(most >> 23) - 127 - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);
-  e = min(max(e, -100), 119);
+  e = min(max(e, least), 119);
   scale = __int_as_float((e + 127) << 23);
   inverse = __int_as_float((127 - e) << 23);
   if (most >= 0x7f800000u) scale = inverse = __int_as_float(0x7fffffff);
