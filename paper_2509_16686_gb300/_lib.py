@@ -306,15 +306,24 @@ def _packed(tokens: int, positions, cu_seqlens, dev: int) -> tuple:
 
 
 def _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev: int) -> tuple:
-    """Pointers of a cache in 8 bits."""
+    """Pages of a cache in 8 bits, and its pointers."""
     pages, size = c8_pool.shape[0], dims.page_size
     codes = c8_pool.dtype
     if codes not in _CODES:
         _refuse(c8_pool, (pages, size, dims.d_c), _CODES, dev, "c8_pool")
-    return (_arg(c8_pool, (pages, size, dims.d_c), codes, dev, "c8_pool"),
-            _arg(scale_pool, (pages, size), torch.float32, dev, "scale_pool"),
-            _arg(krope_pool, (pages, size, dims.d_rope), dtype, dev, "krope_pool"),
-            None if id_pool is None else _arg(id_pool, (pages, size), torch.int32, dev, "id_pool"))
+    return pages, (_arg(c8_pool, (pages, size, dims.d_c), codes, dev, "c8_pool"),
+                   _arg(scale_pool, (pages, size), torch.float32, dev, "scale_pool"),
+                   _arg(krope_pool, (pages, size, dims.d_rope), dtype, dev, "krope_pool"),
+                   None if id_pool is None else _arg(id_pool, (pages, size), torch.int32, dev, "id_pool"))
+
+
+def _status(t: Optional[torch.Tensor], dev: int) -> Optional[int]:
+    """Pointer of a status word."""
+    if t is None:
+        return None
+    if t.dtype is torch.int32 and t.get_device() == dev and t.numel() > 0:
+        return t.data_ptr()
+    _refuse(t, t.shape if t.numel() > 0 else (1,), (torch.int32,), dev, "dev_status")
 
 
 def _stream_on(dev: int, stream) -> int:
@@ -510,7 +519,7 @@ def eg_mla_rope(dims: EgMlaDims, rope: EgMlaRopeDims, q, q_out, k, k_out, positi
             *(none if k is None else _rows(k, keys, dtype, dev, "k")),
             *(none if k is None else _rows(k_out, keys, dtype, dev, "k_out")))
     cu, pos, batch = _packed(tokens, positions, cu_seqlens, dev)
-    _check(load().eg_mla_rope(ctypes.byref(dims), ctypes.byref(rope), *rows, cu, pos, batch, tokens, _ptr(dev_status),
+    _check(load().eg_mla_rope(ctypes.byref(dims), ctypes.byref(rope), *rows, cu, pos, batch, tokens, _status(dev_status, dev),
                               _stream_on(dev, stream)), "eg_mla_rope")
 
 
@@ -519,7 +528,7 @@ def eg_mla_append_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id
     """New tokens into a cache that holds the latent in 8 bits (c8_pool e4m3 or its bytes), a token per sequence
     or packed by cu_seqlens; the rows of c_new and krope_new may be apart: see include/egmla.h."""
     tokens, dtype, dev = c_new.shape[0], _MODEL_DTYPES.get(dims.dtype), c8_pool.get_device()
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
+    pages, cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
     rows = (*_rows(c_new, (tokens, dims.d_c), dtype, dev, "c_new"),
             *_rows(krope_new, (tokens, dims.d_rope), dtype, dev, "krope_new"))
     ids = None if ids_new is None else _arg(ids_new, (tokens,), torch.int32, dev, "ids_new")
@@ -527,7 +536,7 @@ def eg_mla_append_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id
     width = block_table.shape[1]
     table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
     _check(load().eg_mla_append_latent_q8(ctypes.byref(dims), *cache, *rows, ids, cu, pos, table, width, batch, tokens,
-                                          c8_pool.shape[0], _ptr(dev_status), _stream_on(dev, stream)),
+                                          pages, _status(dev_status, dev), _stream_on(dev, stream)),
            "eg_mla_append_latent_q8")
 
 
@@ -535,7 +544,7 @@ def eg_mla_read_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_p
                           ids_out, positions=None, cu_seqlens=None, dev_status=None, stream=None) -> None:
     """Cached tokens of a cache in 8 bits as packed rows (krope_out and ids_out may be None): see include/egmla.h."""
     tokens, dtype, dev = c_out.shape[0], _MODEL_DTYPES.get(dims.dtype), c8_pool.get_device()
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
+    pages, cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
     rows = (*_rows(c_out, (tokens, dims.d_c), dtype, dev, "c_out"),
             *((None, 0) if krope_out is None else _rows(krope_out, (tokens, dims.d_rope), dtype, dev, "krope_out")))
     ids = None if ids_out is None else _arg(ids_out, (tokens,), torch.int32, dev, "ids_out")
@@ -543,23 +552,34 @@ def eg_mla_read_latent_q8(dims: EgMlaDims, c8_pool, scale_pool, krope_pool, id_p
     width = block_table.shape[1]
     table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
     _check(load().eg_mla_read_latent_q8(ctypes.byref(dims), *cache, cu, pos, table, width, *rows, ids, batch, tokens,
-                                        c8_pool.shape[0], _ptr(dev_status), _stream_on(dev, stream)),
+                                        pages, _status(dev_status, dev), _stream_on(dev, stream)),
            "eg_mla_read_latent_q8")
 
 
 def eg_mla_decode_q8(dims: EgMlaDims, q, c8_pool, scale_pool, krope_pool, id_pool, block_table, seq_lens, max_seq_len,
                      gate_table, ln_gamma, ln_beta, w_uk, w_uv, out, workspace, num_splits=0, dev_status=None,
                      stream=None) -> None:
-    """eg_mla_decode over a cache in 8 bits: see include/egmla.h."""
-    dev, batch, width = c8_pool.get_device(), seq_lens.shape[0], block_table.shape[1]
-    cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, _MODEL_DTYPES.get(dims.dtype), dev)
+    """eg_mla_decode over a cache in 8 bits: see include/egmla.h.  (Without a gate gate_table, ln_gamma and ln_beta are
+    not looked at, and the latter two only with a LayerNorm.)"""
+    dev, batch, width, dtype = c8_pool.get_device(), seq_lens.shape[0], block_table.shape[1], _MODEL_DTYPES.get(dims.dtype)
+    pages, cache = _cache_q8(dims, c8_pool, scale_pool, krope_pool, id_pool, dtype, dev)
     table = _arg(block_table, (batch, width), torch.int32, dev, "block_table")
     lens = _arg(seq_lens, (batch,), torch.int32, dev, "seq_lens")
     handle = _stream_on(dev, stream)
+    heads, d_nope, d_v, d_c, mode = dims.num_heads, dims.d_nope, dims.d_v, dims.d_c, dims.gate_mode
+    gate = gamma = beta = None
+    if mode != EG_MLA_GATE_NONE:
+        gate = None if gate_table is None else _arg(gate_table, (dims.vocab, d_c), dtype, dev, "gate_table")
+        if mode != EG_MLA_GATE_MUL:
+            gamma = None if ln_gamma is None else _arg(ln_gamma, (d_c,), torch.float32, dev, "ln_gamma")
+            beta = None if ln_beta is None else _arg(ln_beta, (d_c,), torch.float32, dev, "ln_beta")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(workspace, workspace.shape, (workspace.dtype,), dev, "workspace")
     _check(load().eg_mla_decode_q8(
-        ctypes.byref(dims), _ptr(q), *cache, table, width, lens, int(max_seq_len), batch, c8_pool.shape[0],
-        _ptr(gate_table), _ptr(ln_gamma), _ptr(ln_beta), _ptr(w_uk), _ptr(w_uv), _ptr(out), num_splits, _ptr(workspace),
-        workspace.nbytes, _ptr(dev_status), handle), "eg_mla_decode_q8")
+        ctypes.byref(dims), _arg(q, (batch, heads, d_nope + dims.d_rope), dtype, dev, "q"), *cache, table, width, lens,
+        int(max_seq_len), batch, pages, gate, gamma, beta, _arg(w_uk, (heads, d_nope, d_c), dtype, dev, "w_uk"),
+        _arg(w_uv, (heads, d_v, d_c), dtype, dev, "w_uv"), _arg(out, (batch, heads, d_v), dtype, dev, "out"), num_splits,
+        workspace.data_ptr(), workspace.nbytes, _status(dev_status, dev), handle), "eg_mla_decode_q8")
 
 
 def make_layer_dims(n_embd: int, rope_theta: float = 10000.0, rms_eps: float = 0.0,
