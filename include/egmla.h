@@ -527,10 +527,11 @@ int eg_mla_read_latent_q8(const eg_mla_dims* dims, const void* c8_pool, const fl
  * scale_j x code_j.  The result is eg_mla_decode's over a cache of the values that
  * eg_mla_read_latent_q8 gives, within the same bounds.  (In fp32, at d_c 192 and with the
  * ablation gates it is the same to the bit; at d_c 256 EG_MLA_GATE_MUL_LN's sums come in
- * another order, and ungated at d_c 256 and 512 the codes themselves are multiplied, with
- * queries and softmax weights in eight significant bits, weights below 2^-13 of the largest
- * in four; there tokens of one sequence whose scales are more than 2^100 apart lose weights
- * of the smaller ones.)
+ * another order, and ungated at d_c 256 and 512 the codes themselves are multiplied.  There
+ * queries have eight significant bits down to 2^-13 of a head's largest entry after W_UK, and
+ * 2^-22 of it below; a token's softmax weight times its scale has nine bits down to 2^-25 of
+ * the largest such product, fewer below and none under 2^-34; and tokens of one sequence
+ * whose scales are more than 2^100 apart lose weights of the smaller ones.)
  *
  *   dims         those of eg_mla_decode with d_c a multiple of 16; max_seq_len at most
  *                2^31 - 64

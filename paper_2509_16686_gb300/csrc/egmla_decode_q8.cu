@@ -6,19 +6,22 @@
 // latents fill half the shared memory they would as bf16, and a tile is a whole page also
 // at width 512.  What meets them is in 8 bits too, split so that it keeps its precision:
 //   queries   q^ 2^-k = q1 + q2 / 16 (k per head, the largest magnitude between 224 and 448;
-//             q^ is bf16, whose eight significant bits two codes of four hold exactly as
-//             far as 2^-18 of the head's largest entry).  One product of N = 32 columns
+//             q^ is bf16, whose eight significant bits two codes of four hold exactly down
+//             to 2^-13 of the head's largest entry, and to 2^-22 of that below).  One product of N = 32 columns
 //             (16 heads x 2 parts), summed by the softmax warps:
 //               s_j = scale (2^e_j 2^k (S1 + S2 / 16) + q^R . k^R_j),  2^e_j token j's scale,
 //             with a 2^k below 1 before 2^e_j (up to 2^119, the sums up to 2^27) and one above
 //             behind it, so that no product is infinite where the score is not
-//   weights   P'_j = 2^(s'_j - m + 4), s'_j = s_j log2(e) + e_j: the token's scale goes into
-//             its weight, whose reference m is the largest s'.  P' = p1 + p2 / 16 +
-//             p3 / 2^16: eight significant bits of large weights, four of small ones down
-//             to 2^-34 of the largest (without p3 to 2^-18: 32K tokens of just less each
-//             would be lost, an eighth of the whole).  N = 48 columns, added when the
-//             output is read:  O^T += Z^T P'
-//   l = sum_j P'_j 2^-e_j with the rounded P', so that the rounding cancels in O / l.
+//   weights   P'_j = 2^(s'_j - m + 11), s'_j = s_j log2(e) + e_j: the token's scale goes into
+//             its weight, whose reference m is the largest s'.  P' = p1 + p2 / 8 + p3 / 64 in
+//             e5m2, whose three significant bits reach far down: to half a step of nine bits
+//             (2^-9, bf16's) for weights down to 2^-25 of the largest, four bits at 2^-30,
+//             nothing below 2^-34.  (In e4m3 with p2 / 16 and p3 / 2^16 it was eight bits of
+//             large weights and four of small ones: a head whose largest weight falls on
+//             values that W_UV takes to zero was off by 2.5 %.)  N = 48 columns, added when
+//             the output is read:  O^T += Z^T P'
+//   l = sum_j P'_j 2^-e_j with the rounded P', so that the rounding cancels in O / l (with P'
+//             itself below 2^-25 of the largest).
 // The RoPE part stays bf16 (kind::f16) in columns of its own.
 //
 // 128 ragged sequences of 128 to 16K tokens (337 MB) at d_c 512: 76 us a call, 62.8 of them
@@ -51,10 +54,11 @@ constexpr int kGroupHeads = 8;                       // heads of a softmax group
 constexpr int kSoft2Warp0 = 8;                       // warps 8-11: the second group (a warp reads the TMEM lanes of warp % 4)
 constexpr int kQueryWarp0 = 12, kQueryWarps = 4;
 constexpr int kQParts = 2, kPParts = 3;
-constexpr float kPart2 = 1.f / 16, kPart3 = 1.f / 65536;
-// weights of at most 2^(4 + 4) = 256: below e4m3's 448, and as far above its smallest
-// numbers as that allows
-constexpr float kWeightLog2 = 4.f, kPlainLazy = 4.f;
+constexpr float kQPart2 = 1.f / 16, kPPart2 = 1.f / 8, kPPart3 = 1.f / 64;
+// weights of at most 2^(11 + 4): below e5m2's 57344, and as far above its smallest numbers
+// as that allows; what a partial result holds is 2^-11 of its sums over them (l with 2^100
+// for latents of zero would come near fp32's end)
+constexpr float kWeightLog2 = 11.f, kPlainLazy = 4.f, kWeightUnit = 1.f / 2048;
 
 template <int D_C>
 struct PlainCfg {
@@ -100,11 +104,11 @@ struct PlainBars : Bars {
 };
 static_assert(sizeof(PlainBars) <= 512, "barriers");
 
-// kind::f8f6f4 with e4m3 A and B, fp32 D
-__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, int a_mn, int b_mn) {
-  return idesc_bf16(M, N, a_mn, b_mn) & ~((7u << 7) | (7u << 10));
+// kind::f8f6f4 with e4m3 A, e4m3 or e5m2 B, fp32 D
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, int a_mn, int b_mn, bool b_e5m2) {
+  return (idesc_bf16(M, N, a_mn, b_mn) & ~((7u << 7) | (7u << 10))) | (b_e5m2 ? 1u << 10 : 0u);
 }
-__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                             uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -133,8 +137,12 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
 }
 
 // two codes as fp32 values
-__device__ __forceinline__ float2 decode2(uint32_t c) {
-  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(c), __NV_E4M3)));
+__device__ __forceinline__ float2 decode2(uint32_t c, __nv_fp8_interpretation_t type) {
+  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(c), type)));
+}
+// two values as e5m2 codes, the first in the low byte
+__device__ __forceinline__ uint32_t encode2_e5m2(float lo, float hi) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E5M2);
 }
 
 template <int D_C>
@@ -239,7 +247,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- score MMAs
     if (elect_one()) {
-      constexpr uint32_t IDESC_S = idesc_e4m3(64, kQParts * kHeads, 0, 0), IDESC_R = idesc_bf16(64, kHeads, 0, 0);
+      constexpr uint32_t IDESC_S = idesc_f8(64, kQParts * kHeads, 0, 0, false), IDESC_R = idesc_bf16(64, kHeads, 0, 0);
       const uint64_t zdesc = smem_desc(sbase, 16, 1024, kSwizzle128B);
       const uint64_t qdesc = smem_desc(sbase + C::OFF_QBUF, C::QCORE, 128, kSwizzleNone);
       const uint64_t rdesc = smem_desc(sbase + C::OFF_QBUF + C::Q_ROPE, kQGroupBytes, kQRowGroupBytes, kSwizzleNone);
@@ -264,7 +272,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         const uint32_t ds = tmem + C::COL_S + sb * C::S_COLS;
 #pragma unroll
         for (int kk = 0; kk < D_C / 32; ++kk)
-          mma_e4m3_ss(ds, za + (((kk >> 2) * C::PCHUNK + (kk & 3) * 32) >> 4), qdesc + ((kk * 2 * C::QCORE) >> 4), IDESC_S,
+          mma_f8_ss(ds, za + (((kk >> 2) * C::PCHUNK + (kk & 3) * 32) >> 4), qdesc + ((kk * 2 * C::QCORE) >> 4), IDESC_S,
                       kk > 0);
 #pragma unroll
         for (int kk = 0; kk < kRope / 16; ++kk)
@@ -286,7 +294,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
     // A: the page's codes read MN-major (128 features of a column along M, eight tokens
     // 1 KB apart along K); B: P' MN-major.
     if (elect_one()) {
-      constexpr uint32_t IDESC_O = idesc_e4m3(128, kPParts * kHeads, 1, 1);
+      constexpr uint32_t IDESC_O = idesc_f8(128, kPParts * kHeads, 1, 1, true);
       const uint64_t zdesc = smem_desc(sbase, C::PCHUNK, 1024, kSwizzle128B);
       const uint64_t pdesc = smem_desc(sbase + C::OFF_PBUF, C::PGROUP, 128, kSwizzleNone);
       Walker<kPage> w;
@@ -303,7 +311,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         for (int ks = 0; ks < kPage / 32; ++ks)
 #pragma unroll
           for (int mc = 0; mc < C::NMC; ++mc)
-            mma_e4m3_ss(tmem + C::COL_O + C::O_COLS * mc, za + ((mc * C::PCHUNK + ks * 4096) >> 4),
+            mma_f8_ss(tmem + C::COL_O + C::O_COLS * mc, za + ((mc * C::PCHUNK + ks * 4096) >> 4),
                         pb + ((ks * 4 * C::PGROUP) >> 4), IDESC_O, ks > 0 ? 1u : keep);
         mma_commit(smem_u32(&bars.empty[slot]));
         mma_commit(smem_u32(&bars.pfree[jo % kNP]));
@@ -366,7 +374,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
             const float2 x = unpack_bf16x2(v);
             const float x0 = x.x * inverse, x1 = x.y * inverse;
             const uint32_t c1 = q8_encode2(x0, x1);
-            const float2 d = decode2(c1);
+            const float2 d = decode2(c1, __NV_E4M3);
             const uint32_t c2 = q8_encode2((x0 - d.x) * 16.f, (x1 - d.y) * 16.f);
             if (k % 2 == 0) {
               part[0][k / 2] = c1;
@@ -475,7 +483,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int i = 2 * e + k;
-            const float lat = fmaf(v2[i], kPart2, v1[i]) * qlow[k] * ts[e];
+            const float lat = fmaf(v2[i], kQPart2, v1[i]) * qlow[k] * ts[e];
             const float x = fmaf(lat, qs[k], fmaf(vr[i], scale, lift));
             s[e][k] = valid ? x : -INFINITY;
             exceed = exceed || (x > m_ref[k] + kPlainLazy && valid);
@@ -544,16 +552,21 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
           const float lower = ts[e] != ts[e] ? ts[e] : __uint_as_float((254u << 23) - __float_as_uint(ts[e]));
           const float p0 = ex2_approx(s[e][0] - (m_ref[0] - kWeightLog2));
           const float p1 = ex2_approx(s[e][1] - (m_ref[1] - kWeightLog2));
-          const uint32_t c1 = q8_encode2(p0, p1);
-          const float2 d1 = decode2(c1);
-          const uint32_t c2 = q8_encode2((p0 - d1.x) * 16.f, (p1 - d1.y) * 16.f);
-          const float2 d2 = decode2(c2);
-          const float t0 = fmaf(d2.x, kPart2, d1.x), t1 = fmaf(d2.y, kPart2, d1.y);
-          const float g0 = p0 - t0, g1 = p1 - t1;   // what p3 takes, as far as it reaches
-          const uint32_t c3 = q8_encode2(g0 * 65536.f, g1 * 65536.f);
-          constexpr float kReach = 448.f * kPart3;
-          l_acc[0] = fmaf(t0 + fminf(fmaxf(g0, -kReach), kReach), lower, l_acc[0]);
-          l_acc[1] = fmaf(t1 + fminf(fmaxf(g1, -kReach), kReach), lower, l_acc[1]);
+          const uint32_t c1 = encode2_e5m2(p0, p1);
+          const float2 d1 = decode2(c1, __NV_E5M2);
+          const float g0 = p0 - d1.x, g1 = p1 - d1.y;
+          const uint32_t c2 = encode2_e5m2(g0 * (1.f / kPPart2), g1 * (1.f / kPPart2));
+          const float2 d2 = decode2(c2, __NV_E5M2);
+          const uint32_t c3 = encode2_e5m2(fmaf(d2.x, -kPPart2, g0) * (1.f / kPPart3), fmaf(d2.y, -kPPart2, g1) * (1.f / kPPart3));
+          const float2 d3 = decode2(c3, __NV_E5M2);
+          constexpr float u1 = kWeightUnit, u2 = kWeightUnit * kPPart2, u3 = kWeightUnit * kPPart3;
+          // (a weight below the codes' nine bits counts in l as it is: a latent of zero has 2^-100
+          // in P' and may have as much of l as any other)
+          constexpr float kLeast = 1.f / 16384;
+          const float t0 = p0 < kLeast ? p0 * u1 : fmaf(d3.x, u3, fmaf(d2.x, u2, d1.x * u1));
+          const float t1 = p1 < kLeast ? p1 * u1 : fmaf(d3.y, u3, fmaf(d2.y, u2, d1.y * u1));
+          l_acc[0] = fmaf(t0, lower, l_acc[0]);
+          l_acc[1] = fmaf(t1, lower, l_acc[1]);
           *reinterpret_cast<uint16_t*>(prow) = static_cast<uint16_t>(c1);
           *reinterpret_cast<uint16_t*>(prow + 128) = static_cast<uint16_t>(c2);
           *reinterpret_cast<uint16_t*>(prow + 256) = static_cast<uint16_t>(c3);
@@ -587,7 +600,8 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
             tmem_wait_ld();
             const int f = 128 * mc + 32 * quad + lane;
 #pragma unroll
-            for (int i = 0; i < kGroupHeads; ++i) po[i * D_C + f] = fmaf(o[2][i], kPart3, fmaf(o[1][i], kPart2, o[0][i]));
+            for (int i = 0; i < kGroupHeads; ++i)
+              po[i * D_C + f] = kWeightUnit * fmaf(o[2][i], kPPart3, fmaf(o[1][i], kPPart2, o[0][i]));
           }
           tc_fence_before();
           if (quad == 0 && lane < kGroupHeads) {
@@ -595,7 +609,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 #pragma unroll
             for (int ww = 0; ww < kSoftWarps; ++ww) lh += xsum[ww * kGroupHeads + lane];
             float* ml = p.part_ml + (static_cast<size_t>(slot_out) * kHeads + kGroupHeads * g + lane) * 2;
-            ml[0] = m8 - kWeightLog2;
+            ml[0] = m8;
             ml[1] = lh;
           }
           if (p.fuse) {

@@ -54,3 +54,33 @@ def test_queries_of_zero_and_mixed_sizes(gpu_lib, d_c, power):
     assert dc.read_status() == 0
     for h in (0, 1, 2, 3, 15):
         assert apart(got[:, h] * 2.0 ** -power, want[:, h] * 2.0 ** -power) <= 5e-3, h
+
+
+@pytest.mark.parametrize("d_c", [256, 512])
+@pytest.mark.parametrize("drop", [3.0, 9.0, 12.0, 15.0, 17.0])
+def test_small_weights_beside_one_whose_value_is_not_read(gpu_lib, d_c, drop):
+    """One token has all but a share of the weight, and values in features that W_UV does not look at; the others'
+    weights lie about e^-drop below it, spread, and make up the whole output.  (A bf16 weight is off by 2^-9 of itself at
+    most, at any size: the bound is the one of ordinary weights.)"""
+    _, dc = make([6000, 300], d_c, "none", vocab=100, splits=1)
+    half = d_c // 2
+    dc.c_pool[..., :half] = 0
+    dc.w_uv[..., :half] = 0
+    for b in range(2):
+        page = int(dc.block_table[b, 0])
+        dc.c_pool[page, 0, :half] = dc.c_pool[page, 0, half:]
+        dc.c_pool[page, 0, half:] = 0
+    # scores by the RoPE part alone
+    dc.q.zero_()
+    dc.q[..., 128] = 1.0
+    g = torch.Generator(device="cuda").manual_seed(3)
+    s = -drop + torch.randn(dc.kr_pool.shape[:2], generator=g, device="cuda") * 0.5
+    dc.kr_pool.zero_()
+    dc.kr_pool[..., 0] = (s * 192 ** 0.5).to(torch.bfloat16)
+    for b in range(2):
+        dc.kr_pool[int(dc.block_table[b, 0]), 0, 0] = 0
+    cache, back = quantised(dc)
+    got, want = decode_q8(dc, cache), reference64(dc, back)
+    assert dc.read_status() == 0
+    for b in range(2):
+        assert apart(got[b], want[b]) <= 5e-3, b
