@@ -455,8 +455,9 @@ typedef struct {
  *                the sequence's rows of q_out and k_out as they were.  NULL: 0 (not with
  *                cu_seqlens NULL)
  *   tokens       rows of q and k; those from cu_seqlens[batch] on are left as they were
- * Angles are reduced as 64-bit fractions of a turn, which keeps them to 2^-32 of a turn
- * at any position; sums are fp32, rounded once.  16-byte alignment of rows, heads and
+ * Angles are reduced as 64-bit fractions of a turn and kept to 2^-32 of a turn, beside t 2^-50
+ * radians from the frequency, which is a double (with YARN times beta_fast / (beta_fast -
+ * beta_slow)); sums are fp32, rounded once.  16-byte alignment of rows, heads and
  * pointers is not needed but faster.  Device errors: EG_MLA_ERR_OUT_OF_RANGE for
  * cu_seqlens that do not begin at 0 or that decrease.  Rows that belong to no sequence by them
  * are left as they were, and so are those of a sequence whose two offsets are not in order

@@ -94,8 +94,8 @@ __device__ __forceinline__ bool find_position(const Packed& p, int k, int lane, 
 // pair i of a token at position t turns by t f_i: (x, y) -> m (x cos - y sin, x sin + y cos).
 // The angle is a 64-bit fraction of a turn, t times f_i / (2 pi) (rounded to 2^-64 of a turn
 // and, on the host, to a double): an integer product, whose low 64 bits are what is left
-// after whole turns, so that far positions lose nothing and no double precision runs on the
-// GPU.  Sine and cosine are taken in fp32 of what is left to the nearest quarter turn.
+// after whole turns, so that far positions lose no more than the double's rounding and no
+// double precision runs on the GPU.  Sine and cosine are taken in fp32 of what is left to the nearest quarter turn.
 constexpr int kMaxPairs = 128;
 
 struct RopeArgs {
