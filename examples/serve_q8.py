@@ -9,6 +9,7 @@ within its bounds.
     python examples/serve_q8.py [--prompts 300 70 64 1] [--steps 5]
 """
 import argparse
+import math
 import os
 import sys
 
@@ -42,8 +43,10 @@ def main(prompts=(300, 70, 64, 1), steps=5, seed=0):
     B = len(prompts)
     width = max(pages_of(n + steps) for n in prompts)
     pages = sum(pages_of(n + steps) for n in prompts)
-    dims = _lib.make_dims(HEADS, D_NOPE, D_ROPE, D_NOPE, D_C, VOCAB)
-    rope = _lib.make_rope(scaling="yarn", factor=4.0, original_len=4096)
+    # positions four times as far as trained: YaRN's temperature over the whole score, of which rope turns a part
+    temperature = (0.1 * math.log(4.0) + 1.0) ** 2
+    dims = _lib.make_dims(HEADS, D_NOPE, D_ROPE, D_NOPE, D_C, VOCAB, softmax_scale=temperature * (D_NOPE + D_ROPE) ** -0.5)
+    rope = _lib.make_rope(scaling="yarn", factor=4.0, original_len=4096, magnitude=1.0)
     gate = (normal(VOCAB, D_C, std=0.1, mean=1.0), torch.ones(D_C, device="cuda"), torch.zeros(D_C, device="cuda"))
     weights = [normal(HEADS, D_NOPE, D_C, std=D_C ** -0.5) for _ in range(2)]
     c8 = zeros(pages, PAGE, D_C, dtype=torch.uint8).view(torch.float8_e4m3fn)

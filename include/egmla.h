@@ -419,7 +419,15 @@ int eg_mla_decode_sparse(const eg_mla_dims* dims, const void* q, const void* c_p
  *   EG_MLA_ROPE_NTK       theta s^(d_rope / (d_rope - 2)) in place of theta
  *   EG_MLA_ROPE_YARN      f_i ((1 - g) / s + g) with g = (original_len f_i / (2 pi) -
  *                         beta_slow) / (beta_fast - beta_slow) kept within 0 and 1:
- *                         "NTK by parts" (YaRN, arXiv 2309.00071, Section 3.2)
+ *                         "NTK by parts" (YaRN, arXiv 2309.00071, Section 3.2): linear in
+ *                         the turns that a pair makes in the trained context.  (A ramp over
+ *                         the pair's index i instead gives other frequencies: a model
+ *                         trained with that is not served by this one.)
+ * m is 1 unless `magnitude` says otherwise, with YARN 0.1 ln s + 1: the root of the paper's
+ * temperature, which as a factor of q and k raises the whole score by m^2 where the whole
+ * head is rotated (d_nope = 0).  Of heads with a part that is not, it raises the rotated
+ * part's share alone; for the temperature over the whole score set `magnitude` to 1 and
+ * softmax_scale to (0.1 ln s + 1)^2 / sqrt(d_nope + d_rope).
  * `inverse` turns the other way (times m): the transposed matrix, which takes the
  * gradients of the rotated rows to those of q and k.
  */
@@ -440,7 +448,7 @@ typedef struct {
   float factor;          /* s >= 1; ignored for UNSCALED */
   float beta_fast;       /* YARN: <= 0 selects 32 */
   float beta_slow;       /* YARN: <= 0 selects 1; below beta_fast */
-  float magnitude;       /* m; <= 0 selects 1, with YARN 0.1 ln s + 1 */
+  float magnitude;       /* m; <= 0 selects 1, with YARN 0.1 ln s + 1 (see above) */
 } eg_mla_rope_dims;
 
 /*
