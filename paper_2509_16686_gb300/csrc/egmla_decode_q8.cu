@@ -24,10 +24,11 @@
 //             itself below 2^-25 of the largest).
 // The RoPE part stays bf16 (kind::f16) in columns of its own.
 //
-// 128 ragged sequences of 128 to 16K tokens (337 MB) at d_c 512: 76 us a call, 62.8 of them
-// this kernel (5.4 TB/s, 79 % of the copy rate), with the codes widened to bf16 as for the
-// gate 130, over a bf16 cache 112.  It is bound by the page copies: half the score and
-// output MMAs left out, 75 (a fifth slot and two P' buffers instead of four: 78).
+// 128 ragged sequences of 128 to 16K tokens (337 MB) at d_c 512: 76 us a call, 62 to 65 of them
+// this kernel (5.2 to 5.4 TB/s, 77 to 80 % of the copy rate), with the codes widened to bf16 as
+// for the gate 130, over a bf16 cache 113.  It is bound by the page copies: half the score and
+// output MMAs left out, 75 (a fifth slot and two P' buffers instead of four: 78).  8 x 32K at
+// d_c 256: 33.1 us (over bf16 35.4), where no unit is full.
 //
 // Roles as in egmla_decode_tc.cu, but for the gate warps: the softmax, here the longest of
 // all roles, has two groups of four warps, eight heads each, which need nothing of one
