@@ -17,6 +17,7 @@
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -63,15 +64,23 @@ __device__ __forceinline__ int first_of(const Packed& p, int b, int k) {
   return before <= first && first <= k && k < end && end <= behind ? first : -1;
 }
 
-// Reports offsets that do not begin at 0 or that decrease; warp `w` of `warps` looks at its
-// part of them.  (Where the warp goes on to look for its tokens' sequences, it has brought
-// the lines that this needs.)
+// Reports offsets that do not begin at 0 or that decrease; warp w of the grid's `warps` looks at
+// its part of them, of which there are kOffsetsPerLane to a lane at most (offset_blocks).
+// (Where the warp goes on to look for its tokens' sequences, it has brought the lines that
+// this needs.)
+constexpr int kOffsetsPerLane = 2;
 __device__ __forceinline__ void check_offsets(const Packed& p, int w, int warps, int lane) {
   if (p.cu == nullptr) return;
   bool wrong = w == 0 && __ldg(p.cu) != 0;
+#pragma unroll 1
   for (int64_t i = static_cast<int64_t>(w) * 32 + lane; i < p.batch; i += static_cast<int64_t>(warps) * 32)
-    wrong = wrong || __ldg(p.cu + i) > __ldg(p.cu + i + 1);
+    wrong |= __ldg(p.cu + i) > __ldg(p.cu + i + 1);
   if (wrong) report_status(p.status, kStatusOutOfRange);
+}
+// Blocks that this takes: more than the tokens' where there are many empty sequences.
+int offset_blocks(const Packed& p, int warps_per_block) {
+  const int64_t per_block = 32LL * kOffsetsPerLane * warps_per_block;
+  return p.cu == nullptr ? 0 : static_cast<int>((p.batch + per_block - 1) / per_block);
 }
 
 // Position of packed token k, the same in every lane; false for a token of no sequence or of
@@ -215,7 +224,10 @@ __global__ void __launch_bounds__(32 * WARPS, kRopeResident<HALF, WARPS>) rope_k
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = blockIdx.x * WARPS + warp;
   grid_dependency_wait();
-  if (k >= a.tok.tokens) return;
+  if (k >= a.tok.tokens) {
+    if (blockIdx.y == 0) check_offsets(a.tok, k, gridDim.x * WARPS, lane);
+    return;
+  }
   constexpr int kBytes = sizeof(T);
   const int heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
   const int h0 = heads * part / parts, h1 = heads * (part + 1) / parts;
@@ -236,7 +248,7 @@ __global__ void __launch_bounds__(32 * WARPS, kRopeResident<HALF, WARPS>) rope_k
     for (int j = 0; j < kUnroll; ++j, d.next())
       if (d.h < hend) item[j].load(d.h < a.H ? q + d.h * stride + nope : key, d.r, items);
   }
-  if (part == 0) check_offsets(a.tok, k, a.tok.tokens, lane);
+  if (part == 0) check_offsets(a.tok, k, gridDim.x * WARPS, lane);
   int64_t pos;
   if (!find_position(a.tok, k, lane, pos)) return;
   if (nope > 0 && !a.q_in_place && a.q != nullptr) {
@@ -276,8 +288,8 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int k = blockIdx.x * kTokWarps + warp;
   grid_dependency_wait();
+  if (blockIdx.y == 0) check_offsets(a.tok, k, gridDim.x * kTokWarps, lane);
   if (k >= a.tok.tokens) return;
-  if (blockIdx.y == 0) check_offsets(a.tok, k, a.tok.tokens, lane);
   int64_t pos;
   if (!find_position(a.tok, k, lane, pos)) return;
   const int pairs = a.dr / 2, heads = a.H + 1, parts = gridDim.y, part = blockIdx.y;
@@ -311,7 +323,7 @@ __global__ void __launch_bounds__(kTokThreads) rope_any_kernel(const __grid_cons
 constexpr int kRopeWarps = 8;
 template <typename T, int WARPS>
 cudaError_t launch_rope_units(const RopeArgs& a, int parts, cudaStream_t st) {
-  const dim3 grid((a.tok.tokens + WARPS - 1) / WARPS, parts), block(32 * WARPS);
+  const dim3 grid(std::max((a.tok.tokens + WARPS - 1) / WARPS, offset_blocks(a.tok, WARPS)), parts), block(32 * WARPS);
   return a.half ? launch_chained(rope_kernel<T, true, WARPS>, grid, block, 0, st, a)
                 : launch_chained(rope_kernel<T, false, WARPS>, grid, block, 0, st, a);
 }
@@ -326,8 +338,9 @@ cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
   if (want < 2 && a.tok.tokens <= resident / 2) want = 2;
   const int parts = want < a.H + 1 ? want : a.H + 1;
   if (!units)
-    return launch_chained(rope_any_kernel<T>, dim3((a.tok.tokens + kTokWarps - 1) / kTokWarps, parts), dim3(kTokThreads), 0,
-                          st, a);
+    return launch_chained(rope_any_kernel<T>,
+                          dim3(std::max((a.tok.tokens + kTokWarps - 1) / kTokWarps, offset_blocks(a.tok, kTokWarps)), parts),
+                          dim3(kTokThreads), 0, st, a);
   return parts == 1 ? launch_rope_units<T, 1>(a, parts, st) : launch_rope_units<T, kTokWarps>(a, parts, st);
 }
 
@@ -367,7 +380,7 @@ __device__ __forceinline__ int cache_rows(const CacheArgs& a, int k0, int lane) 
     first = !doubt && begin <= k0 + lane && k0 + lane < last ? begin : -1;   // (below 0 too: of no sequence)
   } else if (a.tok.cu != nullptr) {
     // a search for the first token, and for another only where its sequence ends before it
-    check_offsets(a.tok, k0 / T, (a.tok.tokens + T - 1) / T, lane);
+    check_offsets(a.tok, k0 / T, gridDim.x * kTokWarps, lane);
     int found = 0, end = INT32_MIN;
 #pragma unroll
     for (int i = 0; i < T; ++i) {
@@ -438,7 +451,6 @@ template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_constant__ CacheArgs a) {
   const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
   grid_dependency_wait();
-  if (k0 >= a.tok.tokens) return;
   const int units = a.d_c / 8, kru = a.kr_bytes / 16;
   Packed8<E> x[T][TURNS];
 #pragma unroll
@@ -449,6 +461,7 @@ __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_con
       if (k0 + t < a.tok.tokens && lane + 32 * j < units) x[t][j].load(a.c_rows + (k0 + t) * a.c_stride, lane + 32 * j);
     }
   const int row = cache_rows<T>(a, k0, lane);
+  if (k0 >= a.tok.tokens) return;   // (here for the offsets alone)
   float own_scale = 0.f;
 #pragma unroll
   for (int t = 0; t < T; ++t) {
@@ -494,9 +507,9 @@ template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) read_q8_kernel(const __grid_constant__ CacheArgs a) {
   const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
   grid_dependency_wait();
-  if (k0 >= a.tok.tokens) return;
   const int units = a.d_c / 8, kru = a.kr_bytes / 16;
   const int row = cache_rows<T>(a, k0, lane);
+  if (k0 >= a.tok.tokens) return;   // (here for the offsets alone)
   const float own_scale = lane < T && row >= 0 ? __ldg(a.scale + row) : 0.f;
   uint2 w[T][TURNS];
 #pragma unroll
@@ -543,7 +556,8 @@ template <int T, typename F>
 cudaError_t launch_tokens(const CacheArgs& a, cudaStream_t st, F&& kernel) {
   const bool few = a.tok.tokens <= kSms * kTokFew;
   const int per_block = kTokWarps * (few ? 1 : T);
-  return launch_chained(kernel(few), dim3((a.tok.tokens + per_block - 1) / per_block), dim3(kTokThreads), 0, st, a);
+  const int blocks = std::max((a.tok.tokens + per_block - 1) / per_block, offset_blocks(a.tok, kTokWarps));
+  return launch_chained(kernel(few), dim3(blocks), dim3(kTokThreads), 0, st, a);
 }
 template <typename E>
 cudaError_t launch_append_q8(const CacheArgs& a, cudaStream_t st) {

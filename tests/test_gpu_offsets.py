@@ -116,6 +116,41 @@ def test_offsets_of_a_few_sequences(gpu_lib, dtype, bad, kept):
         assert torch.equal(qo[k], alone[k]) if k in where else bool((qo[k] == 9).all())
 
 
+@pytest.mark.parametrize("batch", [300, 5000, 70000])
+def test_a_few_tokens_of_many_sequences(gpu_lib, batch):
+    """The offsets take more warps than the tokens: all of them are looked at, whatever the call's tokens are."""
+    lens = np.zeros(batch, np.int64)
+    lens[[3, batch // 2, batch - 1]] = [1, 2, 1]
+    dims = _lib.make_dims(16, 128, 64, 128, 64, 1000)
+    rd = _lib.make_dims(1, 0, 8, 128, 256, 100, dtype="fp32")
+    odd = _lib.make_dims(1, 1, 6, 128, 256, 100)
+    c, kr, ids = normal((4, 64), "bf16", 1), normal((4, 64), "bf16", 2), ints([10, 11, 12, 13])
+    table, cu = torch.zeros((batch, 1), dtype=torch.int32, device="cuda"), np.asarray(offsets(lens))
+    for k, b in enumerate((3, batch // 2, batch - 1)):
+        table[b, 0] = k
+    want = torch.full((3, 64), -5, dtype=torch.int32, device="cuda")
+    want[0, 0], want[1, 0], want[1, 1], want[2, 0] = 10, 11, 12, 13
+    q, x = normal((4, 1, 8), "fp32", 3), normal((4, 1, 7), "bf16", 4)
+    r = np.random.default_rng(batch)
+    for j in [None, 1, 2, 32, 33, batch // 2 + 1, batch - 1, batch, *r.integers(1, batch + 1, 12)]:
+        bad = cu.copy()
+        if j is not None:
+            bad[j] = -1 if r.integers(2) or j == batch else 9
+        bad = ints(bad)
+        cache, st = Cache(3, 64, "bf16"), [status_word() for _ in range(4)]
+        _lib.eg_mla_append_latent_q8(dims, *cache.all(), c, kr, ids, table, None, bad, st[0])
+        io = torch.full((4,), -9, dtype=torch.int32, device="cuda")
+        full = Cache(3, 64, "bf16")
+        full.ids.copy_(want)
+        _lib.eg_mla_read_latent_q8(dims, *full.all(), table, torch.empty_like(c), None, io, None, bad, st[1])
+        _lib.eg_mla_rope(rd, _lib.make_rope(), q, torch.empty_like(q), None, None, None, bad, st[2])
+        _lib.eg_mla_rope(odd, _lib.make_rope(), x, torch.empty_like(x), None, None, None, bad, st[3])
+        assert [int(s) for s in st] == [0 if j is None else RANGE] * 4, j
+        if j is None:
+            assert torch.equal(cache.ids, want) and io.tolist() == [10, 11, 12, 13]
+        assert either(cache.ids, want, torch.full_like(want, -5)) and either(io, ids, torch.full_like(io, -9)), j
+
+
 def test_good_offsets_report_nothing(gpu_lib):
     """Empty sequences at either end and in between, and tokens behind the last."""
     for lens in ([0, 0, 3], [3, 0, 0], [0] * 40 + [1, 0, 2] + [0] * 40, [1] * 64):
