@@ -569,7 +569,9 @@ def eg_mla_decode_q8(dims: EgMlaDims, q, c8_pool, scale_pool, krope_pool, id_poo
     heads, d_nope, d_v, d_c, mode = dims.num_heads, dims.d_nope, dims.d_v, dims.d_c, dims.gate_mode
     gate = gamma = beta = None
     if mode != EG_MLA_GATE_NONE:
-        gate = None if gate_table is None else _arg(gate_table, (dims.vocab, d_c), dtype, dev, "gate_table")
+        if gate_table is not None:   # (rows behind the vocabulary, as of a padded table, are not read)
+            rows = max(dims.vocab, gate_table.shape[0])
+            gate = _arg(gate_table, (rows, d_c), dtype, dev, "gate_table")
         if mode != EG_MLA_GATE_MUL:
             gamma = None if ln_gamma is None else _arg(ln_gamma, (d_c,), torch.float32, dev, "ln_gamma")
             beta = None if ln_beta is None else _arg(ln_beta, (d_c,), torch.float32, dev, "ln_beta")

@@ -84,7 +84,9 @@ def _lib_argtypes():
 def bad_forms(t, name):
     """(tensor, what the error says) for everything that a tensor can be wrong in here."""
     yield torch.zeros((*t.shape[:-1], t.shape[-1] + 1), dtype=t.dtype), "shape"
-    yield torch.zeros((t.shape[0] + 1, *t.shape[1:]), dtype=t.dtype), "shape"
+    if name != "gate_table":
+        yield torch.zeros((t.shape[0] + 1, *t.shape[1:]), dtype=t.dtype), "shape"
+    yield torch.zeros((t.shape[0] - 1, *t.shape[1:]), dtype=t.dtype), "shape"
     yield t.unsqueeze(0), "shape"
     yield t.to(torch.float16), "expected, got"
     yield t.double(), "expected, got"
@@ -132,6 +134,11 @@ def test_workspace_and_status_words(lib):
             call(good)
         assert len(lib.calls) == 4
         lib.calls.clear()
+
+
+def test_a_padded_gate_table_is_taken(lib):
+    _lib.eg_mla_decode_q8(**dict(arguments(), gate_table=torch.zeros(VOCAB + 14, DC, dtype=BF16)))
+    assert len(lib.calls) == 1
 
 
 def test_what_a_form_does_not_use_is_not_looked_at(lib):
