@@ -444,9 +444,9 @@ __device__ __forceinline__ void store8(uint8_t* row, int unit, const float (&x)[
 
 // A warp per T tokens, eight features of the latent a lane and turn (TURNS of them).  The
 // tokens' rows are requested before their places are looked up, a chain of three
-// dependent loads that T tokens share.  32,768 tokens at d_c 256 (34 MB): 8.7 us from L2, 12.1
-// cold (2.8 TB/s); from L2 with one token a warp 13.1, two 9.9, eight 10.8.  Nine blocks of
-// four warps an SM: a wave and a half, each of whose warps asks for its k^R rows last.
+// dependent loads that T tokens share.  32,768 tokens at d_c 256 (34 MB): 8.6 us from L2, 12.1
+// cold (2.8 TB/s); from L2 with one token a warp 13.1, two 9.9, eight 10.8.  Ten blocks of
+// four warps an SM: more than a wave, each of whose warps asks for its k^R rows last.
 template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_constant__ CacheArgs a) {
   const int lane = threadIdx.x & 31, k0 = (blockIdx.x * kTokWarps + (threadIdx.x >> 5)) * T;
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kTokThreads) append_q8_kernel(const __grid_con
   }
 }
 
-// A warp per T tokens, likewise.  85K tokens at d_c 256 (66 MB): 13.3 us, 5.0 TB/s, with one
+// A warp per T tokens, likewise.  85K tokens at d_c 256 (66 MB): 13.2 us, 5.0 TB/s, with one
 // token a warp 21.1, two 16.1, eight 16.3 (their last wave is nearly empty).
 template <typename E, int T, int TURNS>
 __global__ void __launch_bounds__(kTokThreads) read_q8_kernel(const __grid_constant__ CacheArgs a) {
